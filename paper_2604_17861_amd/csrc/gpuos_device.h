@@ -3215,9 +3215,7 @@ struct WorkShared {
 // A pointer known to address device or host memory, read from LDS: accessed as such, not with flat instructions.
 template <class T> DEV T* global_ptr(T* p) { return (T*)(__attribute__((address_space(1))) T*)p; }
 
-DEV uint64_t uni64(uint64_t v) {
-  return ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32) | __builtin_amdgcn_readfirstlane((uint32_t)v);
-}
+DEV uint64_t uni64(uint64_t v) { return (uint64_t)(__UINTPTR_TYPE__)uni_ptr(v); }      // (its halves unsigned: the builtin's result is an int, which would be extended by its sign)
 DEV uint64_t lane64(uint64_t v, uint32_t lane) {     // `lane` the same in every lane
   return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), (int)lane) << 32) |
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, (int)lane);
