@@ -81,7 +81,9 @@ enum gpuos_status {
 };
 
 /* ---- element types ------------------------------------------------------ */
-enum gpuos_dtype { GPUOS_F32 = 0, GPUOS_F16 = 1, GPUOS_BF16 = 2, GPUOS_I32 = 3 };
+enum gpuos_dtype { GPUOS_F32 = 0, GPUOS_F16 = 1, GPUOS_BF16 = 2, GPUOS_I32 = 3,
+                   GPUOS_I8 = 4, GPUOS_E4M3 = 5 };   /* the last two: the values of a quantised cache (gpuos_model_task) only;
+                                                        E4M3 is the OCP format without infinities (largest 448) */
 
 /* ---- built-in device implementations an operator-table entry can name -----
  * (operator library, paper Section 5.2: elementwise add / mul / ReLU / GELU and
@@ -123,7 +125,10 @@ enum gpuos_impl {
   GPUOS_IMPL_FAIL = 16,
   GPUOS_IMPL_SOFTMAX_LAST = 17, GPUOS_IMPL_MASKED_SOFTMAX_LAST = 18,
   GPUOS_IMPL_LAYERNORM_LAST = 19,
-  GPUOS_IMPL_COUNT = 20
+  /* model operators (gpuos_model_task, below) */
+  GPUOS_IMPL_NORM_ROPE = 20, GPUOS_IMPL_NORM_ROPE_GRAD = 21, GPUOS_IMPL_GAMMA_SUM = 22,
+  GPUOS_IMPL_CACHE_STORE = 23, GPUOS_IMPL_CACHE_LOAD = 24, GPUOS_IMPL_LOGIT_PENALTY = 25,
+  GPUOS_IMPL_COUNT = 26
 };
 
 /* ---- operator programs: operators defined while the worker runs ----------
@@ -219,6 +224,85 @@ typedef struct gpuos_task {
   uint16_t dep[3];                  /* 0 = none; k = wait for ticket (mine - k)     */
   uint16_t reserved[3];
 } gpuos_task;                       /* 328 bytes */
+
+/* ---- model operators -----------------------------------------------------
+ * The memory-bound steps that stand round a model's matrix products (the paper's
+ * operator library, Section 5.2, names rotary embedding and the updating and
+ * compressing of key / value caches): norm and rotation of queries and keys by
+ * head with its backward pass, an 8-bit paged cache, penalties on logits.  They
+ * take more operands than a gpuos_task holds, so they have a descriptor of their
+ * own.  They are bound to logical operators like every implementation
+ * (gpuos_register_op; gpuos_swap_op takes such an operator to GPUOS_IMPL_FAIL and back, to no
+ * other implementation) and run either as tasks of the ring (gpuos_submit_model:
+ * tickets, dependencies, completions, tracing as for any task) or as ordinary
+ * kernels on a stream of the caller's (gpuos_launch_model).
+ * Operands are numbered; an operand that may be left out has ptr NULL then.
+ * Strides are in elements, >= 0 and below 2^32; where "dense" is said the last
+ * dim's stride is 1, and entries past an operand's dims are ignored.  An
+ * output may be the input it is computed from (same pointer, same strides, same
+ * dtype), and must not overlap any operand otherwise; two elements of an output must not share memory.  Float dtypes are
+ * F32, F16, BF16.  Everything is computed in fp32 and rounded to the output's
+ * dtype once.  A size of 0 in B, S, H, L or V is an empty task.
+ *
+ * NORM_ROPE  size = {B, S, H, D, R, places}, 1 <= D <= 512, R even, R <= D; alpha = epsilon
+ *   0 x [B,S,H,D]  1 gamma [D] or none  2 table [places, R], F32, dense (none if R = 0)
+ *   3 positions [B,S], I32 (none: position = index in S)  4 out [B,S,H,D]
+ *   Every head is normalised, y_j = x_j / sqrt(mean(x^2) + epsilon) * gamma_j, and its
+ *   first R elements are rotated in pairs (j, j + R/2), or with GPUOS_FLAG_PAIRS
+ *   (2j, 2j + 1), j < R/2: the first of a pair becomes y c - y' s, the second y' c + y s,
+ *   with c = table[p, j], s = table[p, R/2 + j] of the token's position p.  A position
+ *   outside 0 .. places - 1 makes the token's rows NaN.  (The squares of a row are summed in
+ *   fp32: rows with elements of over 1e18 leave its range.)
+ * NORM_ROPE_GRAD  size = {B, S, H, D, R, places, parts}; operands 0-3 as above,
+ *   4 dx [B,S,H,D]  5 dout [B,S,H,D]  6 partial [D, parts], F32, dense, or none
+ *   The gradient of x, and in column c of `partial` what the c-th of `parts` equal
+ *   shares of the B*S*H heads adds to the gradient of gamma (1 <= parts <= 1024; every column is
+ *   written).  No sum depends on the order in which anything runs.
+ * GAMMA_SUM  size = {D, parts}: 0 partial [D, parts], F32, dense  1 out [D], any float dtype
+ *   Their sum (parts >= 0; no parts: zeros).
+ * CACHE_STORE  size = {B, S, H, D, pages, page, groups}, D <= 512
+ *   0 x [B,S,H,D]  1 slots [B,S], I32  2 cache [pages, page, H, D], I8 or E4M3, dense
+ *   3 scales [pages, page, H, groups], F32
+ *   Row (b, s) is quantised into slot slots[b,s] = page index * page + place in the
+ *   page.  A group is D / groups consecutive elements: D itself or a power of two from 8 on.
+ *   scale = fl(m / qmax), q = rne(fl(x * fl(qmax / m))) with m = max(max |x|, 2^-100) of the group,
+ *   qmax = 127 or 448.  A group with a NaN or an infinity gets q = 0 and a NaN as its
+ *   scale.  A slot that is negative or not in the cache writes nothing.  Slots must be distinct
+ *   (of a slot named twice the cache holds either row, or a mixture of both).
+ * CACHE_LOAD  size = {B, L, H, D, pages, page, groups, width}, D <= 512
+ *   0 cache, 1 scales as above  2 table [B, width], I32: page indexes of each sequence,
+ *   L <= width * page  3 lengths [B], I32 (none: L)  4 out [B,L,H,D]
+ *   out = q * scale for the first lengths[b] rows of sequence b, zeros behind them.  Rows in
+ *   a page that is not in the cache are NaN.
+ * LOGIT_PENALTY  size = {B, V, N}
+ *   0 x [B,V]  1 out [B,V]  2 history [B,N], I32 or none (N = 0)  3 prompt lengths [B], I32, or none (0)
+ *   4 params [B,3], F32: repetition, frequency, presence (none exactly if history is none)
+ *   5 bias [B,V], any float dtype, or none  6 allowed [B, (V + 31) / 32], I32, or none
+ *   v = x; a token anywhere in the history: v = v > 0 ? v / repetition : v * repetition;
+ *   v = v - count * frequency, then v - presence if count > 0, count = its occurrences from the
+ *   prompt's length on; v = v + bias; -inf if bit v % 32 of word v / 32 of `allowed` is 0.
+ *   Entries of the history that are no token (negative, V and above) count for
+ *   nothing.  A row that nothing is allowed in is all -inf.
+ */
+#define GPUOS_FLAG_PAIRS 4u         /* NORM_ROPE, NORM_ROPE_GRAD: neighbours are pairs      */
+#define GPUOS_MAX_OPERANDS 8
+typedef struct gpuos_model_operand {
+  void*   ptr;                      /* device address, a multiple of the element size; NULL: left out */
+  int64_t stride[4];                /* in elements                                      */
+  uint8_t dtype;                    /* enum gpuos_dtype                                 */
+  uint8_t reserved[7];
+} gpuos_model_operand;              /* 48 bytes */
+typedef struct gpuos_model_task {
+  uint16_t op_id;                   /* logical operator id                              */
+  uint8_t  n_operands;              /* the operator's number of operands, those left out included */
+  uint8_t  reserved0;
+  uint32_t flags;                   /* GPUOS_FLAG_FENCE, GPUOS_FLAG_PAIRS               */
+  int64_t  size[8];                 /* as listed above; entries past those are ignored  */
+  gpuos_model_operand operand[GPUOS_MAX_OPERANDS];
+  float    alpha;
+  uint16_t dep[3];                  /* as in gpuos_task                                 */
+  uint16_t reserved[3];
+} gpuos_model_task;                 /* 472 bytes */
 
 /* per-ticket completion record (paper Section 5.3 tracepoint fields: task id,
  * operator-table version; timestamps are host steady_clock nanoseconds) */
@@ -436,6 +520,26 @@ int gpuos_flush(gpuos_ctx* ctx);
  * doorbell covers until its check word holds.  Same arguments, results and blocking behaviour as
  * gpuos_submit. */
 int gpuos_submit_flush(gpuos_ctx* ctx, const gpuos_task* tasks, uint32_t n, uint64_t* out_first_ticket);
+
+/* gpuos_submit for model operators: same arguments, results, ordering and blocking
+ * behaviour; tickets, dependencies (back-distances) and fences count tasks of both
+ * kinds alike.  Publish with gpuos_flush or gpuos_wait. */
+int gpuos_submit_model(gpuos_ctx* ctx, const gpuos_model_task* tasks, uint32_t n, uint64_t* out_first_ticket);
+
+/* The same operators as ordinary kernels on `stream` (a hipStream_t of `device`; NULL: the null
+ * stream), for programs whose other kernels are on that stream: no context, no worker, nothing is
+ * waited for, and the call may be captured into a graph.  impl_of_op: HOST array of
+ * GPUOS_MAX_OPS impl ids, as for gpuos_launch_per_op.  All tasks are checked first; if one is
+ * refused nothing is launched.  Up to eight tasks of one operator that follow each other and do not
+ * depend on an earlier task of their launch (dep, GPUOS_FLAG_FENCE) are one launch and run at the
+ * same time; launches run in order, and a back-distance past the first task is met by the
+ * stream's order. */
+int gpuos_launch_model(int32_t device, const gpuos_model_task* tasks, uint32_t n, const uint32_t* impl_of_op, void* stream);
+
+/* How such a task is run (no GPU needed): out[0] 1 for rows in vectors, 0 element by element, 2 nothing to
+ * do; out[1], out[2] work units and rows (LOGIT_PENALTY: segments of rows) in a unit as a task of the ring;
+ * out[3], out[4] the same as a kernel; out[5] elements of a segment. */
+int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t out[6]);
 
 /* Flush, then block until `ticket` and every earlier ticket completed
  * (GPUOS_ALL: everything submitted).  timeout_ns == 0 uses wait_timeout_ms.

@@ -2879,9 +2879,12 @@ DEV bool rowop_is_other(const RecHead& h) {
   const uint32_t path = h.path();
   return path == PATH_ROW_RAGGED || (path == PATH_ROW_FUSED && h.red_n() > (h.dtype_out() == GPUOS_F32 ? 4096u : 8192u));
 }
-// ... and those of them that the worker runs by exec_away: softmax rows that do not fit the registers
+// ... and those of them that the worker runs by exec_away: softmax rows that do not fit the registers; and model operators
 DEV bool rowop_is_away(const RecHead& h, uint32_t impl) {
   const uint32_t path = h.path();
+#if !defined(__HIPCC_RTC__)
+  if (path == PATH_MODEL) return impl >= GPUOS_IMPL_NORM_ROPE && impl <= GPUOS_IMPL_LOGIT_PENALTY;      // (else it has been killed)
+#endif
   return impl == GPUOS_IMPL_SOFTMAX_LAST && (path == PATH_ROW_RAGGED || path == PATH_ROW_FUSED) && h.red_n() > 16384u;
 }
 template <int POL, int ROP>
@@ -3559,10 +3562,20 @@ __attribute__((not_tail_called)) PATHFN void softmax_away(WorkShared* s_v, uint3
   const uint32_t per = uni(r->chunk), rows = uni(r->numel), begin = (uni((uint32_t)dec[2]) & 0x3ffu) * per;
   softmax_held_rows<POL_COHERENT, DT, RAGGED>(r, begin, rows - begin < per ? rows : begin + per, s->red, tid);
 }
+#if !defined(__HIPCC_RTC__)
+union ModelRecord;
+__attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r, uint32_t chunk, float* s, uint32_t wave);      // gpuos_model_device.h
+#endif
 __attribute__((not_tail_called)) PATHFN void exec_away(WorkShared* s_v, uint32_t wave_v) {
   WorkShared* s = lds_arg(s_v);
   const uint32_t wave = uni(wave_v);
   const Record* r = &s->rec[(uni(s->dec[0]) >> 8) & 0xffu];
+#if !defined(__HIPCC_RTC__)
+  if (uni((uint32_t)r->path) == PATH_MODEL) {
+    exec_model((const ModelRecord*)r, uni(s->dec[2]) & 0x3ffu, s->red, wave);
+    return;
+  }
+#endif
   const uint32_t k = 2u * uni(r->dtype[3]) + (uni(r->path) == PATH_ROW_RAGGED ? 1u : 0u);
   if (k < 2u) { if (k == 0) softmax_away<GPUOS_F32, false>(s, thread_index(wave)); else softmax_away<GPUOS_F32, true>(s, thread_index(wave)); }
   else if (k < 4u) { if (k == 2) softmax_away<GPUOS_F16, false>(s, thread_index(wave)); else softmax_away<GPUOS_F16, true>(s, thread_index(wave)); }

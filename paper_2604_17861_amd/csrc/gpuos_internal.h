@@ -33,7 +33,8 @@ enum Path : uint8_t {
                          // slices, row and column vectors, mixed dtypes): gathered through LDS
   PATH_ROWS = 10,        // <= 3 outer dims of any strides over rows that are contiguous in every operand
                          // (or one scalar per row): slices, head splits, casts, any row length or alignment
-  PATH_ROW_RAGGED = 11   // as PATH_ROW_FUSED, rows of any length from one vector on and any alignment
+  PATH_ROW_RAGGED = 11,  // as PATH_ROW_FUSED, rows of any length from one vector on and any alignment
+  PATH_MODEL = 12        // a model operator: the record's body is one of those in gpuos_model.h
 };
 
 enum RecFlag : uint8_t {

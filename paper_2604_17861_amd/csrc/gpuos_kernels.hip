@@ -30,6 +30,7 @@
 #include "../../include/gpuos.h"
 #include "gpuos_internal.h"
 #include "gpuos_device.h"
+#include "gpuos_model_device.h"
 
 namespace gpuos {
 

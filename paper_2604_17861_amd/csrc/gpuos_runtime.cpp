@@ -16,6 +16,7 @@
 #include <new>
 #include <string>
 #include <thread>
+#include <type_traits>
 #include <vector>
 
 #include <immintrin.h>
@@ -25,6 +26,7 @@
 
 #include "../../include/gpuos.h"
 #include "gpuos_internal.h"
+#include "gpuos_model.h"
 
 using namespace gpuos;
 
@@ -133,7 +135,9 @@ bool impl_is_reduction(uint32_t impl) {
 bool impl_is_rowop(uint32_t impl) {
   return impl == GPUOS_IMPL_SOFTMAX_LAST || impl == GPUOS_IMPL_MASKED_SOFTMAX_LAST || impl == GPUOS_IMPL_LAYERNORM_LAST;
 }
-int impl_kind(uint32_t impl) { return impl_is_reduction(impl) ? 1 : (impl_is_rowop(impl) ? 2 : 0); }
+// (model operators: a kind each, their descriptors differ)
+int impl_kind(uint32_t impl) { return impl_is_reduction(impl) ? 1 : (impl_is_rowop(impl) ? 2 : (impl_is_model(impl) ? 3 + (int)impl : 0)); }
+uint32_t op_family(uint32_t impl) { return impl == GPUOS_IMPL_FAIL ? 0u : (impl_is_model(impl) ? impl : 1u); }
 bool impl_takes_int(uint32_t impl) {
   return impl == GPUOS_IMPL_ADD || impl == GPUOS_IMPL_SUB || impl == GPUOS_IMPL_MUL ||
          impl == GPUOS_IMPL_COPY || impl_is_reduction(impl);
@@ -809,10 +813,13 @@ uint32_t weighted_sum(const Record& rec) {
 struct OpInfo {
   uint32_t impl = 0;
   uint32_t version = 0;            // 0 = unregistered
+  uint32_t family = 0;             // what its tasks' descriptors are: op_family() of the implementations it has been bound to (0: only FAIL so far)
   uint64_t prev_swap_head = 0;     // tickets submitted before the previous swap returned
 };
 
 }  // namespace
+
+int gpuos::hip_status(int e, const char* what) { return hip_ok((hipError_t)e, what) ? GPUOS_OK : GPUOS_E_HIP; }
 
 struct gpuos_ctx {
   gpuos_config cfg;
@@ -1704,6 +1711,7 @@ int gpuos_register_op(gpuos_ctx* c, uint32_t op_id, uint32_t impl_id, uint32_t* 
   if (c->ops[op_id].version != 0) return GPUOS_E_INVAL;            // already bound: use swap_op
   if (!c->worker_running && !c->worker_joined) return GPUOS_E_DEAD;   // a stopped worker reads the table when it is started again
   OpInfo& o = c->ops[op_id];
+  o.family = op_family(impl_id);
   __atomic_store_n(&o.impl, impl_id, __ATOMIC_RELAXED);
   __atomic_store_n(&o.version, 1u, __ATOMIC_RELEASE);
   o.prev_swap_head = 0;
@@ -1727,6 +1735,9 @@ int gpuos_swap_op(gpuos_ctx* c, uint32_t op_id, uint32_t impl_id, uint32_t* out_
   if (impl_id != GPUOS_IMPL_FAIL && o.impl != GPUOS_IMPL_FAIL &&
       (ctx_impl_arity(c, impl_id) != ctx_impl_arity(c, o.impl) || impl_kind(impl_id) != impl_kind(o.impl)))
     return GPUOS_E_INVAL;
+  // A record that was packed for one kind of descriptor is never run as another's, whatever stood between (FAIL).
+  const uint32_t family = op_family(impl_id);
+  if (family != 0 && o.family != 0 && family != o.family) return GPUOS_E_INVAL;
   // The inactive slot still holds version-1's predecessor.  A task can only hold
   // that entry if it was submitted before the previous swap returned: wait for those.
   if (o.prev_swap_head > c->floor.load(std::memory_order_acquire)) {
@@ -1735,6 +1746,7 @@ int gpuos_swap_op(gpuos_ctx* c, uint32_t op_id, uint32_t impl_id, uint32_t* out_
     if (rc != GPUOS_OK) return rc;
   }
   const uint32_t v = o.version + 1;
+  if (family != 0) o.family = family;
   __atomic_store_n(&c->htable[op_id].slot[v & 1u], pack_entry(impl_id, v), __ATOMIC_RELAXED);  // inactive slot
   if (c->push) _mm_sfence();                 // write-combined stores: the slot before the version
   __atomic_store_n(&c->htable[op_id].version, v, __ATOMIC_RELEASE);                           // flip
@@ -1747,14 +1759,19 @@ int gpuos_swap_op(gpuos_ctx* c, uint32_t op_id, uint32_t impl_id, uint32_t* out_
   return GPUOS_OK;
 }
 
+extern "C++" {
 namespace {
-int submit_impl(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out_first_ticket, bool publish);
+template <class TASK> int submit_impl(gpuos_ctx* c, const TASK* tasks, uint32_t n, uint64_t* out_first_ticket, bool publish);
+}
 }
 int gpuos_submit(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out_first_ticket) {
   return submit_impl(c, tasks, n, out_first_ticket, false);
 }
 int gpuos_submit_flush(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out_first_ticket) {
   return submit_impl(c, tasks, n, out_first_ticket, true);
+}
+int gpuos_submit_model(gpuos_ctx* c, const gpuos_model_task* tasks, uint32_t n, uint64_t* out_first_ticket) {
+  return submit_impl(c, tasks, n, out_first_ticket, false);
 }
 namespace {
 // The implementation that an operator id is bound to (GPUOS_IMPL_NONE: none).
@@ -1843,7 +1860,20 @@ bool submit_in_batches(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, Record
   return true;
 }
 
-int submit_impl(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out_first_ticket, bool publish) {
+extern "C++" {
+// One descriptor of either kind, packed for the ring.
+inline int pack_any(const gpuos_ctx* c, const gpuos_task& t, uint32_t impl, Record* r, int program_arity) {
+  return pack_task(t, impl, r, c->cfg.chunk_elems, program_arity);
+}
+inline int pack_any(const gpuos_ctx*, const gpuos_model_task& t, uint32_t impl, Record* r, int) {
+  ModelRecord m;
+  const int rc = ModelPack::pack(t, impl, &m, kRingCut);
+  if (rc == GPUOS_OK) std::memcpy(r, &m, sizeof(*r));
+  return rc;
+}
+
+template <class TASK> int submit_impl(gpuos_ctx* c, const TASK* tasks, uint32_t n, uint64_t* out_first_ticket, bool publish) {
+  constexpr bool kModel = std::is_same<TASK, gpuos_model_task>::value;      // (runs and the way by batches are for small tasks)
   if (!c || (!tasks && n)) return GPUOS_E_INVAL;
   if (!c->worker_running || worker_exited(c)) return GPUOS_E_DEAD;
   MarkerRange mr(c->cfg.markers != 0, "gpuos_submit %llu tasks", n);
@@ -1861,38 +1891,40 @@ int submit_impl(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out
   } catch (const std::bad_alloc&) {                             // no exception may cross the C boundary
     return GPUOS_E_NOMEM;
   }
-  if (publish && n > 2 * kDispatchBatch && !c->cfg.nonblocking_submit) {
-    int rc = GPUOS_OK;
-    if (submit_in_batches(c, tasks, n, staged.data(), out_first_ticket, &rc)) return rc;
+  if constexpr (!kModel) {
+    if (publish && n > 2 * kDispatchBatch && !c->cfg.nonblocking_submit) {
+      int rc = GPUOS_OK;
+      if (submit_in_batches(c, tasks, n, staged.data(), out_first_ticket, &rc)) return rc;
+    }
   }
   LinkRun run;
   uint32_t summed = 0;
   for (uint32_t i = 0; i < n; ++i) {
-    const gpuos_task& t = tasks[i];
+    const TASK& t = tasks[i];
     uint32_t impl = GPUOS_IMPL_NONE;
     if (t.op_id < GPUOS_MAX_OPS && __atomic_load_n(&c->ops[t.op_id].version, __ATOMIC_ACQUIRE) != 0)
       impl = __atomic_load_n(&c->ops[t.op_id].impl, __ATOMIC_RELAXED);
     int rc;
     if (impl == GPUOS_IMPL_NONE) {
       if (!c->cfg.defer_op_check) return GPUOS_E_BADOP;
-      rc = pack_task(t, GPUOS_IMPL_FAIL, &staged[i], c->cfg.chunk_elems);   // the device reports the bad op id
+      rc = pack_any(c, t, GPUOS_IMPL_FAIL, &staged[i], 0);        // the device reports the bad op id
     } else {
       // a program's arity was stored before its id could be bound to any operator
       const int pa = impl >= GPUOS_IMPL_PROGRAM_BASE ? (int)c->prog_arity[(impl - GPUOS_IMPL_PROGRAM_BASE) % GPUOS_MAX_PROGRAMS] : 0;
-      rc = pack_task(t, impl, &staged[i], c->cfg.chunk_elems, pa);
+      rc = pack_any(c, t, impl, &staged[i], pa);
     }
     if (rc != GPUOS_OK) return rc;
     for (int k = 0; k < 3; ++k)
       if (t.dep[k] >= c->cap) return GPUOS_E_INVAL;
     staged[i].ticket = 0;
-    if (i != 0 && !run.links(staged[i - 1], staged[i])) {
-      run.close(&staged[i]);
+    if (i != 0 && (kModel || !run.links(staged[i - 1], staged[i]))) {
+      if (!kModel) run.close(&staged[i]);
       // The part of the check word that does not depend on the ticket: the weighted sum of the
       // other 63 words, with the record's ticket field zero (the ticket enters through the seed only).
       for (; summed < i; ++summed) staged[summed].check = weighted_sum(staged[summed]);
     }
   }
-  run.close(staged.data() + n);
+  if (!kModel) run.close(staged.data() + n);
   for (; summed < n; ++summed) staged[summed].check = weighted_sum(staged[summed]);
   // pass 2 (one producer at a time): reserve n consecutive tickets and write the records
   std::unique_lock<SpinMutex> lk(c->prod_mu);
@@ -1950,6 +1982,7 @@ int submit_impl(gpuos_ctx* c, const gpuos_task* tasks, uint32_t n, uint64_t* out
   handed_out(c, head);
   return GPUOS_OK;
 }
+}  // extern "C++"
 }  // namespace
 
 int gpuos_flush(gpuos_ctx* c) {

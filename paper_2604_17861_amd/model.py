@@ -1,0 +1,360 @@
+"""Model operators on PyTorch tensors: the memory-bound steps that stand round a model's matrix products.
+
+    q, k = norm_rope_qk(q, k, gamma_q, gamma_k, table, positions)      # norm of every head and rotation, differentiable
+    cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales)  # into a paged cache of 8-bit values
+    k, v = cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, dtype=q.dtype)
+    x = penalize_logits(x, history=tokens, params=params, allowed=bits)
+
+The functions launch the library's kernels on PyTorch's current stream of the tensors' device (gpuos_launch_model): they
+wait for nothing, and may be captured into a graph.  The `*_task` functions make the descriptors that the functions
+launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as tasks of the ring (bind the operators with
+`register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  include/gpuos.h says what every operator computes and takes.
+
+Shapes: rows of heads are [T, H, D] or [B, S, H, D] of any strides, with one position, slot or length for each token or
+sequence.  int32 is the only integer type.  Everything here is checking of shapes and marshalling.
+"""
+import struct
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import runtime as R
+from . import streams as S
+
+_FLOAT = {torch.float32: S.F32, torch.float16: S.F16, torch.bfloat16: S.BF16}
+_DT = dict(_FLOAT)
+_DT.update({torch.int32: S.I32, torch.int8: 4, torch.float8_e4m3fn: 5})
+_CACHE = (torch.int8, torch.float8_e4m3fn)
+FLAG_PAIRS = 4
+PARTS_MAX = 1024
+# struct gpuos_model_task: header, size[8], operand[8] as {ptr, stride[4], dtype, pad}, alpha, dep[3], pad
+_TASK = struct.Struct("<HBBI8q" + "Q4qB7x" * 8 + "f3H6x")
+assert _TASK.size == S.MODEL_TASK_BYTES
+_NONE = (0, 0, 0, 0, 0, 0)
+_PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())
+
+
+def register(rt):
+    """Bind the model operators of `streams.MODEL_OP` on a Runtime."""
+    for name, impl in S.MODEL_IMPL.items():
+        rt.register_op(S.MODEL_OP[name], impl)
+
+
+def launch(*tasks, device=None):
+    """Descriptors as kernels on the current stream of `device` (None: the current device)."""
+    stream = torch.cuda.current_stream(device)
+    R.launch_model(tasks[0] if len(tasks) == 1 else b"".join(tasks), stream.device_index, stream.cuda_stream)
+
+
+def _launch_some(rows, tasks):
+    """launch, without the tasks that have nothing to do (an empty tensor has no address)."""
+    tasks = [t for x, t in zip(rows, tasks) if x.numel() != 0]
+    if tasks:
+        launch(*tasks, device=rows[0].device)
+
+
+# ---- descriptors -----------------------------------------------------------------------------------
+
+def _operand(t):
+    """{ptr, stride[4], dtype} of a tensor of at most four dims, or of none."""
+    if t is None:
+        return _NONE
+    st = t.stride()
+    return (t.data_ptr(), *st, *_PAD[len(st)], _DT[t.dtype])
+
+
+def _rows(t):
+    """Rows of heads as [B, S, H, D]: sizes, and {ptr, stride[4], dtype}."""
+    sh, st = t.shape, t.stride()
+    if len(sh) == 4:
+        return sh, (t.data_ptr(), *st, _DT[t.dtype])
+    return (1, *sh), (t.data_ptr(), 0, *st, _DT[t.dtype])
+
+
+def _tokens(t, four):
+    """A number for each token, [B, S] like the rows it belongs to."""
+    st = t.stride()
+    if len(st) == 1:                                        # (one sequence; or the same numbers for every one)
+        return (t.data_ptr(), 0, st[0], 0, 0, _DT[t.dtype])
+    return (t.data_ptr(), *st, 0, 0, _DT[t.dtype])
+
+
+def _pack(name, flags, sizes, operands, alpha=0.0, deps=()):
+    n, fill = len(operands), []
+    for o in operands:
+        fill += o
+    return _TASK.pack(S.MODEL_OP[name], n, 0, flags, *sizes, *(0,) * (8 - len(sizes)), *fill, *_NONE * (8 - n), alpha, *deps,
+                      *(0,) * (3 - len(deps)))
+
+
+def _need(ok, what, *args):
+    if not ok:
+        raise ValueError(what % args if args else what)
+
+
+def _check(x, what, dtypes=None, dims=None, shape=None, device=None, dense=False):
+    if not isinstance(x, torch.Tensor) or (device is None and x.device.type != "cuda") or (device is not None and x.device != device):
+        raise ValueError("%s is a tensor on %s" % (what, device if device is not None else "a GPU"))
+    if dtypes is not None and x.dtype not in dtypes:
+        raise ValueError("%s is one of %s, not %s" % (what, ", ".join(str(d) for d in dtypes), x.dtype))
+    if dims is not None and x.dim() not in dims:
+        raise ValueError("%s has %s dims, not %d" % (what, " or ".join(map(str, dims)), x.dim()))
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError("%s is %s, not %s" % (what, list(shape), list(x.shape)))
+    if x.is_neg() or x.is_conj():
+        raise ValueError("%s is a lazily negated view" % what)
+
+
+_INT = (torch.int32,)
+_F32 = (torch.float32,)
+
+
+def _check_rope(x, gamma, table, positions, out):
+    _check(x, "x", _FLOAT, (3, 4))
+    dev, sh = x.device, x.shape
+    _check(out, "out", _FLOAT, None, sh, dev)
+    if gamma is not None:
+        _check(gamma, "gamma", _FLOAT, None, sh[-1:], dev)
+    if table is not None:
+        _check(table, "table", _F32, (2,), None, dev)
+        if positions is not None:
+            _check(positions, "positions", _INT, (1, 2), None, dev)
+            ps = tuple(positions.shape)
+            _need(ps == tuple(sh[:-2]) or (len(sh) == 4 and ps == (sh[1],)), "positions are %s for x %s", list(sh[:-2]), list(sh))
+    else:
+        _need(positions is None, "positions without a table")
+
+
+def _rope_operands(x, gamma, table, positions, out):
+    sizes, xo = _rows(x)
+    rot, places = (table.shape[1], table.shape[0]) if table is not None else (0, 0)
+    return ((*sizes, rot, places), (xo, _operand(gamma), _operand(table), _NONE if positions is None else _tokens(positions, len(x.shape) == 4),
+                                    _rows(out)[1]))
+
+
+def norm_rope_task(x, gamma, table, positions, out, *, eps=1e-6, pairs=False, deps=(), fence=False):
+    """NORM_ROPE: every head of x normalised, its first table.shape[1] elements rotated, into out."""
+    _check_rope(x, gamma, table, positions, out)
+    sizes, ops = _rope_operands(x, gamma, table, positions, out)
+    return _pack("NORM_ROPE", (FLAG_PAIRS if pairs else 0) | fence, sizes, ops, eps, deps)
+
+
+def norm_rope_grad_task(dout, x, gamma, table, positions, dx, partial, *, eps=1e-6, pairs=False, deps=(), fence=False):
+    """NORM_ROPE_GRAD: the gradient of x into dx, shares of gamma's gradient into the columns of partial [D, parts] (or None)."""
+    _check_rope(x, gamma, table, positions, dx)
+    _check(dout, "dout", _FLOAT, None, x.shape, x.device)
+    if partial is not None:
+        _check(partial, "partial", _F32, (2,), None, x.device)
+        _need(partial.shape[0] == x.shape[-1], "partial has a row for each of %d elements", x.shape[-1])
+    sizes, ops = _rope_operands(x, gamma, table, positions, dx)
+    return _pack("NORM_ROPE_GRAD", (FLAG_PAIRS if pairs else 0) | fence, (*sizes, partial.shape[1] if partial is not None else 0),
+                 (*ops, _rows(dout)[1], _operand(partial)), eps, deps)
+
+
+def gamma_sum_task(partial, out, *, deps=(), fence=False):
+    """GAMMA_SUM: the sums of partial's rows into out [D]."""
+    _check(partial, "partial", _F32, (2,))
+    _check(out, "out", _FLOAT, None, partial.shape[:1], partial.device)
+    return _pack("GAMMA_SUM", int(fence), tuple(partial.shape), (_operand(partial), _operand(out)), 0.0, deps)
+
+
+def _check_cache(x, what, cache, scales):
+    _check(x, what, _FLOAT, (3, 4))
+    dev = x.device
+    _check(cache, "cache", _CACHE, (4,), None, dev)
+    _check(scales, "scales", _F32, (4,), None, dev)
+    _need(cache.shape[2:] == x.shape[-2:], "cache is [pages, page, %d, %d], not %s", *x.shape[-2:], list(cache.shape))
+    _need(scales.shape[:3] == cache.shape[:3] and scales.shape[3] >= 1 and x.shape[-1] % scales.shape[3] == 0,
+          "scales are [pages, page, heads, groups] of the cache %s, not %s", list(cache.shape), list(scales.shape))
+
+
+def cache_store_task(x, slots, cache, scales, *, deps=(), fence=False):
+    """CACHE_STORE: rows of x quantised into the slots of a cache [pages, page, H, D] and its scales [pages, page, H, groups]."""
+    _check_cache(x, "x", cache, scales)
+    _check(slots, "slots", _INT, None, x.shape[:-2], x.device)
+    sizes, xo = _rows(x)
+    return _pack("CACHE_STORE", int(fence), (*sizes, cache.shape[0], cache.shape[1], scales.shape[3]),
+                 (xo, _tokens(slots, False), _operand(cache), _operand(scales)), 0.0, deps)
+
+
+def cache_load_task(cache, scales, pages, lengths, out, *, deps=(), fence=False):
+    """CACHE_LOAD: sequences of a cache by their page tables [B, width] into out [B, L, H, D]."""
+    _check_cache(out, "out", cache, scales)
+    _need(out.dim() == 4, "out is [B, L, H, D]")
+    _check(pages, "pages", _INT, (2,), None, out.device)
+    _need(pages.shape[0] == out.shape[0], "pages has a row for each of %d sequences", out.shape[0])
+    _need(out.shape[1] <= pages.shape[1] * cache.shape[1], "%d pages of %d do not hold %d rows", pages.shape[1], cache.shape[1], out.shape[1])
+    if lengths is not None:
+        _check(lengths, "lengths", _INT, None, out.shape[:1], out.device)
+    return _pack("CACHE_LOAD", int(fence), (*out.shape, cache.shape[0], cache.shape[1], scales.shape[3], pages.shape[1]),
+                 (_operand(cache), _operand(scales), _operand(pages), _operand(lengths), _rows(out)[1]), 0.0, deps)
+
+
+def penalty_task(x, out, history=None, prompt_lengths=None, params=None, bias=None, allowed=None, *, deps=(), fence=False):
+    """LOGIT_PENALTY on x [B, V] into out.  history [B, N]; params [B, 3]: repetition, frequency, presence; bias [V] or
+    [B, V]; allowed [(V + 31) // 32] or [B, that]: bits."""
+    _check(x, "x", _FLOAT, (2,))
+    b, v = x.shape
+    dev = x.device
+    _check(out, "out", _FLOAT, None, x.shape, dev)
+    _need((history is None) == (params is None), "history and params go together")
+    n = 0
+    if history is not None:
+        _check(history, "history", _INT, (2,), None, dev)
+        _need(history.shape[0] == b, "history has a row for each of %d", b)
+        _check(params, "params", _F32, None, (b, 3), dev)
+        n = history.shape[1]
+        if n == 0:                                          # (nothing is counted: as without one)
+            history = params = prompt_lengths = None
+    if prompt_lengths is not None:
+        _need(history is not None, "prompt_lengths without a history")
+        _check(prompt_lengths, "prompt_lengths", _INT, None, (b,), dev)
+
+    def row(t, width, what, dtypes):
+        if t is None:
+            return _NONE
+        _check(t, what, dtypes, (1, 2), (width,) if t.dim() == 1 else (b, width), dev)
+        return (t.data_ptr(), 0, t.stride(0), 0, 0, _DT[t.dtype]) if t.dim() == 1 else _operand(t)
+    return _pack("LOGIT_PENALTY", int(fence), (b, v, n),
+                 (_operand(x), _operand(out), _operand(history), _operand(prompt_lengths), _operand(params), row(bias, v, "bias", _FLOAT),
+                  row(allowed, (v + 31) // 32, "allowed", _INT)), 0.0, deps)
+
+
+# ---- norm and rotation -----------------------------------------------------------------------------
+
+def _parts(x):
+    """Shares of gamma's gradient: as many as there are passes of a workgroup (16 rows of 128), at most PARTS_MAX."""
+    rows = x.numel() // x.shape[-1]
+    return min(PARTS_MAX, max(1, rows // 16))
+
+
+def _empty_like(x):
+    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+class _NormRope(torch.autograd.Function):
+    """Any number of tensors with their gammas, rotated by one table: x0, gamma0, x1, gamma1, ..."""
+
+    @staticmethod
+    def forward(ctx, table, positions, eps, pairs, *xs):
+        ctx.save_for_backward(table, positions, *xs)
+        ctx.eps, ctx.pairs = eps, pairs
+        return _norm_rope(xs[0::2], xs[1::2], table, positions, eps, pairs, [None] * (len(xs) // 2))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *douts):
+        table, positions, *xs = ctx.saved_tensors
+        dxs, dgs = _norm_rope_backward(douts, xs[0::2], xs[1::2], table, positions, ctx.eps, ctx.pairs)
+        return (None, None, None, None, *(g for pair in zip(dxs, dgs) for g in pair))
+
+
+def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
+    outs = [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
+    _launch_some(xs, [norm_rope_task(x, g, table, positions, o, eps=eps, pairs=pairs) for x, g, o in zip(xs, gammas, outs)])
+    return tuple(outs)
+
+
+def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
+    dxs, dgs, tasks, sums, partials = [], [], [], [], []       # (descriptors keep no memory: partials live until the launch)
+    for dout, x, gamma in zip(douts, xs, gammas):
+        dx = _empty_like(x)
+        dg = partial = None
+        if gamma is not None:
+            if x.numel() == 0:
+                dg = torch.zeros_like(gamma)
+            else:
+                dg = _empty_like(gamma)
+                partial = torch.empty((x.shape[-1], _parts(x)), dtype=torch.float32, device=x.device)
+                partials.append(partial)
+                sums.append(gamma_sum_task(partial, dg))
+        if x.numel() != 0:
+            tasks.append(norm_rope_grad_task(dout, x, gamma, table, positions, dx, partial, eps=eps, pairs=pairs))
+        dxs.append(dx)
+        dgs.append(dg)
+    if tasks:
+        launch(*tasks, *sums, device=xs[0].device)
+    return dxs, dgs
+
+
+def _differentiable(xs, outs):
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in xs):
+        return False
+    _need(all(o is None for o in outs), "out does not go with gradients")
+    return True
+
+
+def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=False, out=None):
+    """Root-mean-square norm of every head of x [T, H, D] or [B, S, H, D] over D, times gamma [D], and the rotation of its
+    first R elements by the angles of table [places, R] (cosines | sines, float32) at the tokens' positions (None: 0, 1, ...
+    in every sequence); pairs: neighbours are rotated together, else the halves.  Differentiable in x and gamma."""
+    if _differentiable((x, gamma), (out,)):
+        return _NormRope.apply(table, positions, eps, pairs, x, gamma)[0]
+    return _norm_rope((x,), (gamma,), table, positions, eps, pairs, (out,))[0]
+
+
+def norm_rope_qk(q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *, eps=1e-6, pairs=False, out=(None, None)):
+    """norm_rope of queries and keys in one launch: (q', k')."""
+    if _differentiable((q, k, gamma_q, gamma_k), out):
+        return _NormRope.apply(table, positions, eps, pairs, q, gamma_q, k, gamma_k)
+    return _norm_rope((q, k), (gamma_q, gamma_k), table, positions, eps, pairs, out)
+
+
+def norm_rope_backward(dout, x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=False):
+    """Gradients of norm_rope for x and gamma (None without one)."""
+    (dx,), (dg,) = _norm_rope_backward((dout,), (x,), (gamma,), table, positions, eps, pairs)
+    return dx, dg
+
+
+def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *, eps=1e-6, pairs=False):
+    """Gradients of norm_rope_qk for q, k, gamma_q and gamma_k, in two launches."""
+    (gq, gk), (ggq, ggk) = _norm_rope_backward((dq, dk), (q, k), (gamma_q, gamma_k), table, positions, eps, pairs)
+    return gq, gk, ggq, ggk
+
+
+# ---- the cache -------------------------------------------------------------------------------------
+
+def cache_store(x, slots, cache, scales):
+    """Quantise rows of x [T, H, D] (or [B, S, H, D]) into slots (page index * page + place; negative: nowhere) of cache
+    [pages, page, H, D] (int8 or float8_e4m3fn) and scales [pages, page, H, groups] (float32).  Slots are distinct."""
+    _launch_some((x,), (cache_store_task(x, slots, cache, scales),))
+
+
+def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
+    """cache_store of keys and values in one launch."""
+    _launch_some((k, v), (cache_store_task(k, slots, k_cache, k_scales), cache_store_task(v, slots, v_cache, v_scales)))
+
+
+def _load_out(cache, pages, length, dtype, out):
+    if out is not None:
+        return out
+    _check(cache, "cache", _CACHE, (4,))
+    _check(pages, "pages", _INT, (2,), None, cache.device)
+    return torch.empty((pages.shape[0], length, *cache.shape[2:]), dtype=dtype, device=cache.device)
+
+
+def cache_load(cache, scales, pages, lengths, length, *, dtype=torch.float32, out=None):
+    """The first lengths[b] rows (None: all `length`) of every sequence b, through pages [B, width], as [B, length, H, D];
+    zeros behind them."""
+    out = _load_out(cache, pages, length, dtype, out)
+    _launch_some((out,), (cache_load_task(cache, scales, pages, lengths, out),))
+    return out
+
+
+def cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, length, *, dtype=torch.float32, out=(None, None)):
+    """cache_load of keys and values in one launch: (k, v)."""
+    k, v = _load_out(k_cache, pages, length, dtype, out[0]), _load_out(v_cache, pages, length, dtype, out[1])
+    _launch_some((k, v), (cache_load_task(k_cache, k_scales, pages, lengths, k), cache_load_task(v_cache, v_scales, pages, lengths, v)))
+    return k, v
+
+
+# ---- logits ----------------------------------------------------------------------------------------
+
+def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=None, allowed=None, out=None):
+    """Penalties of the tokens in history [B, N] (entries that are no token count for nothing; the first prompt_lengths[b] for the
+    repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
+    not set.  out may be x."""
+    _check(x, "x", _FLOAT, (2,))
+    out = _empty_like(x) if out is None else out
+    _launch_some((x,), (penalty_task(x, out, history, prompt_lengths, params, bias, allowed),))
+    return out

@@ -81,6 +81,9 @@ def lib():
         "gpuos_swap_op": (ctypes.c_int, [vp, u32, u32, P(u32)]),
         "gpuos_submit": (ctypes.c_int, [vp, vp, u32, P(u64)]),
         "gpuos_submit_flush": (ctypes.c_int, [vp, vp, u32, P(u64)]),
+        "gpuos_submit_model": (ctypes.c_int, [vp, vp, u32, P(u64)]),
+        "gpuos_launch_model": (ctypes.c_int, [i32, vp, u32, vp, vp]),
+        "gpuos_model_plan": (ctypes.c_int, [vp, u32, vp]),
         "gpuos_flush": (ctypes.c_int, [vp]),
         "gpuos_wait": (ctypes.c_int, [vp, u64, u64]),
         "gpuos_get_completions": (ctypes.c_int, [vp, u64, u32, vp]),
@@ -118,7 +121,7 @@ def lib():
 
 
 EXPORTS = ["gpuos_default_config", "gpuos_init", "gpuos_init_static", "gpuos_register_op", "gpuos_swap_op", "gpuos_submit", "gpuos_submit_flush",
-           "gpuos_flush", "gpuos_wait", "gpuos_get_completions", "gpuos_peek_queue",
+           "gpuos_submit_model", "gpuos_launch_model", "gpuos_model_plan", "gpuos_flush", "gpuos_wait", "gpuos_get_completions", "gpuos_peek_queue",
            "gpuos_worker_alive", "gpuos_set_yield_every", "gpuos_shutdown", "gpuos_stop_worker", "gpuos_start_worker",
            "gpuos_worker_elapsed_ms", "gpuos_worker_stats", "gpuos_run_serial", "gpuos_launch_per_op", "gpuos_task_bytes", "gpuos_task_plan", "gpuos_device_info", "gpuos_define_program", "gpuos_native_info", "gpuos_submit_from_threads", "gpuos_get_trace", "gpuos_op_counts",
            "gpuos_trace_origin", "gpuos_kill_op", "gpuos_audit_log", "gpuos_strerror",
@@ -266,6 +269,18 @@ class Runtime:
         _check(rc, "gpuos_submit")
         return t0.value
 
+    def submit_model(self, tasks, flush=True, check=True):
+        """gpuos_submit_model (+ gpuos_flush) of model operators' descriptors: their bytes one after the other, as
+        `model` makes them.  Returns the first ticket; with check=False (status, first ticket)."""
+        t0 = ctypes.c_uint64()
+        rc = lib().gpuos_submit_model(self._ctx, tasks, _model_count(tasks), ctypes.byref(t0))
+        if rc == OK and flush:
+            rc = lib().gpuos_flush(self._ctx)
+        if not check:
+            return rc, t0.value
+        _check(rc, "gpuos_submit_model")
+        return t0.value
+
     def flush(self):
         _check(lib().gpuos_flush(self._ctx), "gpuos_flush")
 
@@ -407,6 +422,42 @@ def launch_per_op(tasks, table, device=0, sync_each=False, first=0, count=None):
                                    lat.ctypes.data if sync_each else None, ctypes.byref(secs))
     _check(rc, "gpuos_launch_per_op")
     return secs.value, lat
+
+
+def _model_count(tasks):
+    assert isinstance(tasks, bytes) and len(tasks) % S.MODEL_TASK_BYTES == 0
+    return len(tasks) // S.MODEL_TASK_BYTES
+
+
+_model_table = None
+
+
+def launch_model(tasks, device=0, stream=0, table=None):
+    """gpuos_launch_model: model operators' descriptors (bytes, as `model` makes them) as ordinary kernels on `stream` (a
+    stream's handle).  table: logical operator -> implementation (None: streams.MODEL_OP's)."""
+    global _model_table
+    if table is None:
+        if _model_table is None:
+            _model_table = _impl_table({S.MODEL_OP[name]: impl for name, impl in S.MODEL_IMPL.items()})
+        impl = _model_table
+    else:
+        impl = _impl_table(table)
+    _check(lib().gpuos_launch_model(device, tasks, _model_count(tasks), impl, stream), "gpuos_launch_model")
+
+
+def _impl_table(table):
+    impl = (ctypes.c_uint32 * MAX_OPS)()
+    for op, im in table.items():
+        impl[op] = im
+    return impl
+
+
+def model_plan(task, impl):
+    """gpuos_model_plan of one descriptor: how it is run and cut."""
+    out = (ctypes.c_uint32 * 6)()
+    assert _model_count(task) == 1
+    _check(lib().gpuos_model_plan(task, int(impl), out), "gpuos_model_plan")
+    return dict(zip(("vectors", "ring_chunks", "ring_rows", "chunks", "rows", "segment"), (int(x) for x in out)))
 
 
 def task_bytes(tasks, impls):
