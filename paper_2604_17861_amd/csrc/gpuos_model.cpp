@@ -56,37 +56,38 @@ int gpuos_launch_model(int32_t device, const gpuos_model_task* tasks, uint32_t n
   ModelLaunch l;
   uint32_t i = 0;
   while (i < n) {
-    uint32_t count = 0, blocks = 0, impl = 0;
+    uint32_t count = 0, chunks = 0, variant = 0;
     const uint32_t head = i;                                    // (a task waits for those of earlier launches by the stream's order)
     for (; i < n && count < kModelLaunch; ++i) {
       const ModelHead& h = staged[i].h;
       if (h.path == PATH_NOP) continue;
       bool waits = count != 0 && (tasks[i].flags & GPUOS_FLAG_FENCE) != 0;
       for (int k = 0; k < 3; ++k) waits = waits || (count != 0 && tasks[i].dep[k] != 0 && tasks[i].dep[k] <= i - head);
-      if (count != 0 && (waits || h.impl != impl)) break;
-      impl = h.impl;
-      l.rec[count] = staged[i];
-      l.first[count++] = blocks;
-      blocks += h.nchunks;
+      const uint32_t v = model_variant(h.impl, h.vec, h.dtype[0], h.flags);
+      if (count != 0 && (waits || v != variant)) break;
+      variant = v;
+      l.rec[count++] = staged[i];
+      chunks = h.nchunks > chunks ? h.nchunks : chunks;
     }
     if (count == 0) continue;
-    for (uint32_t k = count; k < kModelLaunch; ++k) l.first[k] = 0xffffffffu;
-    const int rc = hip_status(launch_model(l, impl, blocks, stream), "launch of a model operator");
+    const int rc = hip_status(launch_model(l, variant, chunks, count, stream), "launch of a model operator");
     if (rc != GPUOS_OK) return rc;
   }
   return GPUOS_OK;
 }
 
-int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t out[6]) {
+int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t out[8]) {
   if (!task || !out) return GPUOS_E_INVAL;
-  ModelRecord ring, launch;
-  int rc = ModelPack::pack(*task, impl_id, &ring, kRingCut);
-  if (rc == GPUOS_OK) rc = ModelPack::pack(*task, impl_id, &launch, kLaunchCut);
-  if (rc != GPUOS_OK) return rc;
-  out[0] = ring.h.path == PATH_NOP ? 2u : (launch.h.vec != 0 ? 1u : 0u);
-  out[1] = ring.h.nchunks; out[2] = ring.h.chunk;
-  out[3] = launch.h.nchunks; out[4] = launch.h.chunk;
-  out[5] = impl_id == GPUOS_IMPL_LOGIT_PENALTY ? launch.penalty.seg : 0u;
+  const ModelCut cuts[2] = {kRingCut, kLaunchCut};
+  for (int k = 0; k < 2; ++k) {
+    ModelRecord r;
+    const int rc = ModelPack::pack(*task, impl_id, &r, cuts[k]);
+    if (rc != GPUOS_OK) return rc;
+    out[4 * k] = r.h.path == PATH_NOP ? 2u : r.h.vec;
+    out[4 * k + 1] = r.h.nchunks;
+    out[4 * k + 2] = r.h.chunk;
+    out[4 * k + 3] = impl_id == GPUOS_IMPL_LOGIT_PENALTY ? r.penalty.seg : (impl_id == GPUOS_IMPL_GAMMA_SUM ? 1u : r.h.block);
+  }
   return GPUOS_OK;
 }
 

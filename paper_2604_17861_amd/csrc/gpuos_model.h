@@ -33,14 +33,15 @@ struct ModelHead {
   uint8_t  flags;                  // MF_*
   uint8_t  dtype[4];               // x, out, and per operator
   uint8_t  rflags;
-  uint8_t  pad0[3];
+  uint8_t  block;                  // heads of a token that an item has
+  uint8_t  pad0[2];
   uint8_t  sel;
   uint8_t  pad1[2];
   uint32_t impl, version;
   int32_t  status;
   uint32_t nchunks;
-  uint32_t chunk;                  // rows (LOGIT_PENALTY: segments of rows) in a chunk
-  uint32_t rows;                   // ... and in all
+  uint32_t chunk;                  // items (blocks of heads, segments of rows) in a chunk
+  uint32_t items;                  // ... and in all
   uint32_t d;                      // elements of a row
   float    alpha;
   uint16_t dep[3];
@@ -49,10 +50,10 @@ struct ModelHead {
 };
 static_assert(sizeof(ModelHead) == 64 && offsetof(ModelHead, rflags) == offsetof(Record, rflags) && offsetof(ModelHead, sel) == offsetof(Record, sel) &&
               offsetof(ModelHead, impl) == offsetof(Record, impl) && offsetof(ModelHead, nchunks) == offsetof(Record, nchunks) &&
-              offsetof(ModelHead, chunk) == offsetof(Record, chunk) && offsetof(ModelHead, rows) == offsetof(Record, numel) &&
+              offsetof(ModelHead, chunk) == offsetof(Record, chunk) && offsetof(ModelHead, items) == offsetof(Record, numel) &&
               offsetof(ModelHead, dep) == offsetof(Record, dep) && offsetof(ModelHead, run) == offsetof(Record, run) &&
               offsetof(ModelHead, ticket) == offsetof(Record, ticket) && offsetof(ModelHead, path) == offsetof(Record, path), "the words the dispatcher and the worker read");
-enum ModelFlag : uint8_t { MF_PAIRS = 1, MF_TABLE16 = 2 };
+enum ModelFlag : uint8_t { MF_PAIRS = 1 };
 
 struct alignas(16) RopeRecord {    // NORM_ROPE, NORM_ROPE_GRAD, GAMMA_SUM
   ModelHead h;                     // dtype: x, out, gamma, dout
@@ -64,8 +65,9 @@ struct alignas(16) RopeRecord {    // NORM_ROPE, NORM_ROPE_GRAD, GAMMA_SUM
   Div by_seq;
   uint32_t pad0;
   uint32_t unused[2];              // (t_dequeue)
-  Div by_heads;
-  uint32_t spare[5];
+  Div by_blocks;
+  uint32_t blocks;                 // of heads
+  uint32_t spare[4];
   uint32_t check;
 };
 struct alignas(16) CacheRecord {   // CACHE_STORE, CACHE_LOAD
@@ -74,10 +76,9 @@ struct alignas(16) CacheRecord {   // CACHE_STORE, CACHE_LOAD
   uint32_t xs[4], cs[3], ss[4];    // strides of x: B, S, H, D; of the cache: page, place, head; of the scales: page, place, head, group
   uint32_t ps[2], ls;              // of slots (or the table), lengths
   uint32_t pages, page, group;
-  uint32_t heads;
-  Div by_heads;
-  uint32_t pad0[2];
-  uint32_t spare[6];
+  uint32_t heads, blocks;
+  Div by_blocks;
+  uint32_t pad0[7];
   uint32_t unused[2];              // (t_dequeue)
   uint32_t seq;
   Div by_seq, by_page, by_group;   // (by_group: CACHE_LOAD element by element)
@@ -110,15 +111,18 @@ static_assert(offsetof(RopeRecord, unused) == offsetof(Record, t_dequeue) && off
 
 constexpr uint32_t kModelRow = 512;          // elements of a head, at most: 64 lanes of eight
 constexpr uint32_t kModelParts = 1024;       // shares of the gradient of gamma, at most (a unit names its chunk in ten bits)
+// Lanes that a row of vectors takes: a lane has four pairs, or eight elements that are not rotated (neighbours: eight elements).
+GPUOS_HD inline uint32_t rope_units(uint32_t d, uint32_t half, bool pairs) { return pairs ? (d + 7u) / 8u : (half + 3u) / 4u + (d - 2u * half + 7u) / 8u; }
+constexpr uint32_t kRopeBlock = 4, kGradBlock = 2, kCacheBlock = 4;      // heads of an item that goes in vectors
 constexpr uint32_t kModelLaunch = 8;         // tasks of one launch: their records are kernel arguments, 2 KB of the 4 KB there may be
 
-// What gpuos_launch_model hands a kernel: tasks of one operator, and the first block of each.
+// What gpuos_launch_model hands a kernel: tasks of one variant.  (A block's second index is its task's place here: its
+// record is then one trip to memory away, with a table of first blocks it was two.)
 struct alignas(16) ModelLaunch {
   ModelRecord rec[kModelLaunch];
-  uint32_t first[kModelLaunch];    // (0xffffffff behind the last task)
 };
 int hip_status(int e, const char* what);     // GPUOS_OK, or GPUOS_E_HIP with gpuos_last_hip_error() set (gpuos_runtime.cpp)
-int launch_model(const ModelLaunch& l, uint32_t impl, uint32_t blocks, void* stream);      // gpuos_model.hip
+int launch_model(const ModelLaunch& l, uint32_t variant, uint32_t chunks, uint32_t tasks, void* stream);      // gpuos_model.hip
 
 inline bool impl_is_model(uint32_t impl) { return impl >= GPUOS_IMPL_NORM_ROPE && impl <= GPUOS_IMPL_LOGIT_PENALTY; }
 inline int model_arity(uint32_t impl) {
@@ -129,6 +133,15 @@ inline int model_arity(uint32_t impl) {
     case GPUOS_IMPL_CACHE_STORE: return 4;
     default: return -1;
   }
+}
+
+// The executors of the operators, one after the other: rows in vectors by dtype (rotations: halves, then neighbours), then element by
+// element.  A kernel and a function of the worker each, so that none has the registers of another.
+enum ModelVariant : uint32_t { MV_ROPE = 0, MV_GRAD = 7, MV_SUM = 14, MV_STORE = 15, MV_LOAD = 19, MV_PENALTY = 23, MV_COUNT = 27 };
+GPUOS_HD inline uint32_t model_variant(uint32_t impl, uint32_t vec, uint32_t dtype, uint32_t flags) {
+  if (impl == GPUOS_IMPL_GAMMA_SUM) return MV_SUM;
+  if (impl <= GPUOS_IMPL_NORM_ROPE_GRAD) return (impl == GPUOS_IMPL_NORM_ROPE ? MV_ROPE : MV_GRAD) + (vec == 0 ? 6u : dtype + ((flags & MF_PAIRS) ? 3u : 0u));
+  return (impl == GPUOS_IMPL_CACHE_STORE ? MV_STORE : (impl == GPUOS_IMPL_CACHE_LOAD ? MV_LOAD : MV_PENALTY)) + (vec == 0 ? 3u : dtype);
 }
 
 // How a task is cut: chunks of at least so many bytes, at most so many; and whether vectors have to be aligned (the worker's accesses of
@@ -166,7 +179,7 @@ class ModelPack {
     else if (impl == GPUOS_IMPL_GAMMA_SUM) rc = pack_sum(t, r->rope, cut);
     else if (impl == GPUOS_IMPL_LOGIT_PENALTY) rc = pack_penalty(t, r->penalty, cut);
     else rc = pack_cache(t, r->cache, impl == GPUOS_IMPL_CACHE_STORE, cut);
-    if (rc == GPUOS_OK && h.rows == 0) {
+    if (rc == GPUOS_OK && h.items == 0) {
       h.path = PATH_NOP;
       h.nchunks = 1;
     }
@@ -209,15 +222,22 @@ class ModelPack {
     for (int d = 0; d < outer; ++d) ok = ok && (uint64_t)st[d] * es % 8 == 0;
     return ok;
   }
-  // Rows in chunks: by bytes moved, in whole passes of a workgroup, as many chunks as may be.
-  static void cut_rows(ModelHead& h, ModelCut cut, uint64_t row_bytes, uint32_t pass) {
-    uint64_t per = (cut.least_bytes + row_bytes - 1) / row_bytes;
-    const uint64_t even = ((uint64_t)h.rows + cut.most - 1) / cut.most;
+  // The heads of a token in blocks of `block`.
+  template <class RECORD> static void in_blocks(RECORD& r, uint64_t tokens, uint32_t block) {
+    r.h.block = (uint8_t)block;
+    r.blocks = (r.heads + block - 1) / block;
+    r.by_blocks = make_div(r.blocks);
+    r.h.items = (uint32_t)(tokens * r.blocks);
+  }
+  // Items in chunks: by bytes moved, in whole passes of a workgroup, as many chunks as may be.
+  static void cut_items(ModelHead& h, ModelCut cut, uint64_t item_bytes, uint32_t pass) {
+    uint64_t per = (cut.least_bytes + item_bytes - 1) / item_bytes;
+    const uint64_t even = ((uint64_t)h.items + cut.most - 1) / cut.most;
     if (per < even) per = even;
     per = (per + pass - 1) / pass * pass;
     if (per > 0x7fffffffull) per = 0x7fffffffull;
     h.chunk = (uint32_t)per;
-    h.nchunks = h.rows == 0 ? 1u : (uint32_t)((h.rows + per - 1) / per);
+    h.nchunks = h.items == 0 ? 1u : (uint32_t)((h.items + per - 1) / per);
   }
   // rows that the workgroup's 256 lanes take at once, `lanes` of them each
   static uint32_t rows_at_once(uint32_t lanes) {
@@ -264,20 +284,21 @@ class ModelPack {
     r.heads = (uint32_t)z[2];
     r.seq = (uint32_t)z[1];
     r.h.d = (uint32_t)d;
-    r.h.rows = (uint32_t)(tokens * z[2]);
     // (a position that is the index in S needs S by itself)
     const bool joined = (rot == 0 || pos->ptr) && join((uint32_t)z[0], r.seq, r.xs, r.os, r.zs, r.ps);
     r.by_seq = joined ? Div{0, 0} : make_div(r.seq);
-    r.by_heads = make_div(r.heads);
-    // Vectors: a lane takes four elements twice, the two halves of four pairs (or eight that are not rotated).  All operands of one
-    // dtype, rows of whole eights, halves of whole fours.
-    const uint32_t es = size_of(x->dtype);
-    const bool last = d == 1 || (r.xs[3] == 1 && r.os[3] == 1 && r.zs[3] == 1);
-    if (x->dtype == out->dtype && x->dtype == dz->dtype && d % 8 == 0 && r.half % 4 == 0 && vectors(cut, r.x, es, r.xs, 3, last) &&
-        vectors(cut, r.out, es, r.os, 3, last) && vectors(cut, r.dout, es, r.zs, 3, last) && vectors(cut, r.table, 4, &r.ts, 1, true))
+    // Vectors: a lane takes four elements twice, by windows that stay in their part of the row: so a part is nothing or four elements
+    // (neighbours: the row eight, of an even number), and all operands are of one dtype.  Where vectors have to be aligned the parts are whole
+    // numbers of windows.
+    const uint32_t es = size_of(x->dtype), rest = (uint32_t)d - 2u * r.half;
+    const bool last = d == 1 || (r.xs[3] == 1 && r.os[3] == 1 && r.zs[3] == 1), pairs = (t.flags & GPUOS_FLAG_PAIRS) != 0;
+    const bool parts = pairs ? d >= 8 && d % 2 == 0 : (r.half == 0 || r.half >= 4) && (rest == 0 || rest >= 4);
+    if (x->dtype == out->dtype && x->dtype == dz->dtype && parts && rope_units((uint32_t)d, r.half, pairs) <= 64 &&
+        (!cut.aligned || (d % 8 == 0 && r.half % 4 == 0)) && vectors(cut, r.x, es, r.xs, 3, last) && vectors(cut, r.out, es, r.os, 3, last) &&
+        vectors(cut, r.dout, es, r.zs, 3, last) && vectors(cut, r.table, 4, &r.ts, 1, true))
       r.h.vec = 1;
-    const uint32_t pass = rows_at_once(r.h.vec ? (uint32_t)d / 8 : (uint32_t)(d + 1) / 2);
-    cut_rows(r.h, cut, (uint64_t)d * es * (grad ? 3 : 2), pass);
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? (grad ? kGradBlock : kRopeBlock) : 1);
+    cut_items(r.h, cut, (uint64_t)d * es * (grad ? 3 : 2) * r.h.block, rows_at_once(r.h.vec ? rope_units((uint32_t)d, r.half, pairs) : (uint32_t)(d + 1) / 2));
     if (grad && part->ptr) {
       const int64_t parts = z[6], cz[2] = {d, parts};
       uint32_t cs[2];
@@ -286,10 +307,10 @@ class ModelPack {
       r.partial = (uint64_t)part->ptr;
       r.cs = cs[0];
       r.h.nchunks = (uint32_t)parts;                 // every column is written, also of shares with no rows
-      r.h.chunk = (uint32_t)((r.h.rows + parts - 1) / parts);
-      if (r.h.rows == 0) {                           // (not an empty task: see pack)
+      r.h.chunk = (uint32_t)((r.h.items + parts - 1) / parts);
+      if (r.h.items == 0) {                           // (not an empty task: see pack)
         r.h.vec = 0;
-        r.h.rows = kNoRows;
+        r.h.items = kNoRows;
       }
     }
     return GPUOS_OK;
@@ -305,9 +326,9 @@ class ModelPack {
     r.out = (uint64_t)out.ptr;
     r.cs = cs[0];
     r.h.dtype[1] = out.dtype;
-    r.h.rows = (uint32_t)t.size[0];
+    r.h.items = (uint32_t)t.size[0];
     r.h.d = (uint32_t)t.size[1];
-    cut_rows(r.h, cut, 4ull * r.h.d + 4, kThreads / 64);
+    cut_items(r.h, cut, 4ull * r.h.d + 4, 1);
     return GPUOS_OK;
   }
 
@@ -343,15 +364,14 @@ class ModelPack {
     r.heads = (uint32_t)z[2];
     r.seq = (uint32_t)z[1];
     r.h.d = (uint32_t)d;
-    r.h.rows = (uint32_t)(tokens * z[2]);
     r.by_seq = store && join((uint32_t)z[0], r.seq, r.xs, r.ps) ? Div{0, 0} : make_div(r.seq);
-    r.by_heads = make_div(r.heads);
     r.by_page = make_div(r.page);
     r.by_group = make_div(r.group);
-    // Vectors: a lane takes eight elements of a row, 8 bytes of the cache.
+    // Vectors: a lane takes eight elements of a row, 8 bytes of the cache.  (A row that is no whole number of eights is one group.)
     const uint32_t es = size_of(x.dtype);
-    if (d % 8 == 0 && group % 8 == 0 && vectors(cut, r.x, es, r.xs, 3, r.xs[3] == 1) && vectors(cut, r.cache, 1, r.cs, 3, true)) r.h.vec = 1;
-    cut_rows(r.h, cut, (uint64_t)d * (es + 1), rows_at_once(r.h.vec ? (uint32_t)d / 8 : (uint32_t)d));
+    if (d >= 8 && (!cut.aligned || d % 8 == 0) && vectors(cut, r.x, es, r.xs, 3, r.xs[3] == 1) && vectors(cut, r.cache, 1, r.cs, 3, true)) r.h.vec = 1;
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? kCacheBlock : 1);
+    cut_items(r.h, cut, (uint64_t)d * (es + 1) * r.h.block, rows_at_once(r.h.vec ? (uint32_t)(d + 7) / 8 : (uint32_t)d));
     return GPUOS_OK;
   }
 
@@ -380,13 +400,13 @@ class ModelPack {
     if (segs * b > kMost) return GPUOS_E_INVAL;
     r.segs = (uint32_t)segs;
     r.by_segs = make_div(r.segs);
-    r.h.rows = (uint32_t)(segs * b);
+    r.h.items = (uint32_t)(segs * b);
     const bool bias_ok = !bias.ptr || r.bs[1] == 1 || v == 1, allowed_ok = !allowed.ptr || r.as[1] == 1 || az[1] == 1;
     const uint32_t es = size_of(x.dtype);
     if (x.dtype == out.dtype && vectors(cut, r.x, es, r.xs, 1, v == 1 || r.xs[1] == 1) && vectors(cut, r.out, es, r.os, 1, v == 1 || r.os[1] == 1) &&
         bias_ok && allowed_ok)
       r.h.vec = 1;
-    cut_rows(r.h, ModelCut{1, cut.most, cut.aligned}, 1, 1);
+    cut_items(r.h, ModelCut{1, cut.most, cut.aligned}, 1, 1);
     return GPUOS_OK;
   }
 

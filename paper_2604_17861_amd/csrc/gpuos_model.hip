@@ -4,77 +4,32 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "gpuos_model_device.h"
 
 namespace gpuos {
 
-typedef const __attribute__((address_space(4))) ModelRecord* const_record_t;
-
-template <int IMPL> DEV void run_model(const_record_t r, uint32_t chunk, float* s, uint32_t tid) {
-  const uint32_t vec = uni((uint32_t)r->h.vec), dt = uni((uint32_t)r->h.dtype[0]);
-  if constexpr (IMPL == GPUOS_IMPL_NORM_ROPE || IMPL == GPUOS_IMPL_NORM_ROPE_GRAD) {
-    constexpr bool GRAD = IMPL == GPUOS_IMPL_NORM_ROPE_GRAD;
-    const RopeArgs a = rope_args(&r->rope);
-    if (vec == 0) rope_elements<POL_PLAIN, GRAD>(a, chunk, s, tid);
-    else if (!a.pairs) {
-      if (dt == GPUOS_F32) rope_vectors<POL_PLAIN, GPUOS_F32, false, GRAD>(a, chunk, s, tid);
-      else if (dt == GPUOS_F16) rope_vectors<POL_PLAIN, GPUOS_F16, false, GRAD>(a, chunk, s, tid);
-      else rope_vectors<POL_PLAIN, GPUOS_BF16, false, GRAD>(a, chunk, s, tid);
-    } else {
-      if (dt == GPUOS_F32) rope_vectors<POL_PLAIN, GPUOS_F32, true, GRAD>(a, chunk, s, tid);
-      else if (dt == GPUOS_F16) rope_vectors<POL_PLAIN, GPUOS_F16, true, GRAD>(a, chunk, s, tid);
-      else rope_vectors<POL_PLAIN, GPUOS_BF16, true, GRAD>(a, chunk, s, tid);
-    }
-  } else if constexpr (IMPL == GPUOS_IMPL_GAMMA_SUM) {
-    gamma_sum<POL_PLAIN>(rope_args(&r->rope), chunk, tid);
-  } else if constexpr (IMPL == GPUOS_IMPL_CACHE_STORE) {
-    const CacheArgs a = cache_args(&r->cache);
-    if (vec == 0) store_elements<POL_PLAIN>(a, chunk, tid);
-    else if (dt == GPUOS_F32) store_vectors<POL_PLAIN, GPUOS_F32>(a, chunk, tid);
-    else if (dt == GPUOS_F16) store_vectors<POL_PLAIN, GPUOS_F16>(a, chunk, tid);
-    else store_vectors<POL_PLAIN, GPUOS_BF16>(a, chunk, tid);
-  } else if constexpr (IMPL == GPUOS_IMPL_CACHE_LOAD) {
-    const CacheArgs a = cache_args(&r->cache);
-    if (vec == 0) load_elements<POL_PLAIN>(a, chunk, tid);
-    else if (dt == GPUOS_F32) load_vectors<POL_PLAIN, GPUOS_F32>(a, chunk, tid);
-    else if (dt == GPUOS_F16) load_vectors<POL_PLAIN, GPUOS_F16>(a, chunk, tid);
-    else load_vectors<POL_PLAIN, GPUOS_BF16>(a, chunk, tid);
-  } else {
-    const PenaltyArgs a = penalty_args(&r->penalty);
-    if (vec == 0) penalty_segments<POL_PLAIN, -1>(a, chunk, s, tid);
-    else if (dt == GPUOS_F32) penalty_segments<POL_PLAIN, GPUOS_F32>(a, chunk, s, tid);
-    else if (dt == GPUOS_F16) penalty_segments<POL_PLAIN, GPUOS_F16>(a, chunk, s, tid);
-    else penalty_segments<POL_PLAIN, GPUOS_BF16>(a, chunk, s, tid);
-  }
-}
 // LDS of a block, in floats: the partial sums of gamma by groups of lanes; a segment's counts
-template <int IMPL> constexpr uint32_t model_lds() {
-  return IMPL == GPUOS_IMPL_NORM_ROPE_GRAD ? 2048u : (IMPL == GPUOS_IMPL_LOGIT_PENALTY ? ModelPack::kSegment : 1u);
-}
+constexpr uint32_t model_lds(uint32_t v) { return v < MV_GRAD ? 1u : (v < MV_SUM ? 2048u : (v == MV_SUM ? 4u : (v < MV_PENALTY ? 1u : ModelPack::kSegment))); }
+constexpr uint32_t model_threads(uint32_t v) { return v < MV_PENALTY ? kThreads : kPenaltyThreads; }
 
-template <int IMPL> __global__ void __launch_bounds__(kThreads) gpuos_model_kernel(ModelLaunch l) {
-  __shared__ alignas(16) float s[model_lds<IMPL>()];
+template <uint32_t V> __global__ void __launch_bounds__(model_threads(V)) gpuos_model_kernel(ModelLaunch) {
+  __shared__ alignas(16) float s[model_lds(V)];
   typedef const __attribute__((address_space(4))) ModelLaunch* launch_t;
-  const launch_t p = (launch_t)__builtin_amdgcn_kernarg_segment_ptr();
-  uint32_t t = 0;
-#pragma unroll
-  for (uint32_t k = 1; k < kModelLaunch; ++k) t += blockIdx.x >= p->first[k] ? 1u : 0u;
-  run_model<IMPL>(&p->rec[t], blockIdx.x - p->first[t], s, threadIdx.x);
+  const auto r = &((launch_t)__builtin_amdgcn_kernarg_segment_ptr())->rec[blockIdx.y];
+  if (blockIdx.x < r->h.nchunks) run_model<POL_PLAIN, V, model_threads(V)>(r, blockIdx.x, s, threadIdx.x);
 }
 
-int launch_model(const ModelLaunch& l, uint32_t impl, uint32_t blocks, void* stream) {
-  const dim3 grid(blocks), block(kThreads);
-  const hipStream_t st = (hipStream_t)stream;
-  switch (impl) {
-    case GPUOS_IMPL_NORM_ROPE: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_NORM_ROPE>, grid, block, 0, st, l); break;
-    case GPUOS_IMPL_NORM_ROPE_GRAD: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_NORM_ROPE_GRAD>, grid, block, 0, st, l); break;
-    case GPUOS_IMPL_GAMMA_SUM: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_GAMMA_SUM>, grid, block, 0, st, l); break;
-    case GPUOS_IMPL_CACHE_STORE: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_CACHE_STORE>, grid, block, 0, st, l); break;
-    case GPUOS_IMPL_CACHE_LOAD: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_CACHE_LOAD>, grid, block, 0, st, l); break;
-    case GPUOS_IMPL_LOGIT_PENALTY: hipLaunchKernelGGL(gpuos_model_kernel<GPUOS_IMPL_LOGIT_PENALTY>, grid, block, 0, st, l); break;
-    default: return (int)hipErrorInvalidValue;
-  }
-  return (int)hipGetLastError();
+typedef void (*model_kernel_t)(ModelLaunch);
+template <uint32_t... V> struct Kernels { static constexpr model_kernel_t at[] = {gpuos_model_kernel<V>...}; };
+template <uint32_t... V> Kernels<V...> kernels_of(std::integer_sequence<uint32_t, V...>);
+typedef decltype(kernels_of(std::make_integer_sequence<uint32_t, MV_COUNT>())) AllKernels;
+
+int launch_model(const ModelLaunch& l, uint32_t variant, uint32_t chunks, uint32_t tasks, void* stream) {
+  if (variant >= MV_COUNT) return (int)hipErrorInvalidValue;
+  void* args[] = {(void*)&l};
+  return (int)hipLaunchKernel((const void*)AllKernels::at[variant], dim3(chunks, tasks), dim3(model_threads(variant)), args, 0, (hipStream_t)stream);      // (its own status, not the thread's last one)
 }
 
 }  // namespace gpuos

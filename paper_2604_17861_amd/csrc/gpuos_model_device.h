@@ -98,14 +98,43 @@ DEV uint32_t float_size(uint32_t dt) { return dt == GPUOS_F32 ? 4u : 2u; }
 DEV uint32_t ceil_log2(uint32_t n) { return n <= 1 ? 0u : 32u - (uint32_t)__builtin_clz(n - 1); }
 DEV Div uni_div(uint32_t mul, uint32_t shift) { return Div{uni(mul), uni(shift)}; }
 
-// A row of [B, S, H, D] by its number, the head running fastest.
+// Eight elements as they lie in memory, in one piece or in two halves.
+template <int POL, int DT> struct Eight {
+  static constexpr int N = Elem<DT>::ES / 2;
+  v4i q[N];
+  DEV void clear() {
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = v4i{0, 0, 0, 0};
+  }
+  DEV float get(int i) const { return N == 2 ? Elem<DT>::get(q[N == 2 ? i / 4 : 0], i % 4) : Elem<DT>::get(q[0], i); }
+  DEV void put(int i, float f) { if (N == 2) Elem<DT>::put(q[N == 2 ? i / 4 : 0], i % 4, f); else Elem<DT>::put(q[0], i, f); }
+  DEV void load(uint64_t p) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = Glob<POL>::ld16(p + 16 * k);
+  }
+  DEV void load(uint64_t p, uint64_t p2) {
+    if (N == 2) { q[0] = Glob<POL>::ld16(p); q[N - 1] = Glob<POL>::ld16(p2); }
+    else { const v2i a = Glob<POL>::ld8(p), b = Glob<POL>::ld8(p2); q[0] = v4i{a[0], a[1], b[0], b[1]}; }
+  }
+  DEV void store(uint64_t p) const {
+#pragma unroll
+    for (int k = 0; k < N; ++k) Glob<POL>::st16(p + 16 * k, q[k]);
+  }
+  DEV void store(uint64_t p, uint64_t p2) const {
+    if (N == 2) { Glob<POL>::st16(p, q[0]); Glob<POL>::st16(p2, q[N - 1]); }
+    else { Glob<POL>::st8(p, v2i{q[0][0], q[0][1]}); Glob<POL>::st8(p2, v2i{q[0][2], q[0][3]}); }
+  }
+};
+
+// Rows of [B, S, H, D] come in items: a token and the heads [h, h + block) of it, by the item's number, blocks of heads running fastest.
+// What belongs to the token (its position, slot, page, the divisions here) is then found once for a block.
 struct Place { uint32_t b, s, h; };
-DEV Place place(uint32_t row, uint32_t heads, Div by_heads, uint32_t seq, Div by_seq) {
+template <class ARGS> DEV Place place(const ARGS& a, uint32_t item) {
   Place p;
-  const uint32_t token = divided(row, by_heads);
-  p.h = row - token * heads;
-  p.b = divided(token, by_seq);
-  p.s = token - p.b * seq;
+  const uint32_t token = divided(item, a.by_blocks);
+  p.h = (item - token * a.blocks) * a.block;
+  p.b = divided(token, a.by_seq);
+  p.s = token - p.b * a.seq;
   return p;
 }
 DEV uint64_t offset(const Place& p, const uint32_t (&st)[4]) { return (uint64_t)p.b * st[0] + (uint64_t)p.s * st[1] + (uint64_t)p.h * st[2]; }
@@ -121,8 +150,8 @@ DEV uint64_t offset(const Place& p, const uint32_t (&st)[4]) { return (uint64_t)
 // ---------------------------------------------------------------------------
 struct RopeArgs {
   uint64_t x, gamma, table, positions, out, dout, partial;
-  uint32_t xs[4], os[4], zs[4], gs, ts, ps[2], cs, half, places, seq, heads, d, chunk, rows, dtype[4];
-  Div by_seq, by_heads;
+  uint32_t xs[4], os[4], zs[4], gs, ts, ps[2], cs, half, places, seq, heads, block, blocks, d, chunk, items, dtype[4];
+  Div by_seq, by_blocks;
   bool pairs;
   float eps;
 };
@@ -134,8 +163,9 @@ template <class P> DEV RopeArgs rope_args(P p) {
   for (int k = 0; k < 4; ++k) { a.xs[k] = uni(p->xs[k]); a.os[k] = uni(p->os[k]); a.zs[k] = uni(p->zs[k]); a.dtype[k] = uni((uint32_t)p->h.dtype[k]); }
   a.gs = uni(p->gs); a.ts = uni(p->ts); a.ps[0] = uni(p->ps[0]); a.ps[1] = uni(p->ps[1]); a.cs = uni(p->cs);
   a.half = uni(p->half); a.places = uni(p->places); a.seq = uni(p->seq); a.heads = uni(p->heads);
-  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.rows = uni(p->h.rows);
-  a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_heads = uni_div(p->by_heads.mul, p->by_heads.shift);
+  a.block = uni((uint32_t)p->h.block); a.blocks = uni(p->blocks);
+  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
+  a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_blocks = uni_div(p->by_blocks.mul, p->by_blocks.shift);
   a.pairs = (uni((uint32_t)p->h.flags) & MF_PAIRS) != 0;
   a.eps = __builtin_bit_cast(float, uni(__builtin_bit_cast(uint32_t, (float)p->h.alpha)));
   return a;
@@ -158,110 +188,32 @@ template <int POL> DEV void gamma_part(const RopeArgs& a, uint32_t chunk, uint32
   }
 }
 
-template <int POL, int DT, bool PAIRS, bool GRAD, int U>
-DEV void rope_pass(const RopeArgs& a, uint32_t first, uint32_t step, uint32_t end, uint32_t u, bool active, uint32_t lanes, const float (&ga)[4],
-                   const float (&gb)[4], float (&da)[4], float (&db)[4]) {
-  typedef Glob<POL> M;
-  constexpr uint32_t ES = Elem<DT>::ES;
-  const uint32_t turned_units = a.half / 4u;
-  const bool turned = u < turned_units;
-  const uint32_t oa = turned ? (PAIRS ? 8u : 4u) * u : 2u * a.half + 8u * (u - turned_units);
-  const uint32_t ob = turned && !PAIRS ? a.half + 4u * u : oa + 4u;
-  float xe[U][8], ze[U][8], c[U][4], s[U][4];
-  uint64_t to[U];
-  bool ok[U], has[U];
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    uint32_t row = first + k * step;
-    ok[k] = active && row < end;
-    row = row < end ? row : end - 1u;
-    const Place p = place(row, a.heads, a.by_heads, a.seq, a.by_seq);
-    const uint64_t xp = a.x + offset(p, a.xs) * ES;
-    to[k] = a.out + offset(p, a.os) * ES;
-    if (active) {
-      if (PAIRS) M::template ld8e<DT>(xp + oa * ES, xe[k]);
-      else { M::template ld4e<DT>(xp + oa * ES, xe[k]); M::template ld4e<DT>(xp + ob * ES, xe[k] + 4); }
-      if (GRAD) {
-        const uint64_t zp = a.dout + offset(p, a.zs) * ES;
-        if (PAIRS) M::template ld8e<DT>(zp + oa * ES, ze[k]);
-        else { M::template ld4e<DT>(zp + oa * ES, ze[k]); M::template ld4e<DT>(zp + ob * ES, ze[k] + 4); }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) xe[k][i] = ze[k][i] = 0.0f;
-    }
-    has[k] = true;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { c[k][i] = 1.0f; s[k][i] = 0.0f; }
-    if (a.half != 0) {
-      uint64_t row_p;
-      has[k] = table_row<POL>(a, p, row_p);
-      if (turned) {
-        M::template ld4e<GPUOS_F32>(row_p + u * 16u, c[k]);
-        M::template ld4e<GPUOS_F32>(row_p + (a.half + u * 4u) * 4u, s[k]);
-      }
-    }
-  }
-  const float inv_d = 1.0f / (float)a.d;
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    float xa[4], xb[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { xa[i] = xe[k][PAIRS ? 2 * i : i]; xb[i] = xe[k][PAIRS ? 2 * i + 1 : 4 + i]; }
-    float ss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { ss = __builtin_fmaf(xa[i], xa[i], ss); ss = __builtin_fmaf(xb[i], xb[i], ss); }
-    ss = wave_reduce<GPUOS_IMPL_SUM_LAST>(ss, lanes);
-    float r = rsqrtf(__builtin_fmaf(ss, inv_d, a.eps));
-    if (!has[k]) r = __builtin_nanf("");
-    float o[8];
-    if (!GRAD) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float ya = xa[i] * r * ga[i], yb = xb[i] * r * gb[i];
-        o[PAIRS ? 2 * i : i] = __builtin_fmaf(ya, c[k][i], -(yb * s[k][i]));
-        o[PAIRS ? 2 * i + 1 : 4 + i] = __builtin_fmaf(yb, c[k][i], ya * s[k][i]);
-      }
-    } else {
-      float ua[4], ub[4], t = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float za = ze[k][PAIRS ? 2 * i : i], zb = ze[k][PAIRS ? 2 * i + 1 : 4 + i];
-        const float ya = __builtin_fmaf(za, c[k][i], zb * s[k][i]), yb = __builtin_fmaf(zb, c[k][i], -(za * s[k][i]));
-        da[i] += ok[k] ? ya * (xa[i] * r) : 0.0f;
-        db[i] += ok[k] ? yb * (xb[i] * r) : 0.0f;
-        ua[i] = ya * ga[i];
-        ub[i] = yb * gb[i];
-        t = __builtin_fmaf(ua[i], xa[i], t);
-        t = __builtin_fmaf(ub[i], xb[i], t);
-      }
-      t = wave_reduce<GPUOS_IMPL_SUM_LAST>(t, lanes);
-      const float m = (t * inv_d) * r * r;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        o[PAIRS ? 2 * i : i] = r * __builtin_fmaf(-xa[i], m, ua[i]);
-        o[PAIRS ? 2 * i + 1 : 4 + i] = r * __builtin_fmaf(-xb[i], m, ub[i]);
-      }
-    }
-    if (ok[k]) {
-      if (PAIRS) M::template st8e<DT>(to[k] + oa * ES, o);
-      else { M::template st4e<DT>(to[k] + oa * ES, o); M::template st4e<DT>(to[k] + ob * ES, o + 4); }
-    }
-  }
-}
-
 template <int POL, int DT, bool PAIRS, bool GRAD>
 DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
-  constexpr int U = GRAD ? (Elem<DT>::ES == 4 ? 1 : 2) : (Elem<DT>::ES == 4 ? 2 : 4);
-  const uint32_t units = a.d / 8u, lg = ceil_log2(units), lanes = 1u << lg;
+  typedef Eight<POL, DT> E;
+  constexpr uint32_t ES = Elem<DT>::ES;
+  constexpr int U = GRAD ? kGradBlock : kRopeBlock;
+  // A lane's eight elements are two windows of four, oa and ob on.  Halves: the same four of either half, or eight that follow
+  // each other behind them; neighbours: eight that follow each other.  The last window of a part that is no whole number of them begins
+  // early and ends with it: what it shares with the one before (below `from`) both compute and store, and only that one sums.
+  const uint32_t units = rope_units(a.d, a.half, PAIRS), lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const bool active = u < units;
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
-  const uint32_t turned_units = a.half / 4u;
+  const uint32_t begin = chunk * a.chunk, end = a.items <= begin ? begin : (a.items - begin < a.chunk ? a.items : begin + a.chunk);
+  const uint32_t turned_units = PAIRS ? 0u : (a.half + 3u) / 4u, rest = PAIRS ? 8u * u : 2u * a.half + 8u * (u - turned_units);
   const bool turned = u < turned_units;
-  const uint32_t oa = turned ? (PAIRS ? 8u : 4u) * u : 2u * a.half + 8u * (u - turned_units);
-  const uint32_t ob = turned && !PAIRS ? a.half + 4u * u : oa + 4u;
+  uint32_t from_a = turned ? 4u * u : rest, from_b = turned ? a.half + 4u * u : rest + 4u, oa, ob;
+  if (turned) { oa = from_a < a.half - 4u ? from_a : a.half - 4u; ob = oa + a.half; }
+  else if (PAIRS) { oa = from_a < a.d - 8u ? from_a : a.d - 8u; ob = oa + 4u; from_b = from_a; }
+  else { oa = from_a < a.d - 4u ? from_a : a.d - 4u; ob = from_b < a.d - 4u ? from_b : a.d - 4u; }
+  bool va[4], vb[4], turns[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    turns[i] = PAIRS ? oa / 2u + i < a.half : turned;
+    va[i] = (PAIRS ? oa + 2u * i : oa + i) >= from_a;
+    vb[i] = (PAIRS ? oa + 2u * i + 1u : ob + i) >= from_b;
+  }
   float ga[4], gb[4], da[4], db[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -274,19 +226,100 @@ DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid)
       gb[i] = M::ld_rt(a.gamma + (uint64_t)jb * a.gs * float_size(gdt), gdt);
     }
   }
-  uint32_t row = begin;
-  if (begin < a.rows) {
-    for (; row + (U - 1) * step < end; row += U * step) rope_pass<POL, DT, PAIRS, GRAD, U>(a, row + group, step, end, u, active, lanes, ga, gb, da, db);
-    if (U > 1)
-      for (; row < end; row += step) rope_pass<POL, DT, PAIRS, GRAD, 1>(a, row + group, step, end, u, active, lanes, ga, gb, da, db);
+  const float inv_d = 1.0f / (float)a.d;
+  for (uint32_t base = begin; base < end; base += step) {
+    const uint32_t item = base + group;
+    const Place p = place(a, item < end ? item : end - 1u);
+    const uint32_t heads = item < end && active ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
+    const uint64_t xp = a.x + offset(p, a.xs) * ES, zp = a.dout + offset(p, a.zs) * ES, op = a.out + offset(p, a.os) * ES;
+    E x[U], z[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      x[k].clear();
+      if (GRAD) z[k].clear();
+      if ((uint32_t)k < heads) {
+        const uint64_t at = xp + (uint64_t)k * a.xs[2] * ES, zat = zp + (uint64_t)k * a.zs[2] * ES;
+        if (PAIRS) x[k].load(at + oa * ES);
+        else x[k].load(at + oa * ES, at + ob * ES);
+        if (GRAD && PAIRS) z[k].load(zat + oa * ES);
+        if (GRAD && !PAIRS) z[k].load(zat + oa * ES, zat + ob * ES);
+      }
+    }
+    float c[4] = {1.0f, 1.0f, 1.0f, 1.0f}, sn[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    bool has = true;
+    if (a.half != 0) {
+      uint64_t row_p;
+      has = table_row<POL>(a, p, row_p);
+      const uint32_t pair = PAIRS ? oa / 2u : oa;                // of the window's first elements
+      if (PAIRS ? pair + 4u <= a.half : turned) {
+        M::template ld4e<GPUOS_F32>(row_p + pair * 4u, c);
+        M::template ld4e<GPUOS_F32>(row_p + (a.half + pair) * 4u, sn);
+      } else if (PAIRS && pair < a.half) {                       // (the rotated part ends inside)
+#pragma unroll
+        for (uint32_t i = 0; i < 3; ++i) {
+          if (pair + i < a.half) { c[i] = M::ldf(row_p + (pair + i) * 4u); sn[i] = M::ldf(row_p + (a.half + pair + i) * 4u); }
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (__builtin_amdgcn_ballot_w64((uint32_t)k < heads) == 0) continue;       // (the same in every lane: the sums need them all)
+      float xa[4], xb[4], ss = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        xa[i] = x[k].get(PAIRS ? 2 * i : i);
+        xb[i] = x[k].get(PAIRS ? 2 * i + 1 : 4 + i);
+        const float oxa = va[i] ? xa[i] : 0.0f, oxb = vb[i] ? xb[i] : 0.0f;
+        ss = __builtin_fmaf(oxa, oxa, ss);
+        ss = __builtin_fmaf(oxb, oxb, ss);
+      }
+      ss = wave_reduce<GPUOS_IMPL_SUM_LAST>(ss, lanes);
+      float r = rsqrtf(__builtin_fmaf(ss, inv_d, a.eps));
+      if (!has) r = __builtin_nanf("");
+      E o;
+      if (!GRAD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ya = xa[i] * r * ga[i], yb = xb[i] * r * gb[i];
+          o.put(PAIRS ? 2 * i : i, turns[i] ? __builtin_fmaf(ya, c[i], -(yb * sn[i])) : ya);          // (not by an angle of 0: the other may be no number)
+          o.put(PAIRS ? 2 * i + 1 : 4 + i, turns[i] ? __builtin_fmaf(yb, c[i], ya * sn[i]) : yb);
+        }
+      } else {
+        float ua[4], ub[4], t = 0.0f;
+        const float rk = (uint32_t)k < heads ? r : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float za = z[k].get(PAIRS ? 2 * i : i), zb = z[k].get(PAIRS ? 2 * i + 1 : 4 + i);
+          const float ya = turns[i] ? __builtin_fmaf(za, c[i], zb * sn[i]) : za, yb = turns[i] ? __builtin_fmaf(zb, c[i], -(za * sn[i])) : zb;
+          da[i] = __builtin_fmaf(ya, xa[i] * rk, da[i]);         // (rows that are not there: 0 * 0)
+          db[i] = __builtin_fmaf(yb, xb[i] * rk, db[i]);
+          ua[i] = ya * ga[i];
+          ub[i] = yb * gb[i];
+          t += va[i] ? ua[i] * xa[i] : 0.0f;
+          t += vb[i] ? ub[i] * xb[i] : 0.0f;
+        }
+        t = wave_reduce<GPUOS_IMPL_SUM_LAST>(t, lanes);
+        const float m = (t * inv_d) * r * r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          o.put(PAIRS ? 2 * i : i, r * __builtin_fmaf(-xa[i], m, ua[i]));
+          o.put(PAIRS ? 2 * i + 1 : 4 + i, r * __builtin_fmaf(-xb[i], m, ub[i]));
+        }
+      }
+      if ((uint32_t)k < heads) {
+        const uint64_t to = op + (uint64_t)k * a.os[2] * ES;
+        if (PAIRS) o.store(to + oa * ES);
+        else o.store(to + oa * ES, to + ob * ES);
+      }
+    }
   }
   if (GRAD && a.partial != 0) {
     if (active) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t ja = PAIRS ? oa + 2u * i : oa + i, jb = PAIRS ? oa + 2u * i + 1u : ob + i;
-        s[group * a.d + ja] = da[i];
-        s[group * a.d + jb] = db[i];
+        if (va[i]) s[group * a.d + ja] = da[i];
+        if (vb[i]) s[group * a.d + jb] = db[i];
       }
     }
     gamma_part<POL>(a, chunk, step, s, tid);
@@ -302,8 +335,8 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
   const uint32_t rest = a.d - 2u * a.half, rest_pairs = (rest + 1u) / 2u, pairs = a.half + rest_pairs;
   const uint32_t lg = pairs > 64u ? 6u : ceil_log2(pairs), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
-  const bool empty = a.rows == ModelPack::kNoRows;
-  const uint32_t rows = empty ? 0u : a.rows, begin = chunk * a.chunk, end = rows <= begin ? begin : (rows - begin < a.chunk ? rows : begin + a.chunk);
+  const uint32_t rows = a.items == ModelPack::kNoRows ? 0u : a.items;
+  const uint32_t begin = chunk * a.chunk, end = rows <= begin ? begin : (rows - begin < a.chunk ? rows : begin + a.chunk);
   const uint32_t es = float_size(a.dtype[0]), eo = float_size(a.dtype[1]), ez = float_size(a.dtype[3]);
   uint32_t ja[K], jb[K];
   bool in_a[K], in_b[K], turned[K];
@@ -325,8 +358,7 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
   const float inv_d = 1.0f / (float)a.d;
   for (uint32_t base = begin; base < end; base += step) {
     const bool in = base + group < end;
-    const uint32_t row = in ? base + group : end - 1u;
-    const Place p = place(row, a.heads, a.by_heads, a.seq, a.by_seq);
+    const Place p = place(a, in ? base + group : end - 1u);
     const uint64_t xp = a.x + offset(p, a.xs) * es, op = a.out + offset(p, a.os) * eo, zp = a.dout + offset(p, a.zs) * ez;
     uint64_t row_p = 0;
     bool has = true;
@@ -358,14 +390,14 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const float ya = xa[k] * r * ga[k], yb = xb[k] * r * gb[k];
-        oa[k] = __builtin_fmaf(ya, c[k], -(yb * sn[k]));
-        ob[k] = __builtin_fmaf(yb, c[k], ya * sn[k]);
+        oa[k] = turned[k] ? __builtin_fmaf(ya, c[k], -(yb * sn[k])) : ya;
+        ob[k] = turned[k] ? __builtin_fmaf(yb, c[k], ya * sn[k]) : yb;
       }
     } else {
       float t = 0.0f;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const float ya = __builtin_fmaf(za[k], c[k], zb[k] * sn[k]), yb = __builtin_fmaf(zb[k], c[k], -(za[k] * sn[k]));
+        const float ya = turned[k] ? __builtin_fmaf(za[k], c[k], zb[k] * sn[k]) : za[k], yb = turned[k] ? __builtin_fmaf(zb[k], c[k], -(za[k] * sn[k])) : zb[k];
         da[k] += in ? ya * (xa[k] * r) : 0.0f;
         db[k] += in ? yb * (xb[k] * r) : 0.0f;
         oa[k] = ya * ga[k];
@@ -394,21 +426,24 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
   }
 }
 
-// GAMMA_SUM: a wavefront a row of the partial sums, always in the same order.
-template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, uint32_t tid) {
+// GAMMA_SUM: the workgroup a row of the partial sums (4 KB at most), always in the same order.
+template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
-  const uint32_t lane = tid & 63u;
-  for (uint32_t row = begin + (tid >> 6); row < end; row += kThreads / 64u) {
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
+  for (uint32_t row = begin; row < end; ++row) {
     const uint64_t p = a.partial + (uint64_t)row * a.cs * 4u;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t i = lane; i < a.d; i += 256u) {
+    float sum = 0.0f;
+    for (uint32_t i = tid; i < a.d; i += 4u * kThreads) {
+      float f[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (i + k * 64u < a.d) sum[k] += M::ldf(p + (uint64_t)(i + k * 64u) * 4u);
+      for (int k = 0; k < 4; ++k) f[k] = i + k * kThreads < a.d ? M::ldf(p + (uint64_t)(i + k * kThreads) * 4u) : 0.0f;
+      sum += (f[0] + f[1]) + (f[2] + f[3]);
     }
-    const float all = wave_reduce<GPUOS_IMPL_SUM_LAST>((sum[0] + sum[1]) + (sum[2] + sum[3]), 64u);
-    if (lane == 0) M::st_rt(a.out + (uint64_t)row * a.os[0] * float_size(a.dtype[1]), a.dtype[1], all);
+    sum = wave_reduce<GPUOS_IMPL_SUM_LAST>(sum, 64u);
+    if (row != begin) __syncthreads();
+    if ((tid & 63u) == 0) s[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) M::st_rt(a.out + (uint64_t)row * a.os[0] * float_size(a.dtype[1]), a.dtype[1], (s[0] + s[1]) + (s[2] + s[3]));
   }
 }
 
@@ -421,8 +456,8 @@ template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, uint32_
 // ---------------------------------------------------------------------------
 struct CacheArgs {
   uint64_t x, cache, scales, slots, lengths;
-  uint32_t xs[4], cs[3], ss[4], ps[2], ls, pages, page, group, heads, seq, d, chunk, rows, dtype, format;
-  Div by_heads, by_seq, by_page, by_group;
+  uint32_t xs[4], cs[3], ss[4], ps[2], ls, pages, page, group, heads, seq, block, blocks, d, chunk, items, dtype, format;
+  Div by_blocks, by_seq, by_page, by_group;
 };
 template <class P> DEV CacheArgs cache_args(P p) {
   CacheArgs a;
@@ -433,9 +468,10 @@ template <class P> DEV CacheArgs cache_args(P p) {
   for (int k = 0; k < 3; ++k) a.cs[k] = uni(p->cs[k]);
   a.ps[0] = uni(p->ps[0]); a.ps[1] = uni(p->ps[1]); a.ls = uni(p->ls);
   a.pages = uni(p->pages); a.page = uni(p->page); a.group = uni(p->group); a.heads = uni(p->heads); a.seq = uni(p->seq);
-  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.rows = uni(p->h.rows);
+  a.block = uni((uint32_t)p->h.block); a.blocks = uni(p->blocks);
+  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
   a.dtype = uni((uint32_t)p->h.dtype[0]); a.format = uni((uint32_t)p->h.dtype[1]);
-  a.by_heads = uni_div(p->by_heads.mul, p->by_heads.shift); a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_page = uni_div(p->by_page.mul, p->by_page.shift); a.by_group = uni_div(p->by_group.mul, p->by_group.shift);
+  a.by_blocks = uni_div(p->by_blocks.mul, p->by_blocks.shift); a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_page = uni_div(p->by_page.mul, p->by_page.shift); a.by_group = uni_div(p->by_group.mul, p->by_group.shift);
   return a;
 }
 struct Quant { float inv, scale; bool bad; };
@@ -474,53 +510,48 @@ DEV uint64_t scale_at(const CacheArgs& a, uint32_t page, uint32_t in, uint32_t h
   return a.scales + ((uint64_t)page * a.ss[0] + (uint64_t)in * a.ss[1] + (uint64_t)h * a.ss[2] + (uint64_t)g * a.ss[3]) * 4u;
 }
 
-template <int POL, int DT, int U>
-DEV void store_pass(const CacheArgs& a, uint32_t first, uint32_t step, uint32_t end, uint32_t u, bool active, uint32_t width, uint32_t lg_width) {
-  typedef Glob<POL> M;
-  float x[U][8];
-  int32_t slot[U];
-  uint32_t h[U];
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const uint32_t row = first + k * step;
-    const bool in = row < end;
-    const Place p = place(in ? row : end - 1u, a.heads, a.by_heads, a.seq, a.by_seq);
-    h[k] = p.h;
-    slot[k] = M::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)p.s * a.ps[1]) * 4u);
-    if (!in || (uint32_t)slot[k] >= a.pages * a.page) slot[k] = -1;
-    if (active) M::template ld8e<DT>(a.x + (offset(p, a.xs) + u * 8u) * Elem<DT>::ES, x[k]);
-    else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[k][i] = 0.0f;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { const uint32_t m = magnitude(x[k][i]); top = m > top ? m : top; }
-    top = (uint32_t)wave_reduce<GPUOS_IMPL_MAX_LAST>((int32_t)top, width);
-    const Quant q = quant(top, a.format);
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = q.bad ? 0.0f : x[k][i] * q.inv;
-    const v2i w = {(int)pack_q(y, a.format), (int)pack_q(y + 4, a.format)};
-    if (slot[k] >= 0 && active) {
-      const uint32_t page = divided((uint32_t)slot[k], a.by_page), in = (uint32_t)slot[k] - page * a.page;
-      M::st8b(cache_at(a, page, in, h[k]) + u * 8u, w);
-      if ((u & (width - 1u)) == 0) M::stf(scale_at(a, page, in, h[k], u >> lg_width), q.scale);
-    }
-  }
-}
 template <int POL, int DT> DEV void store_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
-  constexpr int U = Elem<DT>::ES == 4 ? 2 : 4;
-  const uint32_t units = a.d / 8u, lg = ceil_log2(units), lanes = 1u << lg;
+  typedef Glob<POL> M;
+  typedef Eight<POL, DT> E;
+  constexpr int U = kCacheBlock;
+  const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
+  const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;      // (the last window ends with the row: what two have both write alike)
   const uint32_t lg_width = a.group == a.d ? lg : ceil_log2(a.group) - 3u, width = 1u << lg_width;
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
-  uint32_t row = begin;
-  for (; row + (U - 1) * step < end; row += U * step) store_pass<POL, DT, U>(a, row + group, step, end, u, u < units, width, lg_width);
-  for (; row < end; row += step) store_pass<POL, DT, 1>(a, row + group, step, end, u, u < units, width, lg_width);
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
+  for (uint32_t base = begin; base < end; base += step) {
+    const uint32_t item = base + group;
+    const Place p = place(a, item < end ? item : end - 1u);
+    const uint32_t heads = item < end && u < units ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
+    const uint64_t xp = a.x + (offset(p, a.xs) + at) * Elem<DT>::ES;
+    const uint32_t slot = (uint32_t)M::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)p.s * a.ps[1]) * 4u);
+    E x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      x[k].clear();
+      if ((uint32_t)k < heads) x[k].load(xp + (uint64_t)k * a.xs[2] * Elem<DT>::ES);
+    }
+    const bool has = slot < a.pages * a.page;
+    const uint32_t page = divided(has ? slot : 0u, a.by_page), in = slot - page * a.page;
+    const uint64_t to = cache_at(a, page, in, p.h) + at, scale_to = scale_at(a, page, in, p.h, u >> lg_width);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (__builtin_amdgcn_ballot_w64((uint32_t)k < heads) == 0) continue;       // (the same in every lane: the maxima need them all)
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { const uint32_t m = magnitude(x[k].get(i)); top = m > top ? m : top; }
+      top = (uint32_t)wave_reduce<GPUOS_IMPL_MAX_LAST>((int32_t)top, width);
+      const Quant q = quant(top, a.format);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = q.bad ? 0.0f : x[k].get(i) * q.inv;
+      const v2i w = {(int)pack_q(y, a.format), (int)pack_q(y + 4, a.format)};
+      if (has && (uint32_t)k < heads) {
+        M::st8b(to + (uint64_t)k * a.cs[2], w);
+        if ((u & (width - 1u)) == 0) M::stf(scale_to + (uint64_t)k * a.ss[2] * 4u, q.scale);
+      }
+    }
+  }
 }
 // rows of any length, strides and alignment: element by element, neighbouring lanes neighbouring elements
 template <int POL> DEV void store_elements(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
@@ -528,13 +559,13 @@ template <int POL> DEV void store_elements(const CacheArgs& a, uint32_t chunk, u
   constexpr int K = 8;
   const uint32_t lg = a.d > 64u ? 6u : ceil_log2(a.d), lanes = 1u << lg, u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t es = float_size(a.dtype);
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
   // A group is the row, or a power of two: then `width` lanes of a register hold it, or `span` registers of all lanes.
   const bool whole = a.group == a.d;
   const uint32_t width = whole || a.group >= lanes ? lanes : a.group, span = whole ? (uint32_t)K : (a.group > lanes ? a.group >> lg : 1u);
   for (uint32_t base = begin; base < end; base += step) {
     const bool in_row = base + group < end;
-    const Place p = place(in_row ? base + group : end - 1u, a.heads, a.by_heads, a.seq, a.by_seq);
+    const Place p = place(a, in_row ? base + group : end - 1u);
     int32_t slot = M::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)p.s * a.ps[1]) * 4u);
     if (!in_row || (uint32_t)slot >= a.pages * a.page) slot = -1;
     const uint64_t xp = a.x + offset(p, a.xs) * es;
@@ -584,56 +615,56 @@ template <int POL> DEV uint32_t sequence_row(const CacheArgs& a, const Place& p,
   page = (uint32_t)Glob<POL>::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)nth * a.ps[1]) * 4u);
   return page < a.pages ? 0u : 2u;
 }
-template <int POL, int DT, int U>
-DEV void load_pass(const CacheArgs& a, uint32_t first, uint32_t step, uint32_t end, uint32_t u, bool active, uint32_t lg_width) {
+template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
-  v2i w[U];
-  float scale[U];
-  uint32_t what[U];
-  uint64_t to[U];
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const uint32_t row = first + k * step;
-    const bool in_row = row < end;
-    const Place p = place(in_row ? row : end - 1u, a.heads, a.by_heads, a.seq, a.by_seq);
-    to[k] = in_row && active ? a.x + (offset(p, a.xs) + u * 8u) * Elem<DT>::ES : 0;
+  constexpr int U = kCacheBlock;
+  const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
+  const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
+  const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;
+  const uint32_t lg_width = a.group == a.d ? lg : ceil_log2(a.group) - 3u;
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
+  if (u >= units) return;
+  for (uint32_t item = begin + group; item < end; item += step) {
+    const Place p = place(a, item);
+    const uint32_t heads = a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U;
+    const uint64_t to = a.x + (offset(p, a.xs) + at) * Elem<DT>::ES;
     uint32_t page, in;
-    what[k] = sequence_row<POL>(a, p, page, in);
-    w[k] = v2i{0, 0};
-    scale[k] = what[k] == 1u ? 0.0f : __builtin_nanf("");
-    if (what[k] == 0u && active) {
-      w[k] = M::ld8b(cache_at(a, page, in, p.h) + u * 8u);
-      scale[k] = M::ldf(scale_at(a, page, in, p.h, u >> lg_width));
+    const uint32_t what = sequence_row<POL>(a, p, page, in);
+    const uint64_t from = cache_at(a, page, in, p.h) + at, scale_from = scale_at(a, page, in, p.h, u >> lg_width);
+    v2i w[U];
+    float scale[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      w[k] = v2i{0, 0};
+      scale[k] = what == 1u ? 0.0f : __builtin_nanf("");
+      if (what == 0u && (uint32_t)k < heads) {
+        w[k] = M::ld8b(from + (uint64_t)k * a.cs[2]);
+        scale[k] = M::ldf(scale_from + (uint64_t)k * a.ss[2] * 4u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if ((uint32_t)k < heads) {
+        float y[8];
+        unpack_q((uint32_t)w[k][0], a.format, y);
+        unpack_q((uint32_t)w[k][1], a.format, y + 4);
+        Eight<POL, DT> o;
+        o.clear();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o.put(i, y[i] * scale[k]);
+        o.store(to + (uint64_t)k * a.xs[2] * Elem<DT>::ES);
+      }
     }
   }
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    float y[8];
-    unpack_q((uint32_t)w[k][0], a.format, y);
-    unpack_q((uint32_t)w[k][1], a.format, y + 4);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] *= scale[k];
-    if (to[k] != 0) M::template st8e<DT>(to[k], y);
-  }
-}
-template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
-  constexpr int U = 4;
-  const uint32_t units = a.d / 8u, lg = ceil_log2(units), lanes = 1u << lg;
-  const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
-  const uint32_t lg_width = a.group == a.d ? lg : ceil_log2(a.group) - 3u;
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
-  uint32_t row = begin;
-  for (; row + (U - 1) * step < end; row += U * step) load_pass<POL, DT, U>(a, row + group, step, end, u, u < units, lg_width);
-  for (; row < end; row += step) load_pass<POL, DT, 1>(a, row + group, step, end, u, u < units, lg_width);
 }
 template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
   constexpr int K = 8;
   const uint32_t lg = a.d > 64u ? 6u : ceil_log2(a.d), lanes = 1u << lg, u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t es = float_size(a.dtype);
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
   for (uint32_t row = begin + group; row < end; row += step) {
-    const Place p = place(row, a.heads, a.by_heads, a.seq, a.by_seq);
+    const Place p = place(a, row);
     uint32_t page, in;
     const uint32_t what = sequence_row<POL>(a, p, page, in);
     const uint64_t from = cache_at(a, page, in, p.h), to = a.x + offset(p, a.xs) * es;
@@ -664,12 +695,12 @@ template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, ui
 //
 // Bound by memory (one read and one write of the logits) while the history is short.  The workgroup takes a row in segments: the
 // tokens of the row's history that fall into the segment are counted in LDS (additions of integers: their order does not matter), then
-// the segment is read, changed and written once.  Every segment reads the row's history, from the cache after the first.
+// the segment is changed and written.  Every segment reads the row's history, from the cache after the first.
 // A count has 31 bits; the top bit says that the token is in the prompt.
 // ---------------------------------------------------------------------------
 struct PenaltyArgs {
   uint64_t x, out, history, prompts, params, bias, allowed;
-  uint32_t xs[2], os[2], hs[2], ps, ms[2], bs[2], as[2], n, seg, segs, v, chunk, rows, dtype[3];
+  uint32_t xs[2], os[2], hs[2], ps, ms[2], bs[2], as[2], n, seg, segs, v, chunk, items, dtype[3];
   Div by_segs;
 };
 template <class P> DEV PenaltyArgs penalty_args(P p) {
@@ -680,7 +711,7 @@ template <class P> DEV PenaltyArgs penalty_args(P p) {
   for (int k = 0; k < 2; ++k) {
     a.xs[k] = uni(p->xs[k]); a.os[k] = uni(p->os[k]); a.hs[k] = uni(p->hs[k]); a.ms[k] = uni(p->ms[k]); a.bs[k] = uni(p->bs[k]); a.as[k] = uni(p->as[k]);
   }
-  a.ps = uni(p->ps); a.n = uni(p->n); a.seg = uni(p->seg); a.segs = uni(p->segs); a.v = uni(p->h.d); a.chunk = uni(p->h.chunk); a.rows = uni(p->h.rows);
+  a.ps = uni(p->ps); a.n = uni(p->n); a.seg = uni(p->seg); a.segs = uni(p->segs); a.v = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
 #pragma unroll
   for (int k = 0; k < 3; ++k) a.dtype[k] = uni((uint32_t)p->h.dtype[k]);
   a.by_segs = uni_div(p->by_segs.mul, p->by_segs.shift);
@@ -695,13 +726,21 @@ DEV float penalize(float v, uint32_t seen, const Penalty& p) {
   }
   return v;
 }
-template <int POL> DEV void count_tokens(const PenaltyArgs& a, uint32_t row, uint32_t v0, uint32_t nv, uint32_t* seen, uint32_t tid) {
+// The history goes by K loads of 16 bytes a lane, the next ones on their way while these are counted (and the first while the counts are
+// cleared).
+template <int POL, uint32_t T> DEV void count_tokens(const PenaltyArgs& a, uint32_t row, uint32_t v0, uint32_t nv, uint32_t* seen, uint32_t tid) {
   typedef Glob<POL> M;
-  constexpr int K = 4;
+  constexpr uint32_t K = 2, kRound = K * T * 4u;
   const uint64_t h = a.history + (uint64_t)row * a.hs[0] * 4u;
   const int32_t prompt = a.prompts != 0 ? M::ldi(a.prompts + (uint64_t)row * a.ps * 4u) : 0;
-  for (uint32_t j = tid; j < (nv + 3u) / 4u; j += kThreads) ((v4i*)seen)[j] = v4i{0, 0, 0, 0};
-  __syncthreads();
+  const uint32_t whole = POL == POL_PLAIN && a.hs[1] == 1u ? a.n & ~3u : 0u;      // what goes by fours
+  auto ask = [&](v4i (&q)[K], uint32_t i) {
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) {
+      q[k] = v4i{-1, -1, -1, -1};
+      if (i + (k * T + tid) * 4u < whole) q[k] = M::ld16(h + ((uint64_t)i + (k * T + tid) * 4u) * 4u);
+    }
+  };
   auto take = [&](int32_t id, uint32_t i) {
     const uint32_t j = (uint32_t)id - v0;              // (an id below v0, negative ones too, is over nv so)
     if (j < nv) {
@@ -709,134 +748,159 @@ template <int POL> DEV void count_tokens(const PenaltyArgs& a, uint32_t row, uin
       else __hip_atomic_fetch_add(&seen[j], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   };
-  uint32_t i = 0;
-  if (POL == POL_PLAIN && a.hs[1] == 1u) {
-    for (; i + K * kThreads * 4u <= a.n; i += K * kThreads * 4u) {
-      v4i q[K];
+  v4i q[K], next[K];
+  ask(q, 0);
+  for (uint32_t j = tid; j < (nv + 3u) / 4u; j += T) ((v4i*)seen)[j] = v4i{0, 0, 0, 0};
+  __syncthreads();
+  for (uint32_t i = 0; i < whole; i += kRound) {
+    ask(next, i + kRound);
 #pragma unroll
-      for (int k = 0; k < K; ++k) q[k] = M::ld16(h + ((uint64_t)i + (k * kThreads + tid) * 4u) * 4u);
+    for (uint32_t k = 0; k < K; ++k) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) take(q[k][e], i + (k * kThreads + tid) * 4u + e);
-      }
+      for (uint32_t e = 0; e < 4; ++e) take(q[k][e], i + (k * T + tid) * 4u + e);
+      q[k] = next[k];
     }
   }
-  for (i += tid; i < a.n; i += K * kThreads) {
-    int32_t id[K];
+  for (uint32_t i = whole + tid; i < a.n; i += 4u * T) {
+    int32_t id[4];
 #pragma unroll
-    for (int k = 0; k < K; ++k) id[k] = i + k * kThreads < a.n ? M::ldi(h + (uint64_t)(i + k * kThreads) * a.hs[1] * 4u) : -1;
+    for (uint32_t k = 0; k < 4; ++k) id[k] = i + k * T < a.n ? M::ldi(h + (uint64_t)(i + k * T) * a.hs[1] * 4u) : -1;
 #pragma unroll
-    for (int k = 0; k < K; ++k) take(id[k], i + k * kThreads);
+    for (uint32_t k = 0; k < 4; ++k) take(id[k], i + k * T);
   }
   __syncthreads();
 }
-// one element of any operand
-template <int POL> DEV void penalize_one(const PenaltyArgs& a, uint32_t row, uint32_t v, uint32_t seen, const Penalty& pen) {
+// one element of any operand, as it is to be written
+template <int POL> DEV float penalized(const PenaltyArgs& a, uint32_t row, uint32_t v, uint32_t seen, const Penalty& pen) {
   typedef Glob<POL> M;
   float y = M::ld_rt(a.x + ((uint64_t)row * a.xs[0] + (uint64_t)v * a.xs[1]) * float_size(a.dtype[0]), a.dtype[0]);
   y = penalize(y, seen, pen);
   if (a.bias != 0) y += M::ld_rt(a.bias + ((uint64_t)row * a.bs[0] + (uint64_t)v * a.bs[1]) * float_size(a.dtype[2]), a.dtype[2]);
   if (a.allowed != 0 && ((M::template at<uint32_t>(a.allowed + ((uint64_t)row * a.as[0] + (uint64_t)(v >> 5) * a.as[1]) * 4u) >> (v & 31u)) & 1u) == 0)
     y = -__builtin_inff();
-  M::st_rt(a.out + ((uint64_t)row * a.os[0] + (uint64_t)v * a.os[1]) * float_size(a.dtype[1]), a.dtype[1], y);
+  return y;
 }
-// DT < 0: element by element
-template <int POL, int DT> DEV void penalty_segments(const PenaltyArgs& a, uint32_t chunk, float* s, uint32_t tid) {
+template <int POL> DEV void put_logit(const PenaltyArgs& a, uint32_t row, uint32_t v, float y) {
+  Glob<POL>::st_rt(a.out + ((uint64_t)row * a.os[0] + (uint64_t)v * a.os[1]) * float_size(a.dtype[1]), a.dtype[1], y);
+}
+// T threads; DT < 0: element by element
+template <int POL, int DT, uint32_t T> DEV void penalty_segments(const PenaltyArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
   uint32_t* seen = (uint32_t*)s;
-  const uint32_t begin = chunk * a.chunk, end = a.rows - begin < a.chunk ? a.rows : begin + a.chunk;
+  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
   for (uint32_t item = begin; item < end; ++item) {
     const uint32_t row = divided(item, a.by_segs), v0 = (item - row * a.segs) * a.seg, nv = a.v - v0 < a.seg ? a.v - v0 : a.seg;
+    if (a.history != 0 && item != begin) __syncthreads();        // (the counts of the segment before have been read)
     Penalty pen = {1.0f, 0.0f, 0.0f};
     if (a.history != 0) {
-      if (item != begin) __syncthreads();              // (the counts of the segment before have been read)
       const uint64_t p = a.params + (uint64_t)row * a.ms[0] * 4u;
       pen = {M::ldf(p), M::ldf(p + (uint64_t)a.ms[1] * 4u), M::ldf(p + (uint64_t)a.ms[1] * 8u)};
-      count_tokens<POL>(a, row, v0, nv, seen, tid);
     }
-    uint32_t done = 0;
-    if constexpr (DT >= 0) {
-      constexpr uint32_t ES = Elem<DT>::ES;
+    if constexpr (DT < 0) {
+      if (a.history != 0) count_tokens<POL, T>(a, row, v0, nv, seen, tid);
+      for (uint32_t j = tid; j < nv; j += T) put_logit<POL>(a, row, v0 + j, penalized<POL>(a, row, v0 + j, a.history != 0 ? seen[j] : 0u, pen));
+    } else {
+      // The segment's elements and bits are asked for before its tokens are counted, eight to a lane.
+      constexpr uint32_t ES = Elem<DT>::ES, U = ModelPack::kSegment / (8u * T);
       const uint64_t xp = a.x + ((uint64_t)row * a.xs[0] + v0) * ES, op = a.out + ((uint64_t)row * a.os[0] + v0) * ES;
       const uint64_t bp = a.bias + ((uint64_t)row * a.bs[0] + v0) * float_size(a.dtype[2]), ap = a.allowed + (uint64_t)row * a.as[0] * 4u;
-      done = nv & ~7u;
-      for (uint32_t j = tid * 8u; j < done; j += kThreads * 8u) {
-        float y[8];
-        M::template ld8e<DT>(xp + j * ES, y);
-        uint32_t bits = 0xffu;
-        if (a.allowed != 0) bits = M::template at<uint32_t>(ap + ((v0 + j) >> 5) * 4u) >> ((v0 + j) & 31u);
-        if (a.history != 0) {
-          const v4i lo = *(const v4i*)(seen + j), hi = *(const v4i*)(seen + j + 4);
-          if ((lo[0] | lo[1] | lo[2] | lo[3] | hi[0] | hi[1] | hi[2] | hi[3]) != 0) {
+      const uint32_t whole = nv & ~7u;
+      Eight<POL, DT> x[U];
+      uint32_t bits[U];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) { y[k] = penalize(y[k], (uint32_t)lo[k], pen); y[4 + k] = penalize(y[4 + k], (uint32_t)hi[k], pen); }
-          }
+      for (uint32_t k = 0; k < U; ++k) {
+        const uint32_t j = (k * T + tid) * 8u;
+        x[k].clear();
+        bits[k] = 0xffu;
+        if (j < whole) {
+          x[k].load(xp + j * ES);
+          if (a.allowed != 0) bits[k] = M::template at<uint32_t>(ap + ((v0 + j) >> 5) * 4u) >> ((v0 + j) & 31u);
         }
-        if (a.bias != 0) {
-          float b[8];
-          if (POL == POL_COHERENT) {
+      }
+      if (a.history != 0) count_tokens<POL, T>(a, row, v0, nv, seen, tid);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) b[k] = M::ld_rt(bp + (j + k) * float_size(a.dtype[2]), a.dtype[2]);
+      for (uint32_t k = 0; k < U; ++k) {
+        const uint32_t j = (k * T + tid) * 8u;
+        if (j >= whole) continue;
+        float b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+        if (a.bias != 0) {
+          if (POL == POL_COHERENT) {                   // (its vectors need an alignment that nothing gives the bias)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = M::ld_rt(bp + (j + i) * float_size(a.dtype[2]), a.dtype[2]);
           } else if (a.dtype[2] == GPUOS_F32) M::template ld8e<GPUOS_F32>(bp + j * 4u, b);
           else if (a.dtype[2] == GPUOS_F16) M::template ld8e<GPUOS_F16>(bp + j * 2u, b);
           else M::template ld8e<GPUOS_BF16>(bp + j * 2u, b);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] += b[k];
         }
+        float y[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = (bits >> k) & 1u ? y[k] : -__builtin_inff();
-        M::template st8e<DT>(op + j * ES, y);
+        for (int i = 0; i < 8; ++i) y[i] = x[k].get(i);
+        if (a.history != 0) {
+          // The penalty costs a division, and few tokens of a segment are in the history: each lane goes through its own, one a step.
+          const v4i lo = *(const v4i*)(seen + j), hi = *(const v4i*)(seen + j + 4);
+          uint32_t left = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) left |= (lo[i] != 0 ? 1u << i : 0u) | (hi[i] != 0 ? 16u << i : 0u);
+          while (left != 0) {
+            const uint32_t at = (uint32_t)__builtin_ctz(left);
+            float v = y[0];
+#pragma unroll
+            for (uint32_t i = 1; i < 8; ++i) v = at == i ? y[i] : v;
+            v = penalize(v, seen[j + at], pen);
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) y[i] = at == i ? v : y[i];
+            left &= left - 1u;
+          }
+        }
+        Eight<POL, DT> o;
+        o.clear();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (a.bias != 0) y[i] += b[i];
+          o.put(i, (bits[k] >> i) & 1u ? y[i] : -__builtin_inff());
+        }
+        o.store(op + j * ES);
       }
+      if (tid < nv - whole) put_logit<POL>(a, row, v0 + whole + tid, penalized<POL>(a, row, v0 + whole + tid, a.history != 0 ? seen[whole + tid] : 0u, pen));
     }
-    for (uint32_t j = done + tid; j < nv; j += kThreads) penalize_one<POL>(a, row, v0 + j, a.history != 0 ? seen[j] : 0u, pen);
   }
 }
-static_assert(ModelPack::kSegment <= kScratchFloats && ModelPack::kSegment % 32 == 0, "a segment's counts fit the LDS scratch; its words of bits are whole");
+constexpr uint32_t kPenaltyThreads = 512;              // of a kernel's workgroup
+static_assert(ModelPack::kSegment <= kScratchFloats && ModelPack::kSegment % (8 * kPenaltyThreads) == 0, "a segment's counts fit the worker's scratch; its vectors are shared out evenly");
 
 // ---------------------------------------------------------------------------
-// the executors of the worker: functions of their own, like its others
+// the executor of a variant; and the worker's, functions of their own like its others
 // ---------------------------------------------------------------------------
-template <int VARIANT> PATHFN void rope_path(const RopeRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t tid) {
-  const RopeArgs a = rope_args(lds_arg(r_v));
-  float* s = lds_arg(s_v);
-  const uint32_t chunk = uni(chunk_v);
-  if constexpr (VARIANT < 12) rope_vectors<POL_COHERENT, VARIANT % 3, (VARIANT / 3) % 2 != 0, VARIANT / 6 != 0>(a, chunk, s, tid);
-  else if constexpr (VARIANT == 12) rope_elements<POL_COHERENT, false>(a, chunk, s, tid);
-  else if constexpr (VARIANT == 13) rope_elements<POL_COHERENT, true>(a, chunk, s, tid);
-  else gamma_sum<POL_COHERENT>(a, chunk, tid);
+template <int POL, uint32_t V, uint32_t T, class P> DEV void run_model(P r, uint32_t chunk, float* s, uint32_t tid) {
+  if constexpr (V < MV_SUM) {
+    constexpr bool GRAD = V >= MV_GRAD;
+    constexpr uint32_t K = V % MV_GRAD;
+    const RopeArgs a = rope_args(&r->rope);
+    if constexpr (K < 6) rope_vectors<POL, K % 3, K / 3 != 0, GRAD>(a, chunk, s, tid);
+    else rope_elements<POL, GRAD>(a, chunk, s, tid);
+  } else if constexpr (V == MV_SUM) {
+    gamma_sum<POL>(rope_args(&r->rope), chunk, s, tid);
+  } else if constexpr (V < MV_LOAD) {
+    const CacheArgs a = cache_args(&r->cache);
+    if constexpr (V < MV_STORE + 3) store_vectors<POL, V - MV_STORE>(a, chunk, tid);
+    else store_elements<POL>(a, chunk, tid);
+  } else if constexpr (V < MV_PENALTY) {
+    const CacheArgs a = cache_args(&r->cache);
+    if constexpr (V < MV_LOAD + 3) load_vectors<POL, V - MV_LOAD>(a, chunk, tid);
+    else load_elements<POL>(a, chunk, tid);
+  } else {
+    penalty_segments<POL, V == MV_PENALTY + 3 ? -1 : (int)(V - MV_PENALTY), T>(penalty_args(&r->penalty), chunk, s, tid);
+  }
 }
-template <int VARIANT> PATHFN void cache_path(const CacheRecord* r_v, uint32_t chunk_v, uint32_t tid) {
-  const CacheArgs a = cache_args(lds_arg(r_v));
-  const uint32_t chunk = uni(chunk_v);
-  if constexpr (VARIANT < 3) store_vectors<POL_COHERENT, VARIANT>(a, chunk, tid);
-  else if constexpr (VARIANT == 3) store_elements<POL_COHERENT>(a, chunk, tid);
-  else if constexpr (VARIANT < 7) load_vectors<POL_COHERENT, VARIANT - 4>(a, chunk, tid);
-  else load_elements<POL_COHERENT>(a, chunk, tid);
+template <uint32_t V> PATHFN void model_path(const ModelRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t tid) {
+  run_model<POL_COHERENT, V, kThreads>((const ModelRecord*)lds_arg(r_v), uni(chunk_v), lds_arg(s_v), tid);
 }
-template <int DT> PATHFN void penalty_path(const PenaltyRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t tid) {
-  const PenaltyArgs a = penalty_args(lds_arg(r_v));
-  penalty_segments<POL_COHERENT, DT>(a, uni(chunk_v), lds_arg(s_v), tid);
-}
-struct RopeExec { template <int K> static DEV void run(const RopeRecord* r, uint32_t chunk, float* s, uint32_t tid) { rope_path<K>(r, chunk, s, tid); } };
-struct CacheExec { template <int K> static DEV void run(const CacheRecord* r, uint32_t chunk, uint32_t tid) { cache_path<K>(r, chunk, tid); } };
-struct PenaltyExec { template <int K> static DEV void run(const PenaltyRecord* r, uint32_t chunk, float* s, uint32_t tid) { penalty_path<K - 1>(r, chunk, s, tid); } };
-
-// which executor a record asks for
-DEV uint32_t rope_variant(uint32_t impl, uint32_t vec, uint32_t dt, bool pairs) {
-  const uint32_t grad = impl == GPUOS_IMPL_NORM_ROPE_GRAD ? 1u : 0u;
-  return impl == GPUOS_IMPL_GAMMA_SUM ? 14u : (vec != 0 ? dt + (pairs ? 3u : 0u) + 6u * grad : 12u + grad);
-}
-DEV uint32_t cache_variant(uint32_t impl, uint32_t vec, uint32_t dt) { return (vec != 0 ? dt : 3u) + (impl == GPUOS_IMPL_CACHE_LOAD ? 4u : 0u); }
-
+struct ModelExec { template <int K> static DEV void run(const ModelRecord* r, uint32_t chunk, float* s, uint32_t tid) { model_path<K>(r, chunk, s, tid); } };
 __attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t wave_v) {
   const ModelRecord* r = lds_arg(r_v);
-  float* s = lds_arg(s_v);
-  const uint32_t chunk = uni(chunk_v), tid = thread_index(uni(wave_v));
-  const uint32_t impl = uni(r->h.impl), vec = uni((uint32_t)r->h.vec), dt = uni((uint32_t)r->h.dtype[0]);
-  if (impl <= GPUOS_IMPL_GAMMA_SUM) pick<0, 15, RopeExec>(rope_variant(impl, vec, dt, (uni((uint32_t)r->h.flags) & MF_PAIRS) != 0), &r->rope, chunk, s, tid);
-  else if (impl != GPUOS_IMPL_LOGIT_PENALTY) pick<0, 8, CacheExec>(cache_variant(impl, vec, dt), &r->cache, chunk, tid);
-  else pick<0, 4, PenaltyExec>(vec != 0 ? dt + 1u : 0u, &r->penalty, chunk, s, tid);
+  const uint32_t v = model_variant(uni(r->h.impl), uni((uint32_t)r->h.vec), uni((uint32_t)r->h.dtype[0]), uni((uint32_t)r->h.flags));
+  pick<0, MV_COUNT, ModelExec>(v, r, uni(chunk_v), lds_arg(s_v), thread_index(uni(wave_v)));
 }
 
 }  // namespace gpuos

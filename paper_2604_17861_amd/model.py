@@ -14,6 +14,7 @@ Shapes: rows of heads are [T, H, D] or [B, S, H, D] of any strides, with one pos
 sequence.  int32 is the only integer type.  Everything here is checking of shapes and marshalling.
 """
 import struct
+from array import array
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -46,11 +47,55 @@ def launch(*tasks, device=None):
     R.launch_model(tasks[0] if len(tasks) == 1 else b"".join(tasks), stream.device_index, stream.cuda_stream)
 
 
-def _launch_some(rows, tasks):
-    """launch, without the tasks that have nothing to do (an empty tensor has no address)."""
-    tasks = [t for x, t in zip(rows, tasks) if x.numel() != 0]
-    if tasks:
-        launch(*tasks, device=rows[0].device)
+# A call's descriptors by everything about it but addresses: checked and packed once, then only the addresses are put in.  (Checking and
+# packing one of five operands takes 6.5 us, looking it up 2.)
+_plans = {}
+_WORDS = S.MODEL_TASK_BYTES // 8
+_POINTER = 9                       # word of the first operand's address; the others' every six words
+
+
+def _sig(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device(), t.is_neg())
+
+
+class _Plan:
+    """The descriptors of one or more tasks, without those that have nothing to do (an empty tensor has no address).
+    rows: what tells which those are; operands: of every task, in the descriptor's order (None: left out)."""
+    __slots__ = ("words", "n", "device", "at")
+
+    def __init__(self, rows, tasks, operands):
+        tasks = [t for x, t in zip(rows, tasks) if x.numel() != 0]
+        self.words = array("Q", b"".join(tasks))
+        self.n, self.device = len(tasks), rows[0].get_device()
+        self.at = []                                        # (word, which of all the operands)
+        first, place = 0, 0
+        for x, mine in zip(rows, operands):
+            if x.numel() != 0:
+                for o in range(8):
+                    self.words[first + _POINTER + 6 * o] = 0
+                self.at += [(first + _POINTER + 6 * o, place + o) for o, t in enumerate(mine) if t is not None]
+                first += _WORDS
+            place += len(mine)
+
+
+def _keep(key, plan):
+    if len(_plans) >= 4096:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _run(plan, operands):
+    """Launch with these addresses: the operands of all tasks, one after the other."""
+    if plan.n:
+        words = plan.words[:]
+        for word, k in plan.at:
+            words[word] = operands[k].data_ptr()
+        R.launch_model_at(words.buffer_info()[0], plan.n, plan.device, _stream_of(plan.device))
+
+
+# the handle of a device's current stream: torch.cuda.current_stream(device).cuda_stream, which makes two objects for it (1.1 us)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 # ---- descriptors -----------------------------------------------------------------------------------
@@ -223,13 +268,13 @@ def penalty_task(x, out, history=None, prompt_lengths=None, params=None, bias=No
 # ---- norm and rotation -----------------------------------------------------------------------------
 
 def _parts(x):
-    """Shares of gamma's gradient: as many as there are passes of a workgroup (16 rows of 128), at most PARTS_MAX."""
+    """Shares of gamma's gradient: as many as there are passes of a workgroup (32 rows of 128), at most PARTS_MAX."""
     rows = x.numel() // x.shape[-1]
-    return min(PARTS_MAX, max(1, rows // 16))
+    return min(PARTS_MAX, max(1, rows // 32))
 
 
 def _empty_like(x):
-    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 class _NormRope(torch.autograd.Function):
@@ -250,30 +295,38 @@ class _NormRope(torch.autograd.Function):
 
 
 def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
+    key = ("norm_rope", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in outs])
+    plan = _plans.get(key)
     outs = [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
-    _launch_some(xs, [norm_rope_task(x, g, table, positions, o, eps=eps, pairs=pairs) for x, g, o in zip(xs, gammas, outs)])
+    operands = [(x, g, table, positions, o) for x, g, o in zip(xs, gammas, outs)]
+    if plan is None:
+        plan = _keep(key, _Plan(xs, [norm_rope_task(*o, eps=eps, pairs=pairs) for o in operands], operands))
+    _run(plan, sum(operands, ()))
     return tuple(outs)
 
 
 def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
-    dxs, dgs, tasks, sums, partials = [], [], [], [], []       # (descriptors keep no memory: partials live until the launch)
+    key = ("backward", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in douts])
+    plans = _plans.get(key)
+    dxs, dgs, grads, sums = [], [], [], []
     for dout, x, gamma in zip(douts, xs, gammas):
-        dx = _empty_like(x)
-        dg = partial = None
+        dx, dg, partial = _empty_like(x), None, None
         if gamma is not None:
             if x.numel() == 0:
                 dg = torch.zeros_like(gamma)
             else:
-                dg = _empty_like(gamma)
-                partial = torch.empty((x.shape[-1], _parts(x)), dtype=torch.float32, device=x.device)
-                partials.append(partial)
-                sums.append(gamma_sum_task(partial, dg))
-        if x.numel() != 0:
-            tasks.append(norm_rope_grad_task(dout, x, gamma, table, positions, dx, partial, eps=eps, pairs=pairs))
+                dg, partial = _empty_like(gamma), x.new_empty((x.shape[-1], _parts(x)), dtype=torch.float32)
+                sums.append((partial, dg))
+        grads.append((x, gamma, table, positions, dx, dout, partial))
         dxs.append(dx)
         dgs.append(dg)
-    if tasks:
-        launch(*tasks, *sums, device=xs[0].device)
+    if plans is None:
+        plans = _keep(key, (
+            _Plan(xs, [norm_rope_grad_task(o[5], *o[:5], o[6], eps=eps, pairs=pairs) for o in grads], grads),
+            _Plan([o[0] for o in sums], [gamma_sum_task(*o) for o in sums], sums) if sums else None))
+    _run(plans[0], sum(grads, ()))
+    if sums:
+        _run(plans[1], sum(sums, ()))
     return dxs, dgs
 
 
@@ -314,38 +367,50 @@ def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, 
 
 # ---- the cache -------------------------------------------------------------------------------------
 
+def _store(xs, slots, caches, scales):
+    key = ("store", _sig(slots), *[_sig(t) for t in xs], *[_sig(t) for t in caches], *[_sig(t) for t in scales])
+    plan = _plans.get(key)
+    operands = [(x, slots, c, s) for x, c, s in zip(xs, caches, scales)]
+    if plan is None:
+        plan = _keep(key, _Plan(xs, [cache_store_task(*o) for o in operands], operands))
+    _run(plan, sum(operands, ()))
+
+
 def cache_store(x, slots, cache, scales):
     """Quantise rows of x [T, H, D] (or [B, S, H, D]) into slots (page index * page + place; negative: nowhere) of cache
     [pages, page, H, D] (int8 or float8_e4m3fn) and scales [pages, page, H, groups] (float32).  Slots are distinct."""
-    _launch_some((x,), (cache_store_task(x, slots, cache, scales),))
+    _store((x,), slots, (cache,), (scales,))
 
 
 def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
     """cache_store of keys and values in one launch."""
-    _launch_some((k, v), (cache_store_task(k, slots, k_cache, k_scales), cache_store_task(v, slots, v_cache, v_scales)))
+    _store((k, v), slots, (k_cache, v_cache), (k_scales, v_scales))
 
 
-def _load_out(cache, pages, length, dtype, out):
-    if out is not None:
-        return out
-    _check(cache, "cache", _CACHE, (4,))
-    _check(pages, "pages", _INT, (2,), None, cache.device)
-    return torch.empty((pages.shape[0], length, *cache.shape[2:]), dtype=dtype, device=cache.device)
+def _load(caches, scales, pages, lengths, length, dtype, outs):
+    key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
+    plan = _plans.get(key)
+    if plan is None:
+        for c in caches:
+            _check(c, "cache", _CACHE, (4,))
+        _check(pages, "pages", _INT, (2,), None, caches[0].device)
+    outs = [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype) if o is None else o for c, o in zip(caches, outs)]
+    operands = [(c, s, pages, lengths, o) for c, s, o in zip(caches, scales, outs)]
+    if plan is None:
+        plan = _keep(key, _Plan(outs, [cache_load_task(*o) for o in operands], operands))
+    _run(plan, sum(operands, ()))
+    return tuple(outs)
 
 
 def cache_load(cache, scales, pages, lengths, length, *, dtype=torch.float32, out=None):
     """The first lengths[b] rows (None: all `length`) of every sequence b, through pages [B, width], as [B, length, H, D];
     zeros behind them."""
-    out = _load_out(cache, pages, length, dtype, out)
-    _launch_some((out,), (cache_load_task(cache, scales, pages, lengths, out),))
-    return out
+    return _load((cache,), (scales,), pages, lengths, length, dtype, (out,))[0]
 
 
 def cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, length, *, dtype=torch.float32, out=(None, None)):
     """cache_load of keys and values in one launch: (k, v)."""
-    k, v = _load_out(k_cache, pages, length, dtype, out[0]), _load_out(v_cache, pages, length, dtype, out[1])
-    _launch_some((k, v), (cache_load_task(k_cache, k_scales, pages, lengths, k), cache_load_task(v_cache, v_scales, pages, lengths, v)))
-    return k, v
+    return _load((k_cache, v_cache), (k_scales, v_scales), pages, lengths, length, dtype, out)
 
 
 # ---- logits ----------------------------------------------------------------------------------------
@@ -354,7 +419,16 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
     """Penalties of the tokens in history [B, N] (entries that are no token count for nothing; the first prompt_lengths[b] for the
     repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
     not set.  out may be x."""
-    _check(x, "x", _FLOAT, (2,))
+    key = ("penalty", _sig(x), _sig(history), _sig(prompt_lengths), _sig(params), _sig(bias), _sig(allowed), _sig(out))
+    plan = _plans.get(key)
+    if plan is None:
+        _check(x, "x", _FLOAT, (2,))
     out = _empty_like(x) if out is None else out
-    _launch_some((x,), (penalty_task(x, out, history, prompt_lengths, params, bias, allowed),))
+    operands = (x, out, history, prompt_lengths, params, bias, allowed)
+    if plan is None:
+        task = penalty_task(*operands)
+        if history is not None and history.shape[1] == 0:   # (nothing is counted: as without one)
+            operands = (x, out, None, None, None, bias, allowed)
+        plan = _keep(key, _Plan((x,), (task,), (operands,)))
+    _run(plan, operands)
     return out

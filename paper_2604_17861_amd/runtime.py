@@ -429,20 +429,27 @@ def _model_count(tasks):
     return len(tasks) // S.MODEL_TASK_BYTES
 
 
-_model_table = None
+_launch_model = _model_table = None
 
 
 def launch_model(tasks, device=0, stream=0, table=None):
     """gpuos_launch_model: model operators' descriptors (bytes, as `model` makes them) as ordinary kernels on `stream` (a
     stream's handle).  table: logical operator -> implementation (None: streams.MODEL_OP's)."""
-    global _model_table
     if table is None:
-        if _model_table is None:
-            _model_table = _impl_table({S.MODEL_OP[name]: impl for name, impl in S.MODEL_IMPL.items()})
-        impl = _model_table
+        launch_model_at(tasks, _model_count(tasks), device, stream)
     else:
-        impl = _impl_table(table)
-    _check(lib().gpuos_launch_model(device, tasks, _model_count(tasks), impl, stream), "gpuos_launch_model")
+        _check(lib().gpuos_launch_model(device, tasks, _model_count(tasks), _impl_table(table), stream), "gpuos_launch_model")
+
+
+def launch_model_at(tasks, n, device, stream):
+    """launch_model of n descriptors at an address."""
+    global _launch_model, _model_table
+    if _launch_model is None:
+        _model_table = _impl_table({S.MODEL_OP[name]: impl for name, impl in S.MODEL_IMPL.items()})
+        _launch_model = lib().gpuos_launch_model
+    rc = _launch_model(device, tasks, n, _model_table, stream)
+    if rc != OK:
+        raise GpuosError(rc, "gpuos_launch_model")
 
 
 def _impl_table(table):
@@ -453,11 +460,12 @@ def _impl_table(table):
 
 
 def model_plan(task, impl):
-    """gpuos_model_plan of one descriptor: how it is run and cut."""
-    out = (ctypes.c_uint32 * 6)()
+    """gpuos_model_plan of one descriptor: how it is run and cut, as a task of the ring and as a kernel."""
+    out = (ctypes.c_uint32 * 8)()
     assert _model_count(task) == 1
     _check(lib().gpuos_model_plan(task, int(impl), out), "gpuos_model_plan")
-    return dict(zip(("vectors", "ring_chunks", "ring_rows", "chunks", "rows", "segment"), (int(x) for x in out)))
+    keys = ("vectors", "chunks", "items", "item")
+    return dict(zip(keys, out[:4])), dict(zip(keys, out[4:]))
 
 
 def task_bytes(tasks, impls):

@@ -144,6 +144,18 @@ ROPE = [
     ((3, 2, 512), 10, True, F16, F32, "plain", "each"),
     ((1000, 12, 64), 64, False, F16, F16, "plain", "each"),         # more rows than one pass of all chunks
     ((130, 3, 24), 0, False, BF16, F32, "plain", None),
+    # parts that are no whole number of windows
+    ((37, 5, 66), 66, False, BF16, F32, "plain", "each"),
+    ((37, 5, 66), 20, True, F16, F32, "fused", "each"),
+    ((19, 6, 64), 20, False, F32, BF16, "plain", "each"),
+    ((2, 19, 7, 100), 100, False, BF16, BF16, "heads", "each"),
+    ((19, 3, 100), 100, True, F16, F16, "wide", "each"),
+    ((19, 3, 90), 10, False, F16, F16, "plain", "each"),
+    ((19, 4, 90), 82, False, F32, F32, "wide", "each"),
+    ((33, 4, 12), 8, False, F32, F32, "plain", "each"),
+    ((33, 4, 4), 0, False, BF16, F32, "plain", None),
+    ((9, 9, 250), 250, True, BF16, F32, "plain", "each"),
+    ((9, 2, 510), 508, False, BF16, F32, "plain", "each"),          # a rest of two: element by element
 ]
 
 
@@ -257,6 +269,28 @@ def test_positions_outside_the_table_and_values_without_a_norm(route):
         assert torch.isnan(o[2]).all() if dtype == F32 else (o[2] == 0).all()      # 0 * 1 / sqrt(0); with epsilon 0
 
 
+@pytest.mark.parametrize("route", ROUTES)
+@pytest.mark.parametrize("pairs", (False, True))
+@pytest.mark.parametrize("d,r", ((64, 32), (66, 20), (65, 32)))
+def test_an_infinity_reaches_its_own_pair_only(d, r, pairs, route):
+    gen, x, g, table, p = rope_inputs((4, 2, d), r, F32, F32, "each", 3)
+    for t, j in enumerate((0, r - 1, r, d - 1)):
+        x[t, 0, j] = float("inf")
+    want, _ = ref.norm_rope(x, g, table, p, 1e-6, pairs)
+    out = torch.zeros(4, 2, d, device="cuda")
+    run(route, M.norm_rope_task(up(x), up(g), up(table), up(p), out, pairs=pairs))
+    assert torch.equal(torch.isnan(out.cpu()), torch.isnan(want)) and (out.cpu()[:, 0].nan_to_num() == 0).all()
+    # and backwards from dout: elements that are not rotated stay by themselves
+    x = normal(gen, 4, 2, d)
+    dz = normal(gen, 4, 2, d)
+    dz[:, :, d - 1] = float("inf")
+    dx = torch.zeros(4, 2, d, device="cuda")
+    partial = torch.zeros(d, 3, device="cuda")
+    run(route, M.norm_rope_grad_task(up(dz), up(x), up(g), up(table), up(p), dx, partial, pairs=pairs))
+    dg = partial.sum(1).cpu()
+    assert torch.isfinite(dg[:d - 1]).all() and not torch.isfinite(dg[d - 1])
+
+
 def cache_of(pages, page, h, d, groups, fmt, layout):
     """A cache with something in it, on the CPU and on the GPU in some layout."""
     gen = torch.Generator().manual_seed(3)
@@ -294,6 +328,10 @@ CACHE = [
     ((7,), 1, 512, 1, torch.float8_e4m3fn, 5, F16, "plain", "plain"),
     ((7,), 1, 512, 2, torch.int8, 5, F16, "wide", "odd"),
     ((1500,), 8, 64, 2, torch.int8, 64, F16, "plain", "plain"),
+    ((50,), 5, 100, 1, torch.int8, 16, BF16, "plain", "plain"),
+    ((50,), 6, 250, 1, torch.float8_e4m3fn, 16, F32, "wide", "odd"),
+    ((50,), 7, 9, 1, torch.int8, 16, F16, "fused", "heads"),
+    ((50,), 9, 8, 1, torch.float8_e4m3fn, 16, F16, "plain", "plain"),
 ]
 
 

@@ -95,7 +95,7 @@ BAD = {
 
 @pytest.mark.parametrize("case", range(len(GOOD)))
 def test_descriptors_that_are_taken(case):
-    assert isinstance(GOOD[case](), dict)
+    assert isinstance(GOOD[case](), tuple)
 
 
 @pytest.mark.parametrize("what", list(BAD))
@@ -112,10 +112,10 @@ def test_an_unknown_implementation_is_refused():
 
 
 def test_empty_sizes_are_empty_tasks():
-    for p in (rope(b=0), rope(s=0), rope(h=0), store(s=0), load(b=0), load(l=0), penalty(b=0), penalty(v=0),
-              plan("GAMMA_SUM", (0, 5), (op(F32, 5, 1), op(BF16, 1)))):
-        assert p["vectors"] == 2 and p["ring_chunks"] == p["chunks"] == 1
-    assert grad(b=0)["vectors"] == 0 and grad(b=0)["chunks"] == 5      # its shares are written all the same
+    for plans in (rope(b=0), rope(s=0), rope(h=0), store(s=0), load(b=0), load(l=0), penalty(b=0), penalty(v=0),
+                  plan("GAMMA_SUM", (0, 5), (op(F32, 5, 1), op(BF16, 1)))):
+        assert all(p["vectors"] == 2 and p["chunks"] == 1 for p in plans)
+    assert all(p["vectors"] == 0 and p["chunks"] == 5 for p in grad(b=0))      # its shares are written all the same
 
 
 def test_chunks_cover_every_row_once_and_stay_in_their_bounds():
@@ -124,31 +124,37 @@ def test_chunks_cover_every_row_once_and_stay_in_their_bounds():
         b, s, h = (int(2 ** rng.uniform(0, k)) for k in (6, 11, 5))
         d = int(rng.integers(1, 513))
         r = 2 * int(rng.integers(0, d // 2 + 1))
-        rows, items = b * s * h, None
         kind = rng.integers(0, 4)
         if kind == 0:
-            p = rope(b, s, h, d, r, table=op(F32, r, 1) if r else NO, positions=op(I32, s, 1) if r else NO)
+            plans = rope(b, s, h, d, r, table=op(F32, r, 1) if r else NO, positions=op(I32, s, 1) if r else NO)
         elif kind == 1:
-            p = store(b, s, h, d)
+            plans = store(b, s, h, d)
         elif kind == 2:
-            p = load(b, s, h, d, width=s // 16 + 1)
+            plans = load(b, s, h, d, width=s // 16 + 1)
         else:
             v = int(2 ** rng.uniform(0, 18))
-            p = penalty(b, v)
-            rows = b * -(-v // p["segment"])
-            assert 0 < p["segment"] <= 7168
-        for chunks, per, most in ((p["ring_chunks"], p["ring_rows"], 1024), (p["chunks"], p["rows"], 2048)):
-            assert 1 <= chunks <= most and (chunks - 1) * per < rows <= chunks * per
+            plans = penalty(b, v)
+        for p, most in zip(plans, (1024, 2048)):
+            assert p["item"] >= 1 and (kind != 3 or p["item"] <= 7168)         # (a segment's counts lie in LDS)
+            items = b * -(-v // p["item"]) if kind == 3 else b * s * -(-h // p["item"])
+            assert 1 <= p["chunks"] <= most and (p["chunks"] - 1) * p["items"] < items <= p["chunks"] * p["items"]
     for parts in (1, 3, 1024):
-        p = grad(b=7, s=11, parts=parts)
-        assert p["chunks"] == p["ring_chunks"] == parts and p["rows"] * parts >= 7 * 11 * 4
+        for p in grad(b=7, s=11, parts=parts):
+            assert p["chunks"] == parts and p["items"] * parts * p["item"] >= 7 * 11 * 4
 
 
 def test_rows_go_in_vectors_where_they_can():
-    assert rope()["vectors"] == 1 and store()["vectors"] == 1 and load()["vectors"] == 1 and penalty()["vectors"] == 1
-    assert rope(d=60, r=0, table=NO, positions=NO)["vectors"] == 0 and rope(d=64, r=20)["vectors"] == 0
-    assert rope(out=op(F16, 768, 256, 64, 1))["vectors"] == 0 and rope(x=op(BF16, 1536, 512, 128, 2))["vectors"] == 0
-    assert store(d=60)["vectors"] == 0 and penalty(x=op(F32, 2000, 2))["vectors"] == 0
+    both = lambda plans: tuple(p["vectors"] for p in plans)
+    none = dict(r=0, table=NO, positions=NO)
+    for plans in (rope(), rope(flags=4), grad(), store(), load(), penalty(), rope(d=48, **none), store(d=64, groups=8)):
+        assert both(plans) == (1, 1)
+    # a kernel takes them from any address and to any end, the ring on eight bytes
+    for plans in (rope(d=60, **none), rope(d=64, r=20), rope(d=66, r=66, flags=4), rope(x=op(BF16, 769, 257, 65, 1)), rope(x=op(BF16, 768, 256, 64, 1, ptr=AT + 2)),
+                  store(d=60), load(d=100), store(cache=op(I8, 2049, 129, 65, 1)), penalty(v=1001)):
+        assert both(plans) == (0, 1)
+    for plans in (rope(d=65, r=64), rope(d=64, r=6), rope(d=67, r=4, flags=4), rope(d=6, **{**none, "flags": 4}), rope(out=op(F16, 768, 256, 64, 1)),
+                  rope(x=op(BF16, 1536, 512, 128, 2)), store(d=7), load(out=op(F16, 7680, 256, 128, 2)), penalty(x=op(F32, 2000, 2)), penalty(bias=op(F32, 0, 2))):
+        assert both(plans) == (0, 0)
 
 
 def test_the_binding_checks_what_the_library_cannot_see():
