@@ -2879,12 +2879,9 @@ DEV bool rowop_is_other(const RecHead& h) {
   const uint32_t path = h.path();
   return path == PATH_ROW_RAGGED || (path == PATH_ROW_FUSED && h.red_n() > (h.dtype_out() == GPUOS_F32 ? 4096u : 8192u));
 }
-// ... and those of them that the worker runs by exec_away: softmax rows that do not fit the registers; and model operators
+// ... and those of them that the worker runs by exec_away: softmax rows that do not fit the registers
 DEV bool rowop_is_away(const RecHead& h, uint32_t impl) {
   const uint32_t path = h.path();
-#if !defined(__HIPCC_RTC__)
-  if (path == PATH_MODEL) return impl >= GPUOS_IMPL_NORM_ROPE && impl <= GPUOS_IMPL_LOGIT_PENALTY;      // (else it has been killed)
-#endif
   return impl == GPUOS_IMPL_SOFTMAX_LAST && (path == PATH_ROW_RAGGED || path == PATH_ROW_FUSED) && h.red_n() > 16384u;
 }
 template <int POL, int ROP>
@@ -3097,6 +3094,10 @@ DEV int32_t exec_program(const Record* r, const RecHead& h, uint32_t impl, uint3
   return status;
 }
 
+#if !defined(__HIPCC_RTC__)
+union ModelRecord;
+__attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r, uint32_t chunk, float* s, uint32_t tid);      // gpuos_model_device.h
+#endif
 // returns the task status contribution of this chunk (0 or an error)
 template <int POL>
 DEV int32_t exec_chunk(const Record* r, const RecHead& h, uint32_t impl, uint32_t chunk, float* s_red, const ProgramImage* progs, uint32_t tid) {
@@ -3132,7 +3133,14 @@ DEV int32_t exec_chunk(const Record* r, const RecHead& h, uint32_t impl, uint32_
     case GPUOS_IMPL_MASKED_SOFTMAX_LAST: run_rowop<POL, GPUOS_IMPL_MASKED_SOFTMAX_LAST>(r, h, chunk, s_red, tid); break;
     case GPUOS_IMPL_LAYERNORM_LAST: run_rowop<POL, GPUOS_IMPL_LAYERNORM_LAST>(r, h, chunk, s_red, tid); break;
     case GPUOS_IMPL_FAIL: return GPUOS_E_BADOP;       // kill-switch stub: fail fast, write nothing
-    default: return GPUOS_E_BADOP;
+    default:
+#if !defined(__HIPCC_RTC__)
+      if (POL == POL_COHERENT && impl >= GPUOS_IMPL_NORM_ROPE && impl <= GPUOS_IMPL_LOGIT_PENALTY && h.path() == PATH_MODEL) {
+        exec_model((const ModelRecord*)r, chunk, s_red, tid);
+        break;
+      }
+#endif
+      return GPUOS_E_BADOP;
   }
   return GPUOS_OK;
 }
@@ -3562,20 +3570,10 @@ __attribute__((not_tail_called)) PATHFN void softmax_away(WorkShared* s_v, uint3
   const uint32_t per = uni(r->chunk), rows = uni(r->numel), begin = (uni((uint32_t)dec[2]) & 0x3ffu) * per;
   softmax_held_rows<POL_COHERENT, DT, RAGGED>(r, begin, rows - begin < per ? rows : begin + per, s->red, tid);
 }
-#if !defined(__HIPCC_RTC__)
-union ModelRecord;
-__attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r, uint32_t chunk, float* s, uint32_t wave);      // gpuos_model_device.h
-#endif
 __attribute__((not_tail_called)) PATHFN void exec_away(WorkShared* s_v, uint32_t wave_v) {
   WorkShared* s = lds_arg(s_v);
   const uint32_t wave = uni(wave_v);
   const Record* r = &s->rec[(uni(s->dec[0]) >> 8) & 0xffu];
-#if !defined(__HIPCC_RTC__)
-  if (uni((uint32_t)r->path) == PATH_MODEL) {
-    exec_model((const ModelRecord*)r, uni(s->dec[2]) & 0x3ffu, s->red, wave);
-    return;
-  }
-#endif
   const uint32_t k = 2u * uni(r->dtype[3]) + (uni(r->path) == PATH_ROW_RAGGED ? 1u : 0u);
   if (k < 2u) { if (k == 0) softmax_away<GPUOS_F32, false>(s, thread_index(wave)); else softmax_away<GPUOS_F32, true>(s, thread_index(wave)); }
   else if (k < 4u) { if (k == 2) softmax_away<GPUOS_F16, false>(s, thread_index(wave)); else softmax_away<GPUOS_F16, true>(s, thread_index(wave)); }

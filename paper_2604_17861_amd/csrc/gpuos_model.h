@@ -113,7 +113,10 @@ constexpr uint32_t kModelRow = 512;          // elements of a head, at most: 64 
 constexpr uint32_t kModelParts = 1024;       // shares of the gradient of gamma, at most (a unit names its chunk in ten bits)
 // Lanes that a row of vectors takes: a lane has four pairs, or eight elements that are not rotated (neighbours: eight elements).
 GPUOS_HD inline uint32_t rope_units(uint32_t d, uint32_t half, bool pairs) { return pairs ? (d + 7u) / 8u : (half + 3u) / 4u + (d - 2u * half + 7u) / 8u; }
-constexpr uint32_t kRopeBlock = 4, kGradBlock = 2, kCacheBlock = 4;      // heads of an item that goes in vectors
+// Heads of an item that goes in vectors.  The worker has twelve wavefronts on a compute unit where a kernel has up to thirty-two, so
+// its have more on their way each.
+GPUOS_HD constexpr uint32_t rope_block(bool ring, bool grad) { return (grad ? 2u : 4u) * (ring ? 2u : 1u); }
+GPUOS_HD constexpr uint32_t cache_block(bool ring) { return ring ? 8u : 4u; }
 constexpr uint32_t kModelLaunch = 8;         // tasks of one launch: their records are kernel arguments, 2 KB of the 4 KB there may be
 
 // What gpuos_launch_model hands a kernel: tasks of one variant.  (A block's second index is its task's place here: its
@@ -297,7 +300,7 @@ class ModelPack {
         (!cut.aligned || (d % 8 == 0 && r.half % 4 == 0)) && vectors(cut, r.x, es, r.xs, 3, last) && vectors(cut, r.out, es, r.os, 3, last) &&
         vectors(cut, r.dout, es, r.zs, 3, last) && vectors(cut, r.table, 4, &r.ts, 1, true))
       r.h.vec = 1;
-    in_blocks(r, (uint64_t)tokens, r.h.vec ? (grad ? kGradBlock : kRopeBlock) : 1);
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? rope_block(cut.aligned, grad) : 1);
     cut_items(r.h, cut, (uint64_t)d * es * (grad ? 3 : 2) * r.h.block, rows_at_once(r.h.vec ? rope_units((uint32_t)d, r.half, pairs) : (uint32_t)(d + 1) / 2));
     if (grad && part->ptr) {
       const int64_t parts = z[6], cz[2] = {d, parts};
@@ -370,7 +373,7 @@ class ModelPack {
     // Vectors: a lane takes eight elements of a row, 8 bytes of the cache.  (A row that is no whole number of eights is one group.)
     const uint32_t es = size_of(x.dtype);
     if (d >= 8 && (!cut.aligned || d % 8 == 0) && vectors(cut, r.x, es, r.xs, 3, r.xs[3] == 1) && vectors(cut, r.cache, 1, r.cs, 3, true)) r.h.vec = 1;
-    in_blocks(r, (uint64_t)tokens, r.h.vec ? kCacheBlock : 1);
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? cache_block(cut.aligned) : 1);
     cut_items(r.h, cut, (uint64_t)d * (es + 1) * r.h.block, rows_at_once(r.h.vec ? (uint32_t)(d + 7) / 8 : (uint32_t)d));
     return GPUOS_OK;
   }

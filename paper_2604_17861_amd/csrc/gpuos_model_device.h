@@ -193,7 +193,7 @@ DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid)
   typedef Glob<POL> M;
   typedef Eight<POL, DT> E;
   constexpr uint32_t ES = Elem<DT>::ES;
-  constexpr int U = GRAD ? kGradBlock : kRopeBlock;
+  constexpr int U = rope_block(POL == POL_COHERENT, GRAD);
   // A lane's eight elements are two windows of four, oa and ob on.  Halves: the same four of either half, or eight that follow
   // each other behind them; neighbours: eight that follow each other.  The last window of a part that is no whole number of them begins
   // early and ends with it: what it shares with the one before (below `from`) both compute and store, and only that one sums.
@@ -513,7 +513,7 @@ DEV uint64_t scale_at(const CacheArgs& a, uint32_t page, uint32_t in, uint32_t h
 template <int POL, int DT> DEV void store_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
   typedef Eight<POL, DT> E;
-  constexpr int U = kCacheBlock;
+  constexpr int U = cache_block(POL == POL_COHERENT);
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;      // (the last window ends with the row: what two have both write alike)
@@ -617,7 +617,7 @@ template <int POL> DEV uint32_t sequence_row(const CacheArgs& a, const Place& p,
 }
 template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
-  constexpr int U = kCacheBlock;
+  constexpr int U = cache_block(POL == POL_COHERENT);
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;
@@ -897,10 +897,10 @@ template <uint32_t V> PATHFN void model_path(const ModelRecord* r_v, uint32_t ch
   run_model<POL_COHERENT, V, kThreads>((const ModelRecord*)lds_arg(r_v), uni(chunk_v), lds_arg(s_v), tid);
 }
 struct ModelExec { template <int K> static DEV void run(const ModelRecord* r, uint32_t chunk, float* s, uint32_t tid) { model_path<K>(r, chunk, s, tid); } };
-__attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t wave_v) {
+__attribute__((not_tail_called)) PATHFN void exec_model(const ModelRecord* r_v, uint32_t chunk_v, float* s_v, uint32_t tid) {
   const ModelRecord* r = lds_arg(r_v);
   const uint32_t v = model_variant(uni(r->h.impl), uni((uint32_t)r->h.vec), uni((uint32_t)r->h.dtype[0]), uni((uint32_t)r->h.flags));
-  pick<0, MV_COUNT, ModelExec>(v, r, uni(chunk_v), lds_arg(s_v), thread_index(uni(wave_v)));
+  pick<0, MV_COUNT, ModelExec>(v, r, uni(chunk_v), lds_arg(s_v), tid);
 }
 
 }  // namespace gpuos
