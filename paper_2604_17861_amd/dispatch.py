@@ -462,17 +462,33 @@ class GpuosMode(TorchDispatchMode):
     # ---- PyTorch's own path -------------------------------------------------------------------
     def _normal_path(self, func, args, kwargs):
         if self._touch:
-            newest = -1
-            for t in _tensors(args, kwargs):
-                if t.device == self.device:
-                    k = self._touch.get(t.data_ptr() - t.storage_offset() * t.element_size())
-                    if k is not None and k > newest:
-                        newest = k
-            if newest >= 0:
-                self._wait(newest)
+            self._await(_tensors(args, kwargs))
         out = func(*args, **kwargs)
         self._dirty = True
         return out
+
+    def _await(self, tensors):
+        """Until no pending task reads or writes the memory of these."""
+        newest = -1
+        for t in tensors:
+            if t.device == self.device:
+                k = self._touch.get(t.data_ptr() - t.storage_offset() * t.element_size())
+                if k is not None and k > newest:
+                    newest = k
+        if newest >= 0:
+            self._wait(newest)
+
+    def settle(self, tensors):
+        """Before a kernel that this filter does not see is launched on PyTorch's stream: waits for pending tasks on these tensors
+        (None: left out), and takes it that the stream has work of its own from now on."""
+        if self._touch:
+            self._await([t for t in tensors if t is not None])
+        self._dirty = True
+
+    def __enter__(self):
+        r = super().__enter__()
+        R.active_filters.append(self)
+        return r
 
     def _wait(self, ticket):
         """Until `ticket` and every ticket before it have completed (tasks complete in any order, and
@@ -510,6 +526,7 @@ class GpuosMode(TorchDispatchMode):
         try:
             self.synchronize()
         finally:
+            R.active_filters.remove(self)
             r = super().__exit__(*exc)
         return r
 

@@ -42,7 +42,8 @@ def register(rt):
 
 
 def launch(*tasks, device=None):
-    """Descriptors as kernels on the current stream of `device` (None: the current device)."""
+    """Descriptors as kernels on the current stream of `device` (None: the current device).  Under a dispatch filter its tasks on
+    these tensors have to be complete (GpuosMode.settle)."""
     stream = torch.cuda.current_stream(device)
     R.launch_model(tasks[0] if len(tasks) == 1 else b"".join(tasks), stream.device_index, stream.cuda_stream)
 
@@ -88,6 +89,8 @@ def _keep(key, plan):
 def _run(plan, operands):
     """Launch with these addresses: the operands of all tasks, one after the other."""
     if plan.n:
+        for f in R.active_filters:                          # (tasks of the dispatch filter may still be working on these)
+            f.settle(operands)
         words = plan.words[:]
         for word, k in plan.at:
             words[word] = operands[k].data_ptr()
@@ -337,10 +340,16 @@ def _differentiable(xs, outs):
     return True
 
 
+def _no_gradient(what, *xs):
+    if torch.is_grad_enabled():
+        _need(not any(t is not None and t.requires_grad for t in xs), "%s has no gradient here", what)
+
+
 def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=False, out=None):
     """Root-mean-square norm of every head of x [T, H, D] or [B, S, H, D] over D, times gamma [D], and the rotation of its
     first R elements by the angles of table [places, R] (cosines | sines, float32) at the tokens' positions (None: 0, 1, ...
     in every sequence); pairs: neighbours are rotated together, else the halves.  Differentiable in x and gamma."""
+    _no_gradient("table", table)
     if _differentiable((x, gamma), (out,)):
         return _NormRope.apply(table, positions, eps, pairs, x, gamma)[0]
     return _norm_rope((x,), (gamma,), table, positions, eps, pairs, (out,))[0]
@@ -348,6 +357,7 @@ def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=Fals
 
 def norm_rope_qk(q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *, eps=1e-6, pairs=False, out=(None, None)):
     """norm_rope of queries and keys in one launch: (q', k')."""
+    _no_gradient("table", table)
     if _differentiable((q, k, gamma_q, gamma_k), out):
         return _NormRope.apply(table, positions, eps, pairs, q, gamma_q, k, gamma_k)
     return _norm_rope((q, k), (gamma_q, gamma_k), table, positions, eps, pairs, out)
@@ -418,7 +428,8 @@ def cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, length, 
 def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=None, allowed=None, out=None):
     """Penalties of the tokens in history [B, N] (entries that are no token count for nothing; the first prompt_lengths[b] for the
     repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
-    not set.  out may be x."""
+    not set.  out may be x.  Not differentiable: logits that require a gradient are refused where gradients are recorded."""
+    _no_gradient("penalize_logits", x, params, bias)
     key = ("penalty", _sig(x), _sig(history), _sig(prompt_lengths), _sig(params), _sig(bias), _sig(allowed), _sig(out))
     plan = _plans.get(key)
     if plan is None:

@@ -190,6 +190,9 @@ def _tasks_ptr(tasks, first=0):
 
 
 _live = weakref.WeakSet()
+# Dispatch filters (dispatch.GpuosMode) that are active: whoever launches kernels on tensors without PyTorch's dispatcher asks each
+# to settle() them first.
+active_filters = []
 
 
 class Runtime:

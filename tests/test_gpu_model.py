@@ -7,8 +7,6 @@ roundings on the longest way: the sum of squares has at most 8 terms in a lane a
 square root 4 (rsqrtf is good to one step, two half steps), so the root is off by 14 / 2 + 2 < 10; three products and the
 rotation's two roundings come on top: F = 16.  Backwards dx has the root three times (30), the second sum (8 + 6 + 2) and eight
 products: F = 56.  The gradient of gamma adds what its sums take: rows of a lane, 256 groups of lanes, and the parts' sum."""
-import threading
-
 import numpy as np
 import pytest
 import torch
@@ -508,77 +506,80 @@ def test_a_decode_step_by_tasks_that_wait_for_each_other():
     check(probs, torch.softmax(p.double(), -1), torch.softmax(p.double(), -1), 64)
 
 
-def test_a_decode_step_in_a_graph_replayed_on_new_values():
-    t, page, length = decode_step()
-    g = {k: v.cuda() for k, v in t.items()}
-    values, scales, kc, ks = cache_of(9, page, 4, 64, 1, torch.float8_e4m3fn, "plain")
-    _, _, vc, vs = cache_of(9, page, 4, 64, 1, torch.float8_e4m3fn, "plain")
-
-    def step():
-        q, k = M.norm_rope_qk(g["q"], g["k"], g["g"], g["g"], g["table"], g["positions"])
-        M.cache_store_kv(k, g["v"], g["slots"], kc, ks, vc, vs)
-        kb, vb = M.cache_load_kv(kc, ks, vc, vs, g["pages"], g["lengths"], length, dtype=BF16)
-        return q, kb, vb, M.penalize_logits(g["logits"], history=g["history"], params=g["params"])
-
-    step()
+def test_kernels_and_the_dispatch_filter_wait_for_each_other():
+    """Redirected operations feed an operator, its result feeds redirected operations, over and over."""
+    from paper_2604_17861_amd.dispatch import GpuosMode
+    gen = torch.Generator().manual_seed(12)
+    a, b = normal(gen, 40, 4, 64).cuda(), normal(gen, 40, 4, 64).cuda()
+    g = normal(gen, 64, shift=1.0).cuda()
+    want = a
+    for _ in range(6):
+        want = torch.relu(M.norm_rope(torch.relu(want + b) * 0.5, g) + b)
     torch.cuda.synchronize()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        captured = step()
-    for k in range(4):
-        for name in ("q", "k", "v", "logits"):
-            g[name].copy_(normal(torch.Generator().manual_seed(50 + k), *g[name].shape, dtype=g[name].dtype).cuda())
-        graph.replay()
-        torch.cuda.synchronize()
-        got = [c.clone() for c in captured]
-        for a, b in zip(got, step()):
-            assert torch.equal(a, b)
-        z, size = ref.norm_rope(g["q"].cpu(), t["g"], t["table"], t["positions"], 1e-6, False)
-        check(got[0], z, size, 16)
+    mode = GpuosMode(idle_exit_ms=50)
+    try:
+        for _ in range(3):
+            with mode:
+                x = a
+                for _ in range(6):
+                    x = torch.relu(M.norm_rope(torch.relu(x + b) * 0.5, g) + b)
+            assert torch.equal(x.cpu(), want.cpu())
+        assert mode.stats["redirected"] >= 3 * 6 * 5 and not R.active_filters
+    finally:
+        mode.close()
 
 
-def test_a_captured_training_step_beside_an_eager_one_of_the_same_values():
-    gen, x, g, table, p = rope_inputs((33, 4, 64), 64, BF16, F32, "each", 4)
-    leaves = [x.cuda().requires_grad_(), g.cuda().requires_grad_()]
-    table, p = table.cuda(), p.cuda()
-    dz = normal(gen, 33, 4, 64, dtype=BF16).cuda()
-    eager = M.norm_rope(*leaves, table, p)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        inner = [t.detach().requires_grad_() for t in leaves]      # (leaves of its own: a graph's gradients are its own)
-        torch.autograd.grad(M.norm_rope(*inner, table, p), inner, dz)
-    torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        captured = torch.autograd.grad(M.norm_rope(*inner, table, p), inner, dz)
-    want = torch.autograd.grad(eager, leaves, dz)
-    for _ in range(3):
-        graph.replay()
-        torch.cuda.synchronize()
-        for a, b in zip(captured, want):
-            assert torch.equal(a, b)
+def test_every_operand_with_strides_of_its_own():
+    gen = torch.Generator().manual_seed(13)
+    every = lambda t: up(torch.stack((t, t), -1).flatten(-2))[..., ::2]      # every second element of twice as many
+    b, s, h, d = 2, 5, 3, 32
+    x1 = normal(gen, 1, s, 1, d)
+    x = up(x1).expand(b, s, h, d)                            # one row for every sequence and head
+    g, angle = normal(gen, d, shift=1.0), torch.rand(20, d // 2, generator=gen)
+    table = torch.cat((angle.cos(), angle.sin()), 1)
+    p = torch.randint(0, 20, (b, s), generator=gen, dtype=torch.int32)
+    dz1 = normal(gen, b, s, h, 1)
+    wide = torch.zeros(20, d + 4, device="cuda")
+    wide[:, :d] = table.cuda()
+    full, dzf = x1.expand(b, s, h, d), dz1.expand(b, s, h, d)
+    got = M.norm_rope(x, every(g), wide[:, :d], every(p))
+    z, size = ref.norm_rope(full, g, table, p, 1e-6, False)
+    check(got, z, size, 16)
+    dx, dg = M.norm_rope_backward(up(dz1).expand(b, s, h, d), x, every(g), wide[:, :d], every(p))
+    w = ref.norm_rope_grad(dzf, full, g, table, p, 1e-6, False)
+    check(dx, w[0], w[1], 56)
+    check(dg, w[2], w[3], 56 + 256 + 30)
+    shared = torch.arange(s, dtype=torch.int32)              # the same positions for every sequence, and none given
+    for q in (every(shared), None):
+        z, size = ref.norm_rope(full, g, table, shared, 1e-6, False)
+        check(M.norm_rope(x, every(g), wide[:, :d], q), z, size, 16)
+    # the cache: slots, scales and lengths apart; pages of a table with gaps
+    values, scales, kc, ks = cache_of(4, 4, h, d, 2, torch.int8, "heads")
+    slots = torch.randperm(16, generator=gen)[:b * s].to(torch.int32).reshape(b, s)
+    M.cache_store(x, every(slots), kc, every(scales)[:])
+    want, _ = ref.store(full, slots, values, scales)
+    same(kc, want)
+    sc = every(scales)
+    pages = torch.tensor([[2, 0], [3, 1]], dtype=torch.int32)
+    lens = torch.tensor([7, 4], dtype=torch.int32)
+    same(M.cache_load(kc, sc, every(pages), every(lens), 8, dtype=F16), ref.load(want, scales, pages, lens, 8, F16))
+    logits, hist = normal(gen, 2, 90), torch.randint(0, 90, (2, 40), generator=gen, dtype=torch.int32)
+    params, prompts, bias = torch.rand(2, 3, generator=gen) + 0.5, torch.tensor([3, 9], dtype=torch.int32), normal(gen, 2, 90, dtype=F16)
+    bits = torch.randint(-2 ** 31, 2 ** 31, (2, 3), generator=gen).to(torch.int32)
+    got = M.penalize_logits(every(logits), history=every(hist), prompt_lengths=every(prompts), params=every(params), bias=every(bias), allowed=every(bits))
+    same(got, ref.penalties(logits, hist, prompts, params, bias, bits))
+    same(M.penalize_logits(up(logits), bias=up(bias[0]), allowed=up(bits[1])), ref.penalties(logits, bias=bias[0], allowed=bits[1]))
 
 
-def test_streams_threads_and_repetition_give_the_same():
-    gen, x, g, table, p = rope_inputs((300, 8, 128), 128, F16, F16, "each", 6)
-    x, g, table, p, dz = x.cuda(), g.cuda(), table.cuda(), p.cuda(), normal(gen, 300, 8, 128, dtype=F16).cuda()
-    want = M.norm_rope_backward(dz, x, g, table, p)
-    torch.cuda.synchronize()
-    bad = []
-
-    def work():
-        s = torch.cuda.Stream()
-        with torch.cuda.stream(s):
-            for _ in range(20):
-                got = M.norm_rope_backward(dz, x, g, table, p)
-                s.synchronize()
-                if not all(torch.equal(a, b) for a, b in zip(got, want)):
-                    bad.append(1)
-    threads = [threading.Thread(target=work) for _ in range(3)]
-    [t.start() for t in threads]
-    [t.join() for t in threads]
-    assert not bad
+def test_what_has_no_gradient_is_refused():
+    x = torch.randn(2, 10, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError):
+        M.penalize_logits(x)
+    with torch.no_grad():
+        assert torch.equal(M.penalize_logits(x), x)
+    t = torch.randn(4, 8, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError):
+        M.norm_rope(torch.randn(3, 2, 8, device="cuda"), None, t)
 
 
 def test_many_tasks_of_several_operators_in_one_call():
