@@ -255,8 +255,8 @@ typedef struct gpuos_task {
  *   fp32: rows with elements of over 1e18 leave its range.)
  * NORM_ROPE_GRAD  size = {B, S, H, D, R, places, parts}; operands 0-3 as above,
  *   4 dx [B,S,H,D]  5 dout [B,S,H,D]  6 partial [D, parts], F32, dense, or none
- *   The gradient of x, and in column c of `partial` what the c-th of `parts`
- *   shares of the B*S*H heads (in their order) adds to the gradient of gamma (1 <= parts <= 1024; every column is
+ *   The gradient of x, and in each column of `partial` what one of `parts` shares of
+ *   the B*S*H heads adds to the gradient of gamma (1 <= parts <= 1024; every column is
  *   written).  No sum depends on the order in which anything runs.
  * GAMMA_SUM  size = {D, parts}: 0 partial [D, parts], F32, dense  1 out [D], any float dtype
  *   Their sum (parts >= 0; no parts: zeros).
@@ -537,7 +537,7 @@ int gpuos_submit_model(gpuos_ctx* ctx, const gpuos_model_task* tasks, uint32_t n
 int gpuos_launch_model(int32_t device, const gpuos_model_task* tasks, uint32_t n, const uint32_t* impl_of_op, void* stream);
 
 /* How such a task is run (no GPU needed), out[0..3] as a task of the ring, out[4..7] as a kernel: 1 for
- * rows in vectors, 0 element by element, 2 nothing to do; work units; items in a unit; what an item
+ * rows in vectors, 0 element by element, 2 nothing to do; work units; items in a unit at most; what an item
  * is: that many heads of a token at most (LOGIT_PENALTY: elements of a row; GAMMA_SUM: 1, a row). */
 int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t out[8]);
 

@@ -40,7 +40,7 @@ struct ModelHead {
   uint32_t impl, version;
   int32_t  status;
   uint32_t nchunks;
-  uint32_t chunk;                  // items (blocks of heads, segments of rows) in a chunk
+  uint32_t chunk;                  // items (blocks of heads, segments of rows) in a chunk, at most
   uint32_t items;                  // ... and in all
   uint32_t d;                      // elements of a row
   float    alpha;
@@ -53,7 +53,7 @@ static_assert(sizeof(ModelHead) == 64 && offsetof(ModelHead, rflags) == offsetof
               offsetof(ModelHead, chunk) == offsetof(Record, chunk) && offsetof(ModelHead, items) == offsetof(Record, numel) &&
               offsetof(ModelHead, dep) == offsetof(Record, dep) && offsetof(ModelHead, run) == offsetof(Record, run) &&
               offsetof(ModelHead, ticket) == offsetof(Record, ticket) && offsetof(ModelHead, path) == offsetof(Record, path), "the words the dispatcher and the worker read");
-enum ModelFlag : uint8_t { MF_PAIRS = 1 };
+enum ModelFlag : uint8_t { MF_PAIRS = 1, MF_LINES = 2 };      // neighbours are pairs; what a store of a wavefront writes of an output row is whole blocks of 64 bytes
 
 struct alignas(16) RopeRecord {    // NORM_ROPE, NORM_ROPE_GRAD, GAMMA_SUM
   ModelHead h;                     // dtype: x, out, gamma, dout
@@ -113,10 +113,11 @@ constexpr uint32_t kModelRow = 512;          // elements of a head, at most: 64 
 constexpr uint32_t kModelParts = 1024;       // shares of the gradient of gamma, at most (a unit names its chunk in ten bits)
 // Lanes that a row of vectors takes: a lane has four pairs, or eight elements that are not rotated (neighbours: eight elements).
 GPUOS_HD inline uint32_t rope_units(uint32_t d, uint32_t half, bool pairs) { return pairs ? (d + 7u) / 8u : (half + 3u) / 4u + (d - 2u * half + 7u) / 8u; }
-// Heads of an item that goes in vectors.  The worker has twelve wavefronts on a compute unit where a kernel has up to thirty-two, so
-// its have more on their way each.
-GPUOS_HD constexpr uint32_t rope_block(bool ring, bool grad) { return (grad ? 2u : 4u) * (ring ? 2u : 1u); }
-GPUOS_HD constexpr uint32_t cache_block(bool ring) { return ring ? 8u : 4u; }
+// Heads of an item that goes in vectors.  More of them share a token's position, slot and page and have more on their way at once, but the
+// code grows with them and a short call waits for it: 2, 4 and 8 heads (the gradient: 1, 2 and 4) take, for 16 heads of one token
+// and for 327,680 of 128 bf16, norm and rotation 3.6, 4.3, 6.0 and 38.3, 36.9, 35.0 us, the gradient (262,144 heads) 4.2, 4.8, 6.0 and 56.1, 50.3, 49.2;
+// storing 2.4, 3.0, 4.7 and 19.2, 19.8, 22.7 (262,144 heads), reading back 2.2, 2.5, 3.1 and 179, 159, 157 (2,097,152 heads).
+constexpr uint32_t kRopeBlock = 4, kGradBlock = 2, kStoreBlock = 2, kLoadBlock = 4;
 constexpr uint32_t kModelLaunch = 8;         // tasks of one launch: their records are kernel arguments, 2 KB of the 4 KB there may be
 
 // What gpuos_launch_model hands a kernel: tasks of one variant.  (A block's second index is its task's place here: its
@@ -149,9 +150,12 @@ GPUOS_HD inline uint32_t model_variant(uint32_t impl, uint32_t vec, uint32_t dty
 
 // How a task is cut: chunks of at least so many bytes, at most so many; and whether vectors have to be aligned (the worker's accesses of
 // 8 bytes go by atomic loads and stores, a kernel's by ordinary ones, which gfx950 takes at any address of an element).
+// Of the passes that a workgroup makes over all items, chunk c makes every nchunks-th from the c-th on, so that what is worked on at a
+// time lies together in memory: 2,097,152 heads read back in 2,048 chunks of passes that follow each other took 159 us, in 4,096 148, in
+// 16,384, a pass each, 124.
 struct ModelCut { uint32_t least_bytes, most; bool aligned; };
 constexpr ModelCut kRingCut{16384, kMaxChunksPerTask, true};       // a unit costs the dispatcher 12 ns and the worker about a microsecond
-constexpr ModelCut kLaunchCut{4096, 2048, false};                  // a block is cheaper; 2,048 are eight per compute unit, as many as are resident
+constexpr ModelCut kLaunchCut{4096, 65536, false};
 
 // Checks and packs one descriptor.
 class ModelPack {
@@ -232,15 +236,24 @@ class ModelPack {
     r.by_blocks = make_div(r.blocks);
     r.h.items = (uint32_t)(tokens * r.blocks);
   }
-  // Items in chunks: by bytes moved, in whole passes of a workgroup, as many chunks as may be.
+  // whether the rows of an output begin on blocks of 64 bytes, and parts of so many elements are whole blocks
+  static bool lines(uint64_t ptr, uint32_t es, const uint32_t* st, int outer, uint32_t part) {
+    bool ok = ptr % 64 == 0 && (uint64_t)part * es % 64 == 0;
+    for (int d = 0; d < outer; ++d) ok = ok && (uint64_t)st[d] * es % 64 == 0;
+    return ok;
+  }
+  // Items in chunks, `pass` of them at a time.
   static void cut_items(ModelHead& h, ModelCut cut, uint64_t item_bytes, uint32_t pass) {
-    uint64_t per = (cut.least_bytes + item_bytes - 1) / item_bytes;
-    const uint64_t even = ((uint64_t)h.items + cut.most - 1) / cut.most;
+    const uint64_t passes = ((uint64_t)h.items + pass - 1) / pass, pass_bytes = item_bytes * pass;
+    uint64_t per = (cut.least_bytes + pass_bytes - 1) / pass_bytes;
+    const uint64_t even = (passes + cut.most - 1) / cut.most;
     if (per < even) per = even;
-    per = (per + pass - 1) / pass * pass;
-    if (per > 0x7fffffffull) per = 0x7fffffffull;
-    h.chunk = (uint32_t)per;
-    h.nchunks = h.items == 0 ? 1u : (uint32_t)((h.items + per - 1) / per);
+    h.nchunks = passes == 0 ? 1u : (uint32_t)((passes + per - 1) / per);
+    set_most(h, passes, pass);
+  }
+  static void set_most(ModelHead& h, uint64_t passes, uint32_t pass) {
+    const uint64_t most = (passes + h.nchunks - 1) / h.nchunks * pass;
+    h.chunk = most < h.items ? (uint32_t)most : h.items;
   }
   // rows that the workgroup's 256 lanes take at once, `lanes` of them each
   static uint32_t rows_at_once(uint32_t lanes) {
@@ -300,8 +313,11 @@ class ModelPack {
         (!cut.aligned || (d % 8 == 0 && r.half % 4 == 0)) && vectors(cut, r.x, es, r.xs, 3, last) && vectors(cut, r.out, es, r.os, 3, last) &&
         vectors(cut, r.dout, es, r.zs, 3, last) && vectors(cut, r.table, 4, &r.ts, 1, true))
       r.h.vec = 1;
-    in_blocks(r, (uint64_t)tokens, r.h.vec ? rope_block(cut.aligned, grad) : 1);
-    cut_items(r.h, cut, (uint64_t)d * es * (grad ? 3 : 2) * r.h.block, rows_at_once(r.h.vec ? rope_units((uint32_t)d, r.half, pairs) : (uint32_t)(d + 1) / 2));
+    // (halves: a wavefront stores either by itself, and of what is not rotated every second four)
+    if (lines(r.out, es, r.os, 3, (uint32_t)d) && (pairs || (rest == 0 && (uint64_t)r.half * es % 64 == 0))) r.h.flags |= MF_LINES;
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? (grad ? kGradBlock : kRopeBlock) : 1);
+    const uint32_t pass = rows_at_once(r.h.vec ? rope_units((uint32_t)d, r.half, pairs) : (uint32_t)(d + 1) / 2);
+    cut_items(r.h, cut, (uint64_t)d * es * (grad ? 3 : 2) * r.h.block, pass);
     if (grad && part->ptr) {
       const int64_t parts = z[6], cz[2] = {d, parts};
       uint32_t cs[2];
@@ -310,7 +326,7 @@ class ModelPack {
       r.partial = (uint64_t)part->ptr;
       r.cs = cs[0];
       r.h.nchunks = (uint32_t)parts;                 // every column is written, also of shares with no rows
-      r.h.chunk = (uint32_t)((r.h.items + parts - 1) / parts);
+      set_most(r.h, ((uint64_t)r.h.items + pass - 1) / pass, pass);
       if (r.h.items == 0) {                           // (not an empty task: see pack)
         r.h.vec = 0;
         r.h.items = kNoRows;
@@ -373,7 +389,8 @@ class ModelPack {
     // Vectors: a lane takes eight elements of a row, 8 bytes of the cache.  (A row that is no whole number of eights is one group.)
     const uint32_t es = size_of(x.dtype);
     if (d >= 8 && (!cut.aligned || d % 8 == 0) && vectors(cut, r.x, es, r.xs, 3, r.xs[3] == 1) && vectors(cut, r.cache, 1, r.cs, 3, true)) r.h.vec = 1;
-    in_blocks(r, (uint64_t)tokens, r.h.vec ? cache_block(cut.aligned) : 1);
+    if (!store && lines(r.x, es, r.xs, 3, (uint32_t)d)) r.h.flags |= MF_LINES;
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? (store ? kStoreBlock : kLoadBlock) : 1);
     cut_items(r.h, cut, (uint64_t)d * (es + 1) * r.h.block, rows_at_once(r.h.vec ? (uint32_t)(d + 7) / 8 : (uint32_t)d));
     return GPUOS_OK;
   }
@@ -409,6 +426,7 @@ class ModelPack {
     if (x.dtype == out.dtype && vectors(cut, r.x, es, r.xs, 1, v == 1 || r.xs[1] == 1) && vectors(cut, r.out, es, r.os, 1, v == 1 || r.os[1] == 1) &&
         bias_ok && allowed_ok)
       r.h.vec = 1;
+    if (lines(r.out, es, r.os, 1, 64)) r.h.flags |= MF_LINES;
     cut_items(r.h, ModelCut{1, cut.most, cut.aligned}, 1, 1);
     return GPUOS_OK;
   }

@@ -11,6 +11,13 @@ namespace gpuos {
 // memory access by 64-bit address: rows of a chunk lie at any distance from each other, so there is no buffer resource to go by.
 // POL_PLAIN: ordinary accesses, vectors at any address of an element.  POL_COHERENT: atomic ones of 8 bytes and less at the system's
 // scope, which go past the caches that another die's writes do not reach; vectors begin on 8 bytes (ModelCut::aligned).
+//
+// A kernel's vector stores have the non-temporal hint, as those of row operations have it, where each writes whole pieces of 64 bytes
+// (MF_LINES): what an operator writes is a matrix product away from its reader, and the inputs stay in the memory-side cache.  Without
+// and with it, three sets of buffers in turn: norm and rotation of 84 MB 41.4 and 30.9 us, a sequence of 134 MB read back 41.9 and 25.9,
+// penalties on 51 MB 35.6 and 30.1; with an addition that reads the result right behind it 69.4 and 66.2, 91.3 and 86.8, 50.5 and 51.7 (of 42, 34
+// and 168 MB 5 and 8 % behind, and 3).  Pieces of such a block that two stores write each go to memory by themselves: 134 MB of fp32, whose eight
+// elements are two stores, read back in 27.6 and 54, rows of 100 bf16 in 14.2 and 19.3.
 // ---------------------------------------------------------------------------
 typedef int v2i __attribute__((ext_vector_type(2)));
 template <int POL> struct Glob {
@@ -37,12 +44,14 @@ template <int POL> struct Glob {
     }
     return *(const G<v4i_any>*)p;
   }
-  static DEV void st8(uint64_t p, v2i q) {
+  static DEV void st8(uint64_t p, v2i q, bool nt = false) {
     if (POL == POL_COHERENT) put<uint64_t>(p, __builtin_bit_cast(uint64_t, q));
+    else if (nt) __builtin_nontemporal_store((v2i_any)q, (G<v2i_any>*)p);
     else *(G<v2i_any>*)p = q;
   }
-  static DEV void st16(uint64_t p, v4i q) {
+  static DEV void st16(uint64_t p, v4i q, bool nt = false) {
     if (POL == POL_COHERENT) { st8(p, v2i{q[0], q[1]}); st8(p + 8, v2i{q[2], q[3]}); }
+    else if (nt) __builtin_nontemporal_store((v4i_any)q, (G<v4i_any>*)p);
     else *(G<v4i_any>*)p = q;
   }
   static DEV v2i ld8b(uint64_t p) { return POL == POL_COHERENT ? ld8(p) : (v2i)*(const G<v2i_byte>*)p; }      // bytes
@@ -116,13 +125,14 @@ template <int POL, int DT> struct Eight {
     if (N == 2) { q[0] = Glob<POL>::ld16(p); q[N - 1] = Glob<POL>::ld16(p2); }
     else { const v2i a = Glob<POL>::ld8(p), b = Glob<POL>::ld8(p2); q[0] = v4i{a[0], a[1], b[0], b[1]}; }
   }
-  DEV void store(uint64_t p) const {
+  // lines: see MF_LINES
+  DEV void store(uint64_t p, bool lines) const {
 #pragma unroll
-    for (int k = 0; k < N; ++k) Glob<POL>::st16(p + 16 * k, q[k]);
+    for (int k = 0; k < N; ++k) Glob<POL>::st16(p + 16 * k, q[k], N == 1 && lines);
   }
-  DEV void store(uint64_t p, uint64_t p2) const {
-    if (N == 2) { Glob<POL>::st16(p, q[0]); Glob<POL>::st16(p2, q[N - 1]); }
-    else { Glob<POL>::st8(p, v2i{q[0][0], q[0][1]}); Glob<POL>::st8(p2, v2i{q[0][2], q[0][3]}); }
+  DEV void store(uint64_t p, uint64_t p2, bool lines) const {
+    if (N == 2) { Glob<POL>::st16(p, q[0], lines); Glob<POL>::st16(p2, q[N - 1], lines); }
+    else { Glob<POL>::st8(p, v2i{q[0][0], q[0][1]}, lines); Glob<POL>::st8(p2, v2i{q[0][2], q[0][3]}, lines); }
   }
 };
 
@@ -150,9 +160,9 @@ DEV uint64_t offset(const Place& p, const uint32_t (&st)[4]) { return (uint64_t)
 // ---------------------------------------------------------------------------
 struct RopeArgs {
   uint64_t x, gamma, table, positions, out, dout, partial;
-  uint32_t xs[4], os[4], zs[4], gs, ts, ps[2], cs, half, places, seq, heads, block, blocks, d, chunk, items, dtype[4];
+  uint32_t xs[4], os[4], zs[4], gs, ts, ps[2], cs, half, places, seq, heads, block, blocks, d, chunks, items, dtype[4];
   Div by_seq, by_blocks;
-  bool pairs;
+  bool pairs, lines;
   float eps;
 };
 template <class P> DEV RopeArgs rope_args(P p) {
@@ -164,9 +174,10 @@ template <class P> DEV RopeArgs rope_args(P p) {
   a.gs = uni(p->gs); a.ts = uni(p->ts); a.ps[0] = uni(p->ps[0]); a.ps[1] = uni(p->ps[1]); a.cs = uni(p->cs);
   a.half = uni(p->half); a.places = uni(p->places); a.seq = uni(p->seq); a.heads = uni(p->heads);
   a.block = uni((uint32_t)p->h.block); a.blocks = uni(p->blocks);
-  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
+  a.d = uni(p->h.d); a.chunks = uni(p->h.nchunks); a.items = uni(p->h.items);
   a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_blocks = uni_div(p->by_blocks.mul, p->by_blocks.shift);
   a.pairs = (uni((uint32_t)p->h.flags) & MF_PAIRS) != 0;
+  a.lines = (uni((uint32_t)p->h.flags) & MF_LINES) != 0;
   a.eps = __builtin_bit_cast(float, uni(__builtin_bit_cast(uint32_t, (float)p->h.alpha)));
   return a;
 }
@@ -193,14 +204,13 @@ DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid)
   typedef Glob<POL> M;
   typedef Eight<POL, DT> E;
   constexpr uint32_t ES = Elem<DT>::ES;
-  constexpr int U = rope_block(POL == POL_COHERENT, GRAD);
+  constexpr int U = GRAD ? kGradBlock : kRopeBlock;
   // A lane's eight elements are two windows of four, oa and ob on.  Halves: the same four of either half, or eight that follow
   // each other behind them; neighbours: eight that follow each other.  The last window of a part that is no whole number of them begins
   // early and ends with it: what it shares with the one before (below `from`) both compute and store, and only that one sums.
   const uint32_t units = rope_units(a.d, a.half, PAIRS), lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const bool active = u < units;
-  const uint32_t begin = chunk * a.chunk, end = a.items <= begin ? begin : (a.items - begin < a.chunk ? a.items : begin + a.chunk);
   const uint32_t turned_units = PAIRS ? 0u : (a.half + 3u) / 4u, rest = PAIRS ? 8u * u : 2u * a.half + 8u * (u - turned_units);
   const bool turned = u < turned_units;
   uint32_t from_a = turned ? 4u * u : rest, from_b = turned ? a.half + 4u * u : rest + 4u, oa, ob;
@@ -227,10 +237,10 @@ DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid)
     }
   }
   const float inv_d = 1.0f / (float)a.d;
-  for (uint32_t base = begin; base < end; base += step) {
+  for (uint32_t base = chunk * step; base < a.items; base += a.chunks * step) {
     const uint32_t item = base + group;
-    const Place p = place(a, item < end ? item : end - 1u);
-    const uint32_t heads = item < end && active ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
+    const Place p = place(a, item < a.items ? item : a.items - 1u);
+    const uint32_t heads = item < a.items && active ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
     const uint64_t xp = a.x + offset(p, a.xs) * ES, zp = a.dout + offset(p, a.zs) * ES, op = a.out + offset(p, a.os) * ES;
     E x[U], z[U];
 #pragma unroll
@@ -308,8 +318,8 @@ DEV void rope_vectors(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid)
       }
       if ((uint32_t)k < heads) {
         const uint64_t to = op + (uint64_t)k * a.os[2] * ES;
-        if (PAIRS) o.store(to + oa * ES);
-        else o.store(to + oa * ES, to + ob * ES);
+        if (PAIRS) o.store(to + oa * ES, a.lines);
+        else o.store(to + oa * ES, to + ob * ES, a.lines);
       }
     }
   }
@@ -335,8 +345,7 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
   const uint32_t rest = a.d - 2u * a.half, rest_pairs = (rest + 1u) / 2u, pairs = a.half + rest_pairs;
   const uint32_t lg = pairs > 64u ? 6u : ceil_log2(pairs), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
-  const uint32_t rows = a.items == ModelPack::kNoRows ? 0u : a.items;
-  const uint32_t begin = chunk * a.chunk, end = rows <= begin ? begin : (rows - begin < a.chunk ? rows : begin + a.chunk);
+  const uint32_t end = a.items == ModelPack::kNoRows ? 0u : a.items;
   const uint32_t es = float_size(a.dtype[0]), eo = float_size(a.dtype[1]), ez = float_size(a.dtype[3]);
   uint32_t ja[K], jb[K];
   bool in_a[K], in_b[K], turned[K];
@@ -356,7 +365,7 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
     if (a.gamma != 0 && in_b[k]) gb[k] = M::ld_rt(a.gamma + (uint64_t)jb[k] * a.gs * float_size(gdt), gdt);
   }
   const float inv_d = 1.0f / (float)a.d;
-  for (uint32_t base = begin; base < end; base += step) {
+  for (uint32_t base = chunk * step; base < end; base += a.chunks * step) {
     const bool in = base + group < end;
     const Place p = place(a, in ? base + group : end - 1u);
     const uint64_t xp = a.x + offset(p, a.xs) * es, op = a.out + offset(p, a.os) * eo, zp = a.dout + offset(p, a.zs) * ez;
@@ -429,8 +438,7 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
 // GAMMA_SUM: the workgroup a row of the partial sums (4 KB at most), always in the same order.
 template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
-  for (uint32_t row = begin; row < end; ++row) {
+  for (uint32_t row = chunk; row < a.items; row += a.chunks) {
     const uint64_t p = a.partial + (uint64_t)row * a.cs * 4u;
     float sum = 0.0f;
     for (uint32_t i = tid; i < a.d; i += 4u * kThreads) {
@@ -440,7 +448,7 @@ template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* 
       sum += (f[0] + f[1]) + (f[2] + f[3]);
     }
     sum = wave_reduce<GPUOS_IMPL_SUM_LAST>(sum, 64u);
-    if (row != begin) __syncthreads();
+    if (row != chunk) __syncthreads();
     if ((tid & 63u) == 0) s[tid >> 6] = sum;
     __syncthreads();
     if (tid == 0) M::st_rt(a.out + (uint64_t)row * a.os[0] * float_size(a.dtype[1]), a.dtype[1], (s[0] + s[1]) + (s[2] + s[3]));
@@ -456,8 +464,9 @@ template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* 
 // ---------------------------------------------------------------------------
 struct CacheArgs {
   uint64_t x, cache, scales, slots, lengths;
-  uint32_t xs[4], cs[3], ss[4], ps[2], ls, pages, page, group, heads, seq, block, blocks, d, chunk, items, dtype, format;
+  uint32_t xs[4], cs[3], ss[4], ps[2], ls, pages, page, group, heads, seq, block, blocks, d, chunks, items, dtype, format;
   Div by_blocks, by_seq, by_page, by_group;
+  bool lines;
 };
 template <class P> DEV CacheArgs cache_args(P p) {
   CacheArgs a;
@@ -469,8 +478,9 @@ template <class P> DEV CacheArgs cache_args(P p) {
   a.ps[0] = uni(p->ps[0]); a.ps[1] = uni(p->ps[1]); a.ls = uni(p->ls);
   a.pages = uni(p->pages); a.page = uni(p->page); a.group = uni(p->group); a.heads = uni(p->heads); a.seq = uni(p->seq);
   a.block = uni((uint32_t)p->h.block); a.blocks = uni(p->blocks);
-  a.d = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
+  a.d = uni(p->h.d); a.chunks = uni(p->h.nchunks); a.items = uni(p->h.items);
   a.dtype = uni((uint32_t)p->h.dtype[0]); a.format = uni((uint32_t)p->h.dtype[1]);
+  a.lines = (uni((uint32_t)p->h.flags) & MF_LINES) != 0;
   a.by_blocks = uni_div(p->by_blocks.mul, p->by_blocks.shift); a.by_seq = uni_div(p->by_seq.mul, p->by_seq.shift); a.by_page = uni_div(p->by_page.mul, p->by_page.shift); a.by_group = uni_div(p->by_group.mul, p->by_group.shift);
   return a;
 }
@@ -513,16 +523,15 @@ DEV uint64_t scale_at(const CacheArgs& a, uint32_t page, uint32_t in, uint32_t h
 template <int POL, int DT> DEV void store_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
   typedef Eight<POL, DT> E;
-  constexpr int U = cache_block(POL == POL_COHERENT);
+  constexpr int U = kStoreBlock;
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;      // (the last window ends with the row: what two have both write alike)
   const uint32_t lg_width = a.group == a.d ? lg : ceil_log2(a.group) - 3u, width = 1u << lg_width;
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
-  for (uint32_t base = begin; base < end; base += step) {
+  for (uint32_t base = chunk * step; base < a.items; base += a.chunks * step) {
     const uint32_t item = base + group;
-    const Place p = place(a, item < end ? item : end - 1u);
-    const uint32_t heads = item < end && u < units ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
+    const Place p = place(a, item < a.items ? item : a.items - 1u);
+    const uint32_t heads = item < a.items && u < units ? (a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U) : 0u;
     const uint64_t xp = a.x + (offset(p, a.xs) + at) * Elem<DT>::ES;
     const uint32_t slot = (uint32_t)M::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)p.s * a.ps[1]) * 4u);
     E x[U];
@@ -559,13 +568,12 @@ template <int POL> DEV void store_elements(const CacheArgs& a, uint32_t chunk, u
   constexpr int K = 8;
   const uint32_t lg = a.d > 64u ? 6u : ceil_log2(a.d), lanes = 1u << lg, u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t es = float_size(a.dtype);
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
   // A group is the row, or a power of two: then `width` lanes of a register hold it, or `span` registers of all lanes.
   const bool whole = a.group == a.d;
   const uint32_t width = whole || a.group >= lanes ? lanes : a.group, span = whole ? (uint32_t)K : (a.group > lanes ? a.group >> lg : 1u);
-  for (uint32_t base = begin; base < end; base += step) {
-    const bool in_row = base + group < end;
-    const Place p = place(a, in_row ? base + group : end - 1u);
+  for (uint32_t base = chunk * step; base < a.items; base += a.chunks * step) {
+    const bool in_row = base + group < a.items;
+    const Place p = place(a, in_row ? base + group : a.items - 1u);
     int32_t slot = M::ldi(a.slots + ((uint64_t)p.b * a.ps[0] + (uint64_t)p.s * a.ps[1]) * 4u);
     if (!in_row || (uint32_t)slot >= a.pages * a.page) slot = -1;
     const uint64_t xp = a.x + offset(p, a.xs) * es;
@@ -617,14 +625,13 @@ template <int POL> DEV uint32_t sequence_row(const CacheArgs& a, const Place& p,
 }
 template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
-  constexpr int U = cache_block(POL == POL_COHERENT);
+  constexpr int U = kLoadBlock;
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;
   const uint32_t lg_width = a.group == a.d ? lg : ceil_log2(a.group) - 3u;
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
   if (u >= units) return;
-  for (uint32_t item = begin + group; item < end; item += step) {
+  for (uint32_t item = chunk * step + group; item < a.items; item += a.chunks * step) {
     const Place p = place(a, item);
     const uint32_t heads = a.heads - p.h < (uint32_t)U ? a.heads - p.h : (uint32_t)U;
     const uint64_t to = a.x + (offset(p, a.xs) + at) * Elem<DT>::ES;
@@ -652,7 +659,7 @@ template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t ch
         o.clear();
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.put(i, y[i] * scale[k]);
-        o.store(to + (uint64_t)k * a.xs[2] * Elem<DT>::ES);
+        o.store(to + (uint64_t)k * a.xs[2] * Elem<DT>::ES, a.lines);
       }
     }
   }
@@ -662,8 +669,7 @@ template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, ui
   constexpr int K = 8;
   const uint32_t lg = a.d > 64u ? 6u : ceil_log2(a.d), lanes = 1u << lg, u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t es = float_size(a.dtype);
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
-  for (uint32_t row = begin + group; row < end; row += step) {
+  for (uint32_t row = chunk * step + group; row < a.items; row += a.chunks * step) {
     const Place p = place(a, row);
     uint32_t page, in;
     const uint32_t what = sequence_row<POL>(a, p, page, in);
@@ -700,8 +706,9 @@ template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, ui
 // ---------------------------------------------------------------------------
 struct PenaltyArgs {
   uint64_t x, out, history, prompts, params, bias, allowed;
-  uint32_t xs[2], os[2], hs[2], ps, ms[2], bs[2], as[2], n, seg, segs, v, chunk, items, dtype[3];
+  uint32_t xs[2], os[2], hs[2], ps, ms[2], bs[2], as[2], n, seg, segs, v, chunks, items, dtype[3];
   Div by_segs;
+  bool lines;
 };
 template <class P> DEV PenaltyArgs penalty_args(P p) {
   PenaltyArgs a;
@@ -711,10 +718,11 @@ template <class P> DEV PenaltyArgs penalty_args(P p) {
   for (int k = 0; k < 2; ++k) {
     a.xs[k] = uni(p->xs[k]); a.os[k] = uni(p->os[k]); a.hs[k] = uni(p->hs[k]); a.ms[k] = uni(p->ms[k]); a.bs[k] = uni(p->bs[k]); a.as[k] = uni(p->as[k]);
   }
-  a.ps = uni(p->ps); a.n = uni(p->n); a.seg = uni(p->seg); a.segs = uni(p->segs); a.v = uni(p->h.d); a.chunk = uni(p->h.chunk); a.items = uni(p->h.items);
+  a.ps = uni(p->ps); a.n = uni(p->n); a.seg = uni(p->seg); a.segs = uni(p->segs); a.v = uni(p->h.d); a.chunks = uni(p->h.nchunks); a.items = uni(p->h.items);
 #pragma unroll
   for (int k = 0; k < 3; ++k) a.dtype[k] = uni((uint32_t)p->h.dtype[k]);
   a.by_segs = uni_div(p->by_segs.mul, p->by_segs.shift);
+  a.lines = (uni((uint32_t)p->h.flags) & MF_LINES) != 0;
   return a;
 }
 struct Penalty { float rep, freq, pres; };
@@ -787,10 +795,9 @@ template <int POL> DEV void put_logit(const PenaltyArgs& a, uint32_t row, uint32
 template <int POL, int DT, uint32_t T> DEV void penalty_segments(const PenaltyArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
   uint32_t* seen = (uint32_t*)s;
-  const uint32_t begin = chunk * a.chunk, end = a.items - begin < a.chunk ? a.items : begin + a.chunk;
-  for (uint32_t item = begin; item < end; ++item) {
+  for (uint32_t item = chunk; item < a.items; item += a.chunks) {
     const uint32_t row = divided(item, a.by_segs), v0 = (item - row * a.segs) * a.seg, nv = a.v - v0 < a.seg ? a.v - v0 : a.seg;
-    if (a.history != 0 && item != begin) __syncthreads();        // (the counts of the segment before have been read)
+    if (a.history != 0 && item != chunk) __syncthreads();        // (the counts of the segment before have been read)
     Penalty pen = {1.0f, 0.0f, 0.0f};
     if (a.history != 0) {
       const uint64_t p = a.params + (uint64_t)row * a.ms[0] * 4u;
@@ -860,7 +867,7 @@ template <int POL, int DT, uint32_t T> DEV void penalty_segments(const PenaltyAr
           if (a.bias != 0) y[i] += b[i];
           o.put(i, (bits[k] >> i) & 1u ? y[i] : -__builtin_inff());
         }
-        o.store(op + j * ES);
+        o.store(op + j * ES, a.lines);
       }
       if (tid < nv - whole) put_logit<POL>(a, row, v0 + whole + tid, penalized<POL>(a, row, v0 + whole + tid, a.history != 0 ? seen[whole + tid] : 0u, pen));
     }
