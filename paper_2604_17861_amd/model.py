@@ -18,6 +18,8 @@ from array import array
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
+from torch.utils._python_dispatch import _get_current_dispatch_mode_stack
 
 from . import runtime as R
 from . import streams as S
@@ -68,6 +70,7 @@ class _Plan:
         tasks = [t for x, t in zip(rows, tasks) if x.numel() != 0]
         self.words = array("Q", b"".join(tasks))
         self.n, self.device = len(tasks), rows[0].get_device()
+        _need(all(x.get_device() == self.device for x in rows), "the tensors of one call are on one device")
         self.at = []                                        # (word, which of all the operands)
         first, place = 0, 0
         for x, mine in zip(rows, operands):
@@ -89,8 +92,10 @@ def _keep(key, plan):
 def _run(plan, operands):
     """Launch with these addresses: the operands of all tasks, one after the other."""
     if plan.n:
-        for f in R.active_filters:                          # (tasks of the dispatch filter may still be working on these)
-            f.settle(operands)
+        if R.active_filters:                                # (tasks of this thread's dispatch filter may still be working on these)
+            for f in _get_current_dispatch_mode_stack():
+                if f in R.active_filters:
+                    f.settle(operands)
         words = plan.words[:]
         for word, k in plan.at:
             words[word] = operands[k].data_ptr()
@@ -119,7 +124,7 @@ def _rows(t):
     return (1, *sh), (t.data_ptr(), 0, *st, _DT[t.dtype])
 
 
-def _tokens(t, four):
+def _tokens(t):
     """A number for each token, [B, S] like the rows it belongs to."""
     st = t.stride()
     if len(st) == 1:                                        # (one sequence; or the same numbers for every one)
@@ -176,7 +181,7 @@ def _check_rope(x, gamma, table, positions, out):
 def _rope_operands(x, gamma, table, positions, out):
     sizes, xo = _rows(x)
     rot, places = (table.shape[1], table.shape[0]) if table is not None else (0, 0)
-    return ((*sizes, rot, places), (xo, _operand(gamma), _operand(table), _NONE if positions is None else _tokens(positions, len(x.shape) == 4),
+    return ((*sizes, rot, places), (xo, _operand(gamma), _operand(table), _NONE if positions is None else _tokens(positions),
                                     _rows(out)[1]))
 
 
@@ -222,7 +227,7 @@ def cache_store_task(x, slots, cache, scales, *, deps=(), fence=False):
     _check(slots, "slots", _INT, None, x.shape[:-2], x.device)
     sizes, xo = _rows(x)
     return _pack("CACHE_STORE", int(fence), (*sizes, cache.shape[0], cache.shape[1], scales.shape[3]),
-                 (xo, _tokens(slots, False), _operand(cache), _operand(scales)), 0.0, deps)
+                 (xo, _tokens(slots), _operand(cache), _operand(scales)), 0.0, deps)
 
 
 def cache_load_task(cache, scales, pages, lengths, out, *, deps=(), fence=False):
@@ -276,6 +281,15 @@ def _parts(x):
     return min(PARTS_MAX, max(1, rows // 32))
 
 
+def _written(outs):
+    """Outputs of the caller's: what autograd has saved of them is no longer what it was."""
+    for o in outs:
+        if isinstance(o, torch.Tensor):
+            _no_gradient("out", o)
+            if not o.is_inference():
+                increment_version(o)
+
+
 def _empty_like(x):
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
@@ -298,6 +312,7 @@ class _NormRope(torch.autograd.Function):
 
 
 def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
+    eps, pairs = float(eps), bool(pairs)                    # (a key holds values, not objects)
     key = ("norm_rope", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in outs])
     plan = _plans.get(key)
     outs = [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
@@ -309,6 +324,7 @@ def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
 
 
 def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
+    eps, pairs = float(eps), bool(pairs)
     key = ("backward", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in douts])
     plans = _plans.get(key)
     dxs, dgs, grads, sums = [], [], [], []
@@ -352,6 +368,7 @@ def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=Fals
     _no_gradient("table", table)
     if _differentiable((x, gamma), (out,)):
         return _NormRope.apply(table, positions, eps, pairs, x, gamma)[0]
+    _written((out,))
     return _norm_rope((x,), (gamma,), table, positions, eps, pairs, (out,))[0]
 
 
@@ -360,6 +377,7 @@ def norm_rope_qk(q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *
     _no_gradient("table", table)
     if _differentiable((q, k, gamma_q, gamma_k), out):
         return _NormRope.apply(table, positions, eps, pairs, q, gamma_q, k, gamma_k)
+    _written(out)
     return _norm_rope((q, k), (gamma_q, gamma_k), table, positions, eps, pairs, out)
 
 
@@ -398,6 +416,8 @@ def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
 
 
 def _load(caches, scales, pages, lengths, length, dtype, outs):
+    length = int(length)
+    _written(outs)
     key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
     plan = _plans.get(key)
     if plan is None:
@@ -430,6 +450,7 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
     repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
     not set.  out may be x.  Not differentiable: logits that require a gradient are refused where gradients are recorded."""
     _no_gradient("penalize_logits", x, params, bias)
+    _written((out,))
     key = ("penalty", _sig(x), _sig(history), _sig(prompt_lengths), _sig(params), _sig(bias), _sig(allowed), _sig(out))
     plan = _plans.get(key)
     if plan is None:

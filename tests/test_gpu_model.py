@@ -529,6 +529,66 @@ def test_kernels_and_the_dispatch_filter_wait_for_each_other():
         mode.close()
 
 
+def test_only_the_filter_of_the_calling_thread_is_waited_for(monkeypatch):
+    """A filter belongs to its thread: its tables are not to be walked from another.  A backward pass runs on a thread of autograd's with the
+    modes of the one that called it."""
+    import threading
+    from paper_2604_17861_amd.dispatch import GpuosMode
+    x = torch.randn(40, 4, 64, device="cuda")
+    leaf = x.clone().requires_grad_()
+    torch.cuda.synchronize()
+    mode = GpuosMode(idle_exit_ms=50)
+    calls = []
+    settle = mode.settle
+    monkeypatch.setattr(mode, "settle", lambda ts: (calls.append(threading.get_ident()), settle(ts)))
+    try:
+        with mode:
+            other = threading.Thread(target=lambda: M.norm_rope(x))
+            other.start()
+            other.join()
+            assert not calls
+            y = M.norm_rope(leaf)
+            assert len(calls) == 1
+            y.backward(torch.ones_like(y))
+            assert len(calls) == 2
+    finally:
+        mode.close()
+    torch.cuda.synchronize()
+    one = x.clone().requires_grad_()
+    M.norm_rope(one).backward(torch.ones_like(x))
+    assert torch.equal(leaf.grad.cpu(), one.grad.cpu())
+
+
+def test_a_number_in_a_tensor_is_read_at_every_call():
+    x, eps = torch.randn(5, 2, 8, device="cuda"), torch.tensor(1e-6)
+    first = M.norm_rope(x, eps=eps)
+    assert torch.equal(first, M.norm_rope(x, eps=eps.item()))
+    eps.fill_(1.0)
+    second = M.norm_rope(x, eps=eps)
+    assert torch.equal(second, M.norm_rope(x, eps=1.0)) and not torch.equal(first, second)
+
+
+def test_outputs_that_autograd_has_saved_or_watches():
+    x, w = torch.randn(3, 2, 8, device="cuda"), torch.randn(3, 2, 8, device="cuda", requires_grad=True)
+    logits, wl = torch.randn(3, 20, device="cuda"), torch.randn(3, 20, device="cuda", requires_grad=True)
+    _, scales, cache, ks = cache_of(2, 4, 2, 8, 1, torch.int8, "heads")
+    pages, rows, wr = torch.tensor([[1]], dtype=torch.int32, device="cuda"), torch.randn(1, 3, 2, 8, device="cuda"), torch.randn(1, 3, 2, 8, device="cuda", requires_grad=True)
+    calls = [(w, x.clone(), lambda o: M.norm_rope(x, out=o)), (wl, logits.clone(), lambda o: M.penalize_logits(logits, out=o)),
+             (wr, rows, lambda o: M.cache_load(cache, ks, pages, None, 3, out=o)),
+             (w, x.clone(), lambda o: M.norm_rope_qk(x, x, out=(o, None)))]
+    for leaf, out, call in calls:
+        product = leaf * out                                 # keeps `out` for the gradient
+        call(out)
+        with pytest.raises(RuntimeError, match="inplace"):
+            product.sum().backward()
+        with pytest.raises(ValueError):
+            call(leaf)
+        with torch.no_grad():
+            call(leaf)
+        with torch.inference_mode():
+            call(torch.empty_like(out))
+
+
 def test_every_operand_with_strides_of_its_own():
     gen = torch.Generator().manual_seed(13)
     every = lambda t: up(torch.stack((t, t), -1).flatten(-2))[..., ::2]      # every second element of twice as many

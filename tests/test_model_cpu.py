@@ -186,3 +186,19 @@ def test_the_definition_of_the_gradients_is_that_of_the_function(d, r, pairs):
     want = torch.autograd.grad(z, (x, g), dz)
     dx, _, dg, _ = ref.norm_rope_grad(dz, x.detach(), g.detach(), table, p, 1e-3, pairs)
     assert torch.allclose(dx, want[0], rtol=1e-12, atol=1e-12) and torch.allclose(dg, want[1], rtol=1e-12, atol=1e-12)
+
+
+def test_tensors_of_one_call_are_on_one_device():
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def get_device(self):
+            return self.device
+
+        def numel(self):
+            return 1
+    task = bytes(S.MODEL_TASK_BYTES)
+    assert M._Plan([On(1), On(1)], [task] * 2, [(), ()]).device == 1
+    with pytest.raises(ValueError):
+        M._Plan([On(0), On(1)], [task] * 2, [(), ()])
