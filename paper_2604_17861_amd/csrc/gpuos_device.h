@@ -3135,7 +3135,7 @@ DEV int32_t exec_chunk(const Record* r, const RecHead& h, uint32_t impl, uint32_
     case GPUOS_IMPL_FAIL: return GPUOS_E_BADOP;       // kill-switch stub: fail fast, write nothing
     default:
 #if !defined(__HIPCC_RTC__)
-      if (POL == POL_COHERENT && impl >= GPUOS_IMPL_NORM_ROPE && impl <= GPUOS_IMPL_LOGIT_PENALTY && h.path() == PATH_MODEL) {
+      if (__builtin_expect(POL == POL_COHERENT && h.path() == PATH_MODEL && impl <= GPUOS_IMPL_LOGIT_PENALTY, 0)) {
         exec_model((const ModelRecord*)r, chunk, s_red, tid);
         break;
       }
