@@ -326,7 +326,7 @@ def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
 def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
     eps, pairs = float(eps), bool(pairs)
     key = ("backward", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in douts])
-    plans = _plans.get(key)
+    plan = _plans.get(key)
     dxs, dgs, grads, sums = [], [], [], []
     for dout, x, gamma in zip(douts, xs, gammas):
         dx, dg, partial = _empty_like(x), None, None
@@ -339,13 +339,10 @@ def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
         grads.append((x, gamma, table, positions, dx, dout, partial))
         dxs.append(dx)
         dgs.append(dg)
-    if plans is None:
-        plans = _keep(key, (
-            _Plan(xs, [norm_rope_grad_task(o[5], *o[:5], o[6], eps=eps, pairs=pairs) for o in grads], grads),
-            _Plan([o[0] for o in sums], [gamma_sum_task(*o) for o in sums], sums) if sums else None))
-    _run(plans[0], sum(grads, ()))
-    if sums:
-        _run(plans[1], sum(sums, ()))
+    if plan is None:                                        # (a sum is another operator than what it adds up, so a launch behind it)
+        tasks = [norm_rope_grad_task(o[5], *o[:5], o[6], eps=eps, pairs=pairs) for o in grads] + [gamma_sum_task(*o) for o in sums]
+        plan = _keep(key, _Plan([o[0] for o in grads + sums], tasks, grads + sums))
+    _run(plan, sum(grads + sums, ()))
     return dxs, dgs
 
 
