@@ -44,14 +44,15 @@ template <int POL> struct Glob {
     }
     return *(const G<v4i_any>*)p;
   }
+  static DEV void apart() { asm volatile(""); }      // (or the compiler makes one store without the hint of the two)
   static DEV void st8(uint64_t p, v2i q, bool nt = false) {
     if (POL == POL_COHERENT) put<uint64_t>(p, __builtin_bit_cast(uint64_t, q));
-    else if (nt) __builtin_nontemporal_store((v2i_any)q, (G<v2i_any>*)p);
+    else if (nt) { apart(); __builtin_nontemporal_store((v2i_any)q, (G<v2i_any>*)p); apart(); }
     else *(G<v2i_any>*)p = q;
   }
   static DEV void st16(uint64_t p, v4i q, bool nt = false) {
     if (POL == POL_COHERENT) { st8(p, v2i{q[0], q[1]}); st8(p + 8, v2i{q[2], q[3]}); }
-    else if (nt) __builtin_nontemporal_store((v4i_any)q, (G<v4i_any>*)p);
+    else if (nt) { apart(); __builtin_nontemporal_store((v4i_any)q, (G<v4i_any>*)p); apart(); }
     else *(G<v4i_any>*)p = q;
   }
   static DEV v2i ld8b(uint64_t p) { return POL == POL_COHERENT ? ld8(p) : (v2i)*(const G<v2i_byte>*)p; }      // bytes
