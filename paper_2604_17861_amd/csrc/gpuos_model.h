@@ -118,6 +118,9 @@ GPUOS_HD inline uint32_t rope_units(uint32_t d, uint32_t half, bool pairs) { ret
 // and for 327,680 of 128 bf16, norm and rotation 3.6, 4.3, 6.0 and 38.3, 36.9, 35.0 us, the gradient (262,144 heads) 4.2, 4.8, 6.0 and 56.1, 50.3, 49.2;
 // storing 2.4, 3.0, 4.7 and 19.2, 19.8, 22.7 (262,144 heads), reading back 2.2, 2.5, 3.1 and 179, 159, 157 (2,097,152 heads).
 constexpr uint32_t kRopeBlock = 4, kGradBlock = 2, kStoreBlock = 2, kLoadBlock = 4;
+// In the ring, whose workgroups do not make up for each other's waits: twice as many of the cache's (744 MB read back 193 -> 168 us, 100 MB stored
+// 52 -> 49, a token's the same); of rotations they made a token 17 us of 14, and 172 MB 64 of 69.
+constexpr uint32_t kRingStoreBlock = 4, kRingLoadBlock = 8;
 constexpr uint32_t kModelLaunch = 8;         // tasks of one launch: their records are kernel arguments, 2 KB of the 4 KB there may be
 
 // What gpuos_launch_model hands a kernel: tasks of one variant.  (A block's second index is its task's place here: its
@@ -153,9 +156,9 @@ GPUOS_HD inline uint32_t model_variant(uint32_t impl, uint32_t vec, uint32_t dty
 // Of the passes that a workgroup makes over all items, chunk c makes every nchunks-th from the c-th on, so that what is worked on at a
 // time lies together in memory: 2,097,152 heads read back in 2,048 chunks of passes that follow each other took 159 us, in 4,096 148, in
 // 16,384, a pass each, 124.
-struct ModelCut { uint32_t least_bytes, most; bool aligned; };
-constexpr ModelCut kRingCut{16384, kMaxChunksPerTask, true};       // a unit costs the dispatcher 12 ns and the worker about a microsecond
-constexpr ModelCut kLaunchCut{4096, 65536, false};
+struct ModelCut { uint32_t least_bytes, most; bool aligned; uint32_t store_block, load_block; };
+constexpr ModelCut kRingCut{16384, kMaxChunksPerTask, true, kRingStoreBlock, kRingLoadBlock};       // a unit costs the dispatcher 12 ns and the worker about a microsecond
+constexpr ModelCut kLaunchCut{4096, 65536, false, kStoreBlock, kLoadBlock};
 
 // Checks and packs one descriptor.
 class ModelPack {
@@ -390,7 +393,7 @@ class ModelPack {
     const uint32_t es = size_of(x.dtype);
     if (d >= 8 && (!cut.aligned || d % 8 == 0) && vectors(cut, r.x, es, r.xs, 3, r.xs[3] == 1) && vectors(cut, r.cache, 1, r.cs, 3, true)) r.h.vec = 1;
     if (!store && lines(r.x, es, r.xs, 3, (uint32_t)d)) r.h.flags |= MF_LINES;
-    in_blocks(r, (uint64_t)tokens, r.h.vec ? (store ? kStoreBlock : kLoadBlock) : 1);
+    in_blocks(r, (uint64_t)tokens, r.h.vec ? (store ? cut.store_block : cut.load_block) : 1);
     cut_items(r.h, cut, (uint64_t)d * (es + 1) * r.h.block, rows_at_once(r.h.vec ? (uint32_t)(d + 7) / 8 : (uint32_t)d));
     return GPUOS_OK;
   }
@@ -427,7 +430,7 @@ class ModelPack {
         bias_ok && allowed_ok)
       r.h.vec = 1;
     if (lines(r.out, es, r.os, 1, 64)) r.h.flags |= MF_LINES;
-    cut_items(r.h, ModelCut{1, cut.most, cut.aligned}, 1, 1);
+    cut_items(r.h, ModelCut{1, cut.most, cut.aligned, 0, 0}, 1, 1);
     return GPUOS_OK;
   }
 

@@ -37,8 +37,20 @@ template <int POL> struct Glob {
     if (POL == POL_COHERENT) return __builtin_bit_cast(v2i, at<uint64_t>(p));
     return *(const G<v2i_any>*)p;
   }
+  // A coherent access of 16 bytes, by a buffer resource: whether the addresses of a wavefront's active lanes lie within a gigabyte of the
+  // first one's; then r begins a gigabyte below that, so that no access reaches its end, and p is `off` from it.  (In two of 8 bytes, with gaps
+  // of as many between the lanes', a store moves half lines: 744 MB read back from the cache 422 us, so 193.)
+  static DEV bool near(uint64_t p, rsrc_t& r, uint32_t& off) {
+    const uint64_t first = uni64(p), base = first > (1ull << 30) ? first - (1ull << 30) : 0;
+    off = (uint32_t)(p - base);
+    r = make_rsrc((const void*)(__UINTPTR_TYPE__)base, 0xffffffffu);
+    return __builtin_amdgcn_ballot_w64((p - base) >> 31 != 0) == 0;
+  }
   static DEV v4i ld16(uint64_t p) {
     if (POL == POL_COHERENT) {
+      rsrc_t r;
+      uint32_t off;
+      if (near(p, r, off)) return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, Mem<POL>::BASE);
       const v2i a = ld8(p), b = ld8(p + 8);
       return v4i{a[0], a[1], b[0], b[1]};
     }
@@ -51,8 +63,12 @@ template <int POL> struct Glob {
     else *(G<v2i_any>*)p = q;
   }
   static DEV void st16(uint64_t p, v4i q, bool nt = false) {
-    if (POL == POL_COHERENT) { st8(p, v2i{q[0], q[1]}); st8(p + 8, v2i{q[2], q[3]}); }
-    else if (nt) { apart(); __builtin_nontemporal_store((v4i_any)q, (G<v4i_any>*)p); apart(); }
+    if (POL == POL_COHERENT) {
+      rsrc_t r;
+      uint32_t off;
+      if (near(p, r, off)) __builtin_amdgcn_raw_buffer_store_b128(q, r, (int)off, 0, Mem<POL>::BASE);
+      else { st8(p, v2i{q[0], q[1]}); st8(p + 8, v2i{q[2], q[3]}); }
+    } else if (nt) { apart(); __builtin_nontemporal_store((v4i_any)q, (G<v4i_any>*)p); apart(); }
     else *(G<v4i_any>*)p = q;
   }
   static DEV v2i ld8b(uint64_t p) { return POL == POL_COHERENT ? ld8(p) : (v2i)*(const G<v2i_byte>*)p; }      // bytes
@@ -158,6 +174,9 @@ DEV uint64_t offset(const Place& p, const uint32_t (&st)[4]) { return (uint64_t)
 // Bound by memory: one read and one write of the rows (two reads backwards), some ten instructions an element.  A part of a wavefront
 // holds a row in registers; what a lane holds are both halves of its pairs, so that a rotation needs no other lane, and of the sums
 // only the row's go over lanes.  A lane has the same elements of every row, so gamma stays in its registers.
+// As kernels, 128 bf16 a head, where a large copy moves 4.76 TB/s: 172 MB forwards 36.3 us (4.7 TB/s), 205 MB backwards 47 (4.4; the sums
+// of gamma's shares another 3); 24 heads of one token 4.8.  As tasks of the ring 69, 96 and 14 us from submission to completion: there a
+// workgroup waits for its loads before it makes the next pass, and three of them share a compute unit.
 // ---------------------------------------------------------------------------
 struct RopeArgs {
   uint64_t x, gamma, table, positions, out, dout, partial;
@@ -462,6 +481,9 @@ template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* 
 // Bound by memory, three bytes of it an element of 16 bits.  A part of a wavefront takes a row: eight elements a lane, one load of 16
 // bytes on the wide side and one of 8 on the cache's; a group's largest magnitude goes over the lanes that hold it, as an integer
 // (magnitudes order like their bits, infinities and NaNs above all).
+// As kernels, 128 bf16 a head: 16,384 tokens of 8 heads of keys and values (98 MB) stored in 19.6 us (5.0 TB/s, a part of it from the
+// memory-side cache), 32 sequences of 4,096 such tokens at most read back (537 MB written, 208 read) in 123 (6.0 TB/s), 64 tokens stored in 3.5; as
+// tasks of the ring 49, 169 and 13 us.
 // ---------------------------------------------------------------------------
 struct CacheArgs {
   uint64_t x, cache, scales, slots, lengths;
@@ -524,7 +546,7 @@ DEV uint64_t scale_at(const CacheArgs& a, uint32_t page, uint32_t in, uint32_t h
 template <int POL, int DT> DEV void store_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
   typedef Eight<POL, DT> E;
-  constexpr int U = kStoreBlock;
+  constexpr int U = POL == POL_COHERENT ? kRingStoreBlock : kStoreBlock;
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;      // (the last window ends with the row: what two have both write alike)
@@ -626,7 +648,7 @@ template <int POL> DEV uint32_t sequence_row(const CacheArgs& a, const Place& p,
 }
 template <int POL, int DT> DEV void load_vectors(const CacheArgs& a, uint32_t chunk, uint32_t tid) {
   typedef Glob<POL> M;
-  constexpr int U = kLoadBlock;
+  constexpr int U = POL == POL_COHERENT ? kRingLoadBlock : kLoadBlock;
   const uint32_t units = (a.d + 7u) / 8u, lg = ceil_log2(units), lanes = 1u << lg;
   const uint32_t u = tid & (lanes - 1u), group = tid >> lg, step = kThreads >> lg;
   const uint32_t at = 8u * u < a.d - 8u ? 8u * u : a.d - 8u;
@@ -702,7 +724,9 @@ template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, ui
 //
 // Bound by memory (one read and one write of the logits) while the history is short.  The workgroup takes a row in segments: the
 // tokens of the row's history that fall into the segment are counted in LDS (additions of integers: their order does not matter), then
-// the segment is changed and written.  Every segment reads the row's history, from the cache after the first.
+// the segment is changed and written.  Every segment reads the row's history, from the cache after the first: for long ones that is
+// what bounds it.  64 rows of 100,352 bf16 with 2,048 tokens, bias and bits 10.6 us as a kernel (27 MB, 5.8 us at a copy's rate, and
+// the 4 that the way from the record over the history to the counts takes), 8 of 65,537 with 32,768 tokens 8.4, one of 32,003 with 200 4.1; as tasks of the ring 46, 37 and 12.
 // A count has 31 bits; the top bit says that the token is in the prompt.
 // ---------------------------------------------------------------------------
 struct PenaltyArgs {
