@@ -174,8 +174,8 @@ DEV uint64_t offset(const Place& p, const uint32_t (&st)[4]) { return (uint64_t)
 // Bound by memory: one read and one write of the rows (two reads backwards), some ten instructions an element.  A part of a wavefront
 // holds a row in registers; what a lane holds are both halves of its pairs, so that a rotation needs no other lane, and of the sums
 // only the row's go over lanes.  A lane has the same elements of every row, so gamma stays in its registers.
-// As kernels, 128 bf16 a head, where a large copy moves 4.76 TB/s: 172 MB forwards 36.3 us (4.7 TB/s), 205 MB backwards 47 (4.4; the sums
-// of gamma's shares another 3); 24 heads of one token 4.8.  As tasks of the ring 69, 96 and 14 us from submission to completion: there a
+// As kernels, 128 bf16 a head, where a large copy moves 4.76 TB/s: 172 MB forwards 36.3 us (4.7 TB/s), 205 MB backwards 43.5 (4.7; the sums
+// of gamma's shares another 4); 24 heads of one token 4.8.  As tasks of the ring 69, 96 and 14 us from submission to completion: there a
 // workgroup waits for its loads before it makes the next pass, and three of them share a compute unit.
 // ---------------------------------------------------------------------------
 struct RopeArgs {

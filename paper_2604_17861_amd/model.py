@@ -275,10 +275,12 @@ def penalty_task(x, out, history=None, prompt_lengths=None, params=None, bias=No
 
 # ---- norm and rotation -----------------------------------------------------------------------------
 
-def _parts(x):
-    """Shares of gamma's gradient: as many as there are passes of a workgroup (32 rows of 128), at most PARTS_MAX."""
+def _parts(x, tensors=1):
+    """Shares of gamma's gradient, a workgroup each: as many as there are passes of one (32 rows of 128), at most PARTS_MAX, and of all tensors of
+    a launch no more than the card's 256 units take at once by their registers (five of 16 bits each, four of 32).  Two of 8,192 x 16 heads
+    of 128 bf16 with 1,024 / 768 / 640 / 512 shares each: 52, 46, 47, 48 us; 8,192 x 32 of fp32 153, 165, 155, 152; one alone 26 to 29."""
     rows = x.numel() // x.shape[-1]
-    return min(PARTS_MAX, max(1, rows // 32))
+    return min(PARTS_MAX, 256 * (4 if x.dtype == torch.float32 else 5) // tensors, max(1, rows // 32))
 
 
 def _written(outs):
@@ -334,7 +336,7 @@ def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
             if x.numel() == 0:
                 dg = torch.zeros_like(gamma)
             else:
-                dg, partial = _empty_like(gamma), x.new_empty((x.shape[-1], _parts(x)), dtype=torch.float32)
+                dg, partial = _empty_like(gamma), x.new_empty((x.shape[-1], _parts(x, len(xs))), dtype=torch.float32)
                 sums.append((partial, dg))
         grads.append((x, gamma, table, positions, dx, dout, partial))
         dxs.append(dx)
