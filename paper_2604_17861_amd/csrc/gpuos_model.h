@@ -350,7 +350,8 @@ class ModelPack {
     r.h.dtype[1] = out.dtype;
     r.h.items = (uint32_t)t.size[0];
     r.h.d = (uint32_t)t.size[1];
-    cut_items(r.h, cut, 4ull * r.h.d + 4, 1);
+    // (a row is a wait for memory and two barriers however short it is: 128 rows of one share each by one workgroup take 49 us, by one each 4)
+    cut_items(r.h, cut, r.h.d < 1024 ? 4096u : 4ull * r.h.d, 1);
     return GPUOS_OK;
   }
 

@@ -118,6 +118,13 @@ def test_empty_sizes_are_empty_tasks():
     assert all(p["vectors"] == 0 and p["chunks"] == 5 for p in grad(b=0))      # its shares are written all the same
 
 
+def test_rows_of_sums_are_shared_out_however_short():
+    """A row takes a workgroup the same time from one share to a thousand."""
+    for shares in (0, 1, 7, 640, 1024):
+        ring, kernel = plan("GAMMA_SUM", (128, shares), (op(F32, shares, 1), op(BF16, 1)))
+        assert ring["chunks"] == 32 and kernel["chunks"] == 128
+
+
 def test_chunks_cover_every_row_once_and_stay_in_their_bounds():
     rng = np.random.default_rng(0)
     for _ in range(400):
