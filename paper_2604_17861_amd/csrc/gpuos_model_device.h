@@ -725,7 +725,7 @@ template <int POL> DEV void load_elements(const CacheArgs& a, uint32_t chunk, ui
 // Bound by memory (one read and one write of the logits) while the history is short.  The workgroup takes a row in segments: the
 // tokens of the row's history that fall into the segment are counted in LDS (additions of integers: their order does not matter), then
 // the segment is changed and written.  Every segment reads the row's history, from the cache after the first: for long ones that is
-// what bounds it.  64 rows of 100,352 bf16 with 2,048 tokens, bias and bits 10.6 us as a kernel (27 MB, 5.8 us at a copy's rate, and
+// what bounds it.  64 rows of 100,352 bf16 with 2,048 tokens, bias and bits 10.2 us as a kernel (27 MB, 5.8 us at a copy's rate, and
 // the 4 that the way from the record over the history to the counts takes), 8 of 65,537 with 32,768 tokens 8.4, one of 32,003 with 200 4.1; as tasks of the ring 46, 37 and 12.
 // A count has 31 bits; the top bit says that the token is in the prompt.
 // ---------------------------------------------------------------------------
