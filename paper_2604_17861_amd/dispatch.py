@@ -43,8 +43,9 @@ HIP worker kernel through the C ABI (Runtime.submit).  Ordering rules that keep 
     (back-distance in the descriptor), so chains need no host wait;
   * a PyTorch kernel that touches memory a pending task reads or writes is held back until that
     task has completed (host wait on its ticket); view operations only pass the storage along;
-  * before the first redirected operation after PyTorch launched work of its own, the current
-    stream is synchronised once (its kernels may still be writing the inputs);
+  * before the first redirected operation after PyTorch launched work of its own, and before the first
+    of every `with` block (what ran outside was not seen), the current stream is synchronised once
+    (its kernels may still be writing the inputs);
   * every tensor a pending task names is kept alive until the task has completed, so the caching
     allocator cannot hand its memory to somebody else;
   * leaving the `with` block (or `synchronize()`) drains everything.
@@ -488,6 +489,7 @@ class GpuosMode(TorchDispatchMode):
     def __enter__(self):
         r = super().__enter__()
         R.active_filters.append(self)
+        self._dirty = True                             # whatever was launched since the last block is not known here
         return r
 
     def _wait(self, ticket):

@@ -396,3 +396,22 @@ def test_results_are_laid_out_as_eager_lays_them_out():
             kinds.add(w.is_contiguous())
         torch.testing.assert_close(got[-1], want[-1])
     assert kinds == {True, False}
+
+
+def test_the_first_redirected_operation_of_every_block_waits_for_the_stream(monkeypatch):
+    """What ran between two blocks was not seen: its kernels may still be writing what the second block reads."""
+    class Gpu:                                     # the tensors' device, by the type that has streams
+        type = "cuda"
+
+        def __eq__(self, other):
+            return other == torch.device("cpu")
+    m = mode()
+    m.device = Gpu()
+    waits = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: SimpleNamespace(synchronize=lambda: waits.append(1)))
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype, device, empty=torch.empty: empty(shape, dtype=dtype))
+    a = torch.randn(3, 4)
+    for block in range(3):
+        with m:
+            torch.relu(torch.relu(a))
+        assert len(waits) == m.stats["stream_syncs"] == block + 1 and m.stats["redirected"] == 2 * block + 2
