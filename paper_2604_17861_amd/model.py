@@ -284,10 +284,10 @@ def _parts(x, tensors=1):
 
 
 def _written(outs):
-    """Outputs of the caller's: what autograd has saved of them is no longer what it was."""
+    """Tensors of the caller's that a call writes: what autograd has saved of them is no longer what it was."""
     for o in outs:
         if isinstance(o, torch.Tensor):
-            _no_gradient("out", o)
+            _no_gradient("what is written", o)
             if not o.is_inference():
                 increment_version(o)
 
@@ -395,6 +395,7 @@ def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, 
 # ---- the cache -------------------------------------------------------------------------------------
 
 def _store(xs, slots, caches, scales):
+    _written((*caches, *scales))
     key = ("store", _sig(slots), *[_sig(t) for t in xs], *[_sig(t) for t in caches], *[_sig(t) for t in scales])
     plan = _plans.get(key)
     operands = [(x, slots, c, s) for x, c, s in zip(xs, caches, scales)]

@@ -1,0 +1,55 @@
+"""What the model operators tell autograd, and what they refuse because they can not: on the CPU, with the library's launch replaced by
+one that takes the descriptors and computes nothing."""
+import pytest
+import torch
+
+from paper_2604_17861_amd import model as M
+from paper_2604_17861_amd import runtime as R
+
+
+@pytest.fixture
+def launched(monkeypatch):
+    """Operators on tensors of the CPU; the number of descriptors of every launch."""
+    calls, check = [], M._check
+    monkeypatch.setattr(M, "_check", lambda x, what, dtypes=None, dims=None, shape=None, device=None, **kw: check(
+        x, what, dtypes, dims, shape, x.device if device is None and isinstance(x, torch.Tensor) else device, **kw))
+    monkeypatch.setattr(M, "_stream_of", lambda device: 0)
+    monkeypatch.setattr(R, "launch_model_at", lambda tasks, n, device, stream: calls.append(n))
+    monkeypatch.setattr(M, "_plans", {})
+    return calls
+
+
+def a_cache(groups=1):
+    return torch.zeros(2, 4, 2, 8, dtype=torch.int8), torch.ones(2, 4, 2, groups)
+
+
+SLOTS = torch.tensor([0, 5, 2], dtype=torch.int32)
+PAGES = torch.tensor([[1]], dtype=torch.int32)
+
+
+def test_stored_rows_count_as_written(launched):
+    x = torch.randn(3, 2, 8)
+    (kc, ks), (vc, vs) = a_cache(), a_cache()
+    scores = torch.randn(2, 4, 2, 1, requires_grad=True)
+    for call, tensors in ((lambda: M.cache_store(x, SLOTS, kc, ks), (kc, ks)), (lambda: M.cache_store_kv(x, x, SLOTS, kc, ks, vc, vs), (kc, ks, vc, vs))):
+        before = [t._version for t in tensors]
+        product = scores * ks                                # keeps the scales for the gradient
+        call()
+        assert all(t._version > v for t, v in zip(tensors, before))
+        with pytest.raises(RuntimeError, match="inplace"):
+            product.sum().backward()
+    assert launched == [1, 2]
+
+
+def test_scales_that_require_a_gradient_are_not_overwritten(launched):
+    x = torch.randn(3, 2, 8)
+    (kc, ks), (vc, vs) = a_cache(), a_cache()
+    vs.requires_grad_()
+    for call in (lambda: M.cache_store(x, SLOTS, vc, vs), lambda: M.cache_store_kv(x, x, SLOTS, kc, ks, vc, vs)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    with torch.inference_mode():                             # (tensors without versions)
+        M.cache_store(x, SLOTS, *a_cache())
+    assert launched == [1, 2, 1]
