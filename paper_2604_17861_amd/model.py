@@ -89,8 +89,9 @@ def _keep(key, plan):
     return plan
 
 
-def _run(plan, operands):
-    """Launch with these addresses: the operands of all tasks, one after the other."""
+def _run(plan, operands, written=()):
+    """Launch with these addresses: the operands of all tasks, one after the other.  written: tensors of the caller's among
+    them (None: left out) that the call writes; what autograd has saved of those is no longer what it was."""
     if plan.n:
         if R.active_filters:                                # (tasks of this thread's dispatch filter may still be working on these)
             for f in _get_current_dispatch_mode_stack():
@@ -100,6 +101,9 @@ def _run(plan, operands):
         for word, k in plan.at:
             words[word] = operands[k].data_ptr()
         R.launch_model_at(words.buffer_info()[0], plan.n, plan.device, _stream_of(plan.device))
+        for o in written:
+            if o is not None and not o.is_inference():
+                increment_version(o)
 
 
 # the handle of a device's current stream: torch.cuda.current_stream(device).cuda_stream, which makes two objects for it (1.1 us)
@@ -283,15 +287,6 @@ def _parts(x, tensors=1):
     return min(PARTS_MAX, 256 * (4 if x.dtype == torch.float32 else 5) // tensors, max(1, rows // 32))
 
 
-def _written(outs):
-    """Tensors of the caller's that a call writes: what autograd has saved of them is no longer what it was."""
-    for o in outs:
-        if isinstance(o, torch.Tensor):
-            _no_gradient("what is written", o)
-            if not o.is_inference():
-                increment_version(o)
-
-
 def _empty_like(x):
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
@@ -317,11 +312,11 @@ def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
     eps, pairs = float(eps), bool(pairs)                    # (a key holds values, not objects)
     key = ("norm_rope", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in outs])
     plan = _plans.get(key)
-    outs = [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
+    given, outs = outs, [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
     operands = [(x, g, table, positions, o) for x, g, o in zip(xs, gammas, outs)]
     if plan is None:
         plan = _keep(key, _Plan(xs, [norm_rope_task(*o, eps=eps, pairs=pairs) for o in operands], operands))
-    _run(plan, sum(operands, ()))
+    _run(plan, sum(operands, ()), given)
     return tuple(outs)
 
 
@@ -367,7 +362,7 @@ def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=Fals
     _no_gradient("table", table)
     if _differentiable((x, gamma), (out,)):
         return _NormRope.apply(table, positions, eps, pairs, x, gamma)[0]
-    _written((out,))
+    _no_gradient("out", out)
     return _norm_rope((x,), (gamma,), table, positions, eps, pairs, (out,))[0]
 
 
@@ -376,7 +371,7 @@ def norm_rope_qk(q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *
     _no_gradient("table", table)
     if _differentiable((q, k, gamma_q, gamma_k), out):
         return _NormRope.apply(table, positions, eps, pairs, q, gamma_q, k, gamma_k)
-    _written(out)
+    _no_gradient("out", *out)
     return _norm_rope((q, k), (gamma_q, gamma_k), table, positions, eps, pairs, out)
 
 
@@ -395,13 +390,13 @@ def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, 
 # ---- the cache -------------------------------------------------------------------------------------
 
 def _store(xs, slots, caches, scales):
-    _written((*caches, *scales))
+    _no_gradient("scales", *scales)
     key = ("store", _sig(slots), *[_sig(t) for t in xs], *[_sig(t) for t in caches], *[_sig(t) for t in scales])
     plan = _plans.get(key)
     operands = [(x, slots, c, s) for x, c, s in zip(xs, caches, scales)]
     if plan is None:
         plan = _keep(key, _Plan(xs, [cache_store_task(*o) for o in operands], operands))
-    _run(plan, sum(operands, ()))
+    _run(plan, sum(operands, ()), (*caches, *scales))
 
 
 def cache_store(x, slots, cache, scales):
@@ -417,18 +412,18 @@ def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
 
 def _load(caches, scales, pages, lengths, length, dtype, outs):
     length = int(length)
-    _written(outs)
+    _no_gradient("out", *outs)
     key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
     plan = _plans.get(key)
     if plan is None:
         for c in caches:
             _check(c, "cache", _CACHE, (4,))
         _check(pages, "pages", _INT, (2,), None, caches[0].device)
-    outs = [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype) if o is None else o for c, o in zip(caches, outs)]
+    given, outs = outs, [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype) if o is None else o for c, o in zip(caches, outs)]
     operands = [(c, s, pages, lengths, o) for c, s, o in zip(caches, scales, outs)]
     if plan is None:
         plan = _keep(key, _Plan(outs, [cache_load_task(*o) for o in operands], operands))
-    _run(plan, sum(operands, ()))
+    _run(plan, sum(operands, ()), given)
     return tuple(outs)
 
 
@@ -449,18 +444,17 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
     """Penalties of the tokens in history [B, N] (entries that are no token count for nothing; the first prompt_lengths[b] for the
     repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
     not set.  out may be x.  Not differentiable: logits that require a gradient are refused where gradients are recorded."""
-    _no_gradient("penalize_logits", x, params, bias)
-    _written((out,))
+    _no_gradient("penalize_logits", x, params, bias, out)
     key = ("penalty", _sig(x), _sig(history), _sig(prompt_lengths), _sig(params), _sig(bias), _sig(allowed), _sig(out))
     plan = _plans.get(key)
     if plan is None:
         _check(x, "x", _FLOAT, (2,))
-    out = _empty_like(x) if out is None else out
+    given, out = out, _empty_like(x) if out is None else out
     operands = (x, out, history, prompt_lengths, params, bias, allowed)
     if plan is None:
         task = penalty_task(*operands)
         if history is not None and history.shape[1] == 0:   # (nothing is counted: as without one)
             operands = (x, out, None, None, None, bias, allowed)
         plan = _keep(key, _Plan((x,), (task,), (operands,)))
-    _run(plan, operands)
+    _run(plan, operands, (given,))
     return out

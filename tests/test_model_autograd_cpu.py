@@ -53,3 +53,25 @@ def test_scales_that_require_a_gradient_are_not_overwritten(launched):
     with torch.inference_mode():                             # (tensors without versions)
         M.cache_store(x, SLOTS, *a_cache())
     assert launched == [1, 2, 1]
+
+
+def test_a_refused_call_has_written_nothing(launched, monkeypatch):
+    x, out, bad = torch.randn(3, 2, 8), torch.zeros(3, 2, 8), torch.zeros(3, 2, 9)
+    (kc, ks), rows = a_cache(), torch.zeros(1, 3, 2, 8)
+    short = torch.zeros(2, dtype=torch.int32)
+    calls = [(out, lambda: M.norm_rope(bad, out=out)), (out, lambda: M.norm_rope_qk(x, bad, out=(out, out))), (rows, lambda: M.cache_load(kc, kc, PAGES, None, 3, out=rows)),
+             (ks, lambda: M.cache_store(x, short, kc, ks)), (out, lambda: M.penalize_logits(x, out=out))]
+    for tensor, call in calls:
+        with pytest.raises(ValueError):
+            call()
+        assert tensor._version == 0
+    for tensor, call in ((out, lambda: M.norm_rope(x, out=out)), (rows, lambda: M.cache_load(kc, ks, PAGES, None, 3, out=rows)), (ks, lambda: M.cache_store(x, SLOTS, kc, ks))):
+        def refuse(*args):
+            raise R.GpuosError(R.E_INVAL, "gpuos_launch_model")
+        with monkeypatch.context() as m:
+            m.setattr(R, "launch_model_at", refuse)          # by the library
+            with pytest.raises(R.GpuosError):
+                call()
+        assert tensor._version == 0
+        call()
+        assert tensor._version == 1
