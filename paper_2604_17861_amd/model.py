@@ -376,13 +376,15 @@ def norm_rope_qk(q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *
 
 
 def norm_rope_backward(dout, x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=False):
-    """Gradients of norm_rope for x and gamma (None without one)."""
+    """Gradients of norm_rope for x and gamma (None without one).  Not differentiable themselves."""
+    _no_gradient("norm_rope_backward", dout, x, gamma, table)
     (dx,), (dg,) = _norm_rope_backward((dout,), (x,), (gamma,), table, positions, eps, pairs)
     return dx, dg
 
 
 def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, positions=None, *, eps=1e-6, pairs=False):
-    """Gradients of norm_rope_qk for q, k, gamma_q and gamma_k, in two launches."""
+    """Gradients of norm_rope_qk for q, k, gamma_q and gamma_k, in two launches.  Not differentiable themselves."""
+    _no_gradient("norm_rope_qk_backward", dq, dk, q, k, gamma_q, gamma_k, table)
     (gq, gk), (ggq, ggk) = _norm_rope_backward((dq, dk), (q, k), (gamma_q, gamma_k), table, positions, eps, pairs)
     return gq, gk, ggq, ggk
 
@@ -390,7 +392,7 @@ def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, 
 # ---- the cache -------------------------------------------------------------------------------------
 
 def _store(xs, slots, caches, scales):
-    _no_gradient("scales", *scales)
+    _no_gradient("cache_store", *xs, *scales)
     key = ("store", _sig(slots), *[_sig(t) for t in xs], *[_sig(t) for t in caches], *[_sig(t) for t in scales])
     plan = _plans.get(key)
     operands = [(x, slots, c, s) for x, c, s in zip(xs, caches, scales)]
@@ -401,7 +403,8 @@ def _store(xs, slots, caches, scales):
 
 def cache_store(x, slots, cache, scales):
     """Quantise rows of x [T, H, D] (or [B, S, H, D]) into slots (page index * page + place; negative: nowhere) of cache
-    [pages, page, H, D] (int8 or float8_e4m3fn) and scales [pages, page, H, groups] (float32).  Slots are distinct."""
+    [pages, page, H, D] (int8 or float8_e4m3fn) and scales [pages, page, H, groups] (float32).  Slots are distinct.  Not
+    differentiable: rows or scales that require a gradient are refused where gradients are recorded."""
     _store((x,), slots, (cache,), (scales,))
 
 
@@ -412,7 +415,7 @@ def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
 
 def _load(caches, scales, pages, lengths, length, dtype, outs):
     length = int(length)
-    _no_gradient("out", *outs)
+    _no_gradient("cache_load", *scales, *outs)
     key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
     plan = _plans.get(key)
     if plan is None:
@@ -429,7 +432,7 @@ def _load(caches, scales, pages, lengths, length, dtype, outs):
 
 def cache_load(cache, scales, pages, lengths, length, *, dtype=torch.float32, out=None):
     """The first lengths[b] rows (None: all `length`) of every sequence b, through pages [B, width], as [B, length, H, D];
-    zeros behind them."""
+    zeros behind them.  Not differentiable: scales that require a gradient are refused where gradients are recorded."""
     return _load((cache,), (scales,), pages, lengths, length, dtype, (out,))[0]
 
 

@@ -75,3 +75,38 @@ def test_a_refused_call_has_written_nothing(launched, monkeypatch):
         assert tensor._version == 0
         call()
         assert tensor._version == 1
+
+
+def test_results_that_would_be_cut_off_from_a_gradient_are_refused(launched):
+    x, w, g = torch.randn(3, 2, 8), torch.randn(3, 2, 8, requires_grad=True), torch.ones(8, requires_grad=True)
+    plain = g.detach()
+    (kc, ks), (vc, vs) = a_cache(), a_cache()
+    ws = ks.clone().requires_grad_()
+    table = torch.randn(4, 8, requires_grad=True)
+    logits, wl = torch.randn(2, 5), torch.randn(2, 5, requires_grad=True)
+    history, params = torch.zeros(2, 3, dtype=torch.int32), torch.ones(2, 3, requires_grad=True)
+    calls = [lambda: M.cache_load(kc, ws, PAGES, None, 3), lambda: M.cache_load_kv(kc, ks, vc, ws, PAGES, None, 3),
+             lambda: M.cache_store(w, SLOTS, kc, ks), lambda: M.cache_store_kv(x, w, SLOTS, kc, ks, vc, vs),
+             lambda: M.norm_rope_backward(w, x), lambda: M.norm_rope_backward(x, w), lambda: M.norm_rope_backward(x, x, g), lambda: M.norm_rope_backward(x, x, plain, table),
+             lambda: M.norm_rope_qk_backward(x, x, x, w), lambda: M.norm_rope_qk_backward(x, x, x, x, plain, g), lambda: M.norm_rope_qk_backward(w, x, x, x),
+             lambda: M.norm_rope(x, plain, table), lambda: M.norm_rope_qk(x, x, plain, plain, table), lambda: M.penalize_logits(wl),
+             lambda: M.penalize_logits(logits, history=history, params=params), lambda: M.penalize_logits(logits, bias=wl)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert not launched
+    with torch.no_grad():
+        for call in calls:
+            call()
+    assert len(launched) == len(calls)
+
+
+def test_backward_passes_go_through(launched):
+    """The refusals are for callers: autograd's own calls are not among them."""
+    q, k, g = torch.randn(3, 2, 8, requires_grad=True), torch.randn(3, 1, 8), torch.ones(8, requires_grad=True)
+    zq, zk = M.norm_rope_qk(q, k, g, g)
+    grads = torch.autograd.grad((zq, zk), (q, g), (torch.ones_like(zq), torch.ones_like(zk)))
+    assert [t.shape for t in grads] == [q.shape, g.shape] and launched == [2, 4]
+    (grad,) = torch.autograd.grad(M.norm_rope(q).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):                        # twice is refused by autograd
+        grad.sum().backward()
