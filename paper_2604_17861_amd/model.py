@@ -17,6 +17,7 @@ import struct
 from array import array
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 from torch.utils._python_dispatch import _get_current_dispatch_mode_stack
@@ -93,6 +94,8 @@ def _run(plan, operands, written=()):
     """Launch with these addresses: the operands of all tasks, one after the other.  written: tensors of the caller's among
     them (None: left out) that the call writes; what autograd has saved of those is no longer what it was."""
     if plan.n:
+        if forward_ad._current_level >= 0:
+            _no_tangent(operands)
         if R.active_filters:                                # (tasks of this thread's dispatch filter may still be working on these)
             for f in _get_current_dispatch_mode_stack():
                 if f in R.active_filters:
@@ -104,6 +107,11 @@ def _run(plan, operands, written=()):
         for o in written:
             if o is not None and not o.is_inference():
                 increment_version(o)
+
+
+def _no_tangent(operands):
+    """Inside forward_ad.dual_level: a tangent has no way through a kernel."""
+    _need(all(t is None or forward_ad.unpack_dual(t).tangent is None for t in operands), "model operators have no forward-mode derivative")
 
 
 # the handle of a device's current stream: torch.cuda.current_stream(device).cuda_stream, which makes two objects for it (1.1 us)
@@ -347,6 +355,8 @@ def _differentiable(xs, outs):
     if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in xs):
         return False
     _need(all(o is None for o in outs), "out does not go with gradients")
+    if forward_ad._current_level >= 0:                      # (the function itself is given them without their tangents)
+        _no_tangent(xs)
     return True
 
 

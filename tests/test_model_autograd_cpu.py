@@ -2,6 +2,7 @@
 one that takes the descriptors and computes nothing."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2604_17861_amd import model as M
 from paper_2604_17861_amd import runtime as R
@@ -110,3 +111,30 @@ def test_backward_passes_go_through(launched):
     (grad,) = torch.autograd.grad(M.norm_rope(q).sum(), q, create_graph=True)
     with pytest.raises(RuntimeError):                        # twice is refused by autograd
         grad.sum().backward()
+
+
+def test_tangents_of_forward_mode_are_refused(launched):
+    x, table, g = torch.randn(3, 2, 8), torch.randn(4, 8), torch.ones(8)
+    logits, bias = torch.randn(2, 5), torch.randn(5)
+    kc, ks = a_cache()
+    leaf = x.clone().requires_grad_()
+    later = M.norm_rope(leaf)                                # a forward pass outside, its gradient inside
+    rows = torch.zeros(1, 3, 2, 8)
+    calls = [(x, lambda d: M.norm_rope(d)), (g, lambda d: M.norm_rope(x, d)), (table, lambda d: M.norm_rope(x, g, d)), (x, lambda d: M.norm_rope_qk(x, d)),
+             (logits, lambda d: M.penalize_logits(d)), (bias, lambda d: M.penalize_logits(logits, bias=d)), (ks, lambda d: M.cache_load(kc, d, PAGES, None, 3)),
+             (x, lambda d: M.cache_store(d, SLOTS, kc, ks)), (x, lambda d: M.norm_rope_backward(d, x)), (x, lambda d: M.norm_rope_backward(x, d)),
+             (rows, lambda d: M.cache_load(kc, ks, PAGES, None, 3, out=d)), (x, lambda d: torch.autograd.grad(later, leaf, d, retain_graph=True))]
+    done = len(launched)
+    with forward_ad.dual_level():
+        for t, call in calls:
+            dual = forward_ad.make_dual(t, torch.ones_like(t))
+            with pytest.raises(ValueError, match="forward-mode"):
+                call(dual)
+        with pytest.raises(ValueError, match="forward-mode"):      # both at once
+            M.norm_rope(forward_ad.make_dual(leaf, torch.ones_like(leaf)))
+        assert len(launched) == done
+        M.norm_rope(x, g, table)                             # without a tangent
+        torch.autograd.grad(later, leaf, x)
+    for t, call in calls[:-1]:
+        call(t)
+    assert len(launched) == done + 2 + len(calls) - 1
