@@ -10,6 +10,9 @@ wait for nothing, and may be captured into a graph.  The `*_task` functions make
 launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as tasks of the ring (bind the operators with
 `register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  include/gpuos.h says what every operator computes and takes.
 
+PyTorch sees no operators here: norm_rope and norm_rope_qk are autograd functions; what has no derivative is refused where gradients are
+recorded, so are forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a call.
+
 Shapes: rows of heads are [T, H, D] or [B, S, H, D] of any strides, with one position, slot or length for each token or
 sequence.  int32 is the only integer type.  Everything here is checking of shapes and marshalling.
 """
@@ -20,6 +23,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
+from torch.fx import _symbolic_trace
 from torch.utils._python_dispatch import _get_current_dispatch_mode_stack
 
 from . import runtime as R
@@ -96,13 +100,13 @@ def _run(plan, operands, written=()):
     if plan.n:
         if forward_ad._current_level >= 0:
             _no_tangent(operands)
-        if R.active_filters:                                # (tasks of this thread's dispatch filter may still be working on these)
-            for f in _get_current_dispatch_mode_stack():
-                if f in R.active_filters:
-                    f.settle(operands)
+        if _modes() or _symbolic_trace._is_fx_tracing_flag or _jit_tracing():
+            _under_modes(operands)
         words = plan.words[:]
         for word, k in plan.at:
-            words[word] = operands[k].data_ptr()
+            words[word] = at = operands[k].data_ptr()
+            if at == 0:
+                _need(operands[k].numel() == 0, "a tensor without memory (of a trace, say)")
         R.launch_model_at(words.buffer_info()[0], plan.n, plan.device, _stream_of(plan.device))
         for o in written:
             if o is not None and not o.is_inference():
@@ -112,6 +116,20 @@ def _run(plan, operands, written=()):
 def _no_tangent(operands):
     """Inside forward_ad.dual_level: a tangent has no way through a kernel."""
     _need(all(t is None or forward_ad.unpack_dual(t).tangent is None for t in operands), "model operators have no forward-mode derivative")
+
+
+_modes, _jit_tracing, _included = torch._C._len_torch_dispatch_stack, torch._C._is_tracing, torch._C._dispatch_tls_is_dispatch_key_included
+
+
+def _under_modes(operands):
+    """Tasks of this thread's dispatch filter may still be working on these.  A trace (the modes that have a key are those of make_fx and
+    torch.export) would hold the results' allocation, and no kernel."""
+    trace = _jit_tracing() or _included(torch._C.DispatchKey.PreDispatch)
+    for f in _get_current_dispatch_mode_stack():
+        if f in R.active_filters:
+            f.settle(operands)
+        trace = trace or getattr(f, "_mode_key", None) is not None
+    _need(not trace, "model operators cannot be traced: PyTorch does not see their kernels")
 
 
 # the handle of a device's current stream: torch.cuda.current_stream(device).cuda_stream, which makes two objects for it (1.1 us)

@@ -1,6 +1,8 @@
 """Model operators and autograd on the GPU: what they write counts as written, and what would lose a derivative is refused."""
 import pytest
 import torch
+from torch.autograd import forward_ad
+from torch.fx.experimental.proxy_tensor import make_fx
 
 from paper_2604_17861_amd import model as M
 from test_gpu_model import _let_go, cache_of  # noqa: F401
@@ -20,3 +22,16 @@ def test_stored_rows_count_as_written():
             product.sum().backward()
     with pytest.raises(ValueError):
         M.cache_store(x, slots, kc, ks.clone().requires_grad_())
+
+
+def test_traces_and_tangents_are_refused():
+    x = torch.randn(3, 2, 8, device="cuda")
+    want = M.norm_rope(x)
+    for trace in (lambda: make_fx(lambda t: M.norm_rope(t))(x), lambda: make_fx(lambda t: M.norm_rope(t), pre_dispatch=True)(x),
+                  lambda: torch.jit.trace(lambda t: M.norm_rope(t), x, check_trace=False)):
+        with pytest.raises(ValueError, match="traced"):
+            trace()
+    with forward_ad.dual_level():
+        with pytest.raises(ValueError, match="forward-mode"):
+            M.norm_rope(forward_ad.make_dual(x, torch.ones_like(x)))
+    assert torch.equal(M.norm_rope(x), want)

@@ -2,7 +2,10 @@
 one that takes the descriptors and computes nothing."""
 import pytest
 import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
 from torch.autograd import forward_ad
+from torch.fx.experimental.proxy_tensor import make_fx
+from torch.utils._python_dispatch import TorchDispatchMode
 
 from paper_2604_17861_amd import model as M
 from paper_2604_17861_amd import runtime as R
@@ -113,6 +116,7 @@ def test_backward_passes_go_through(launched):
         grad.sum().backward()
 
 
+@pytest.mark.filterwarnings("ignore::DeprecationWarning")
 def test_tangents_of_forward_mode_are_refused(launched):
     x, table, g = torch.randn(3, 2, 8), torch.randn(4, 8), torch.ones(8)
     logits, bias = torch.randn(2, 5), torch.randn(5)
@@ -138,3 +142,74 @@ def test_tangents_of_forward_mode_are_refused(launched):
     for t, call in calls[:-1]:
         call(t)
     assert len(launched) == done + 2 + len(calls) - 1
+
+
+TRACES = {"make_fx": dict(), "fake": dict(tracing_mode="fake"), "symbolic": dict(tracing_mode="symbolic"), "before dispatch": dict(pre_dispatch=True)}
+
+
+@pytest.mark.filterwarnings("ignore")
+@pytest.mark.parametrize("how", [*TRACES, "jit", "export", "fake tensors", "functionalize"])
+@pytest.mark.parametrize("seen", (False, True))
+def test_traces_are_refused(launched, how, seen):
+    """A trace would hold the allocation of the results only."""
+    x, logits = torch.randn(3, 2, 8), torch.randn(2, 5)
+    (kc, ks) = a_cache()
+
+    class One(torch.nn.Module):
+        def __init__(self, f):
+            super().__init__()
+            self.f = f
+
+        def forward(self, t):
+            return self.f(t)
+
+    def trace(f, t):
+        if how in TRACES:
+            return make_fx(f, **TRACES[how])(t)
+        if how == "jit":
+            return torch.jit.trace(f, t, check_trace=False)
+        if how == "export":
+            return torch.export.export(One(f), (t,), strict=False)
+        if how == "functionalize":
+            return torch.func.functionalize(f)(t)
+        with FakeTensorMode():
+            fake = torch.empty(t.shape)
+        return f(fake)
+    calls = [(x, lambda t: M.norm_rope(t)), (x, lambda t: M.norm_rope(t, out=t)), (logits, lambda t: M.penalize_logits(t)),
+             (x, lambda t: M.norm_rope_qk(t, t)[0]), (ks, lambda t: M.cache_load(kc, t, PAGES, None, 3)), (x, lambda t: M.norm_rope_backward(t, t)[0])]
+    for t, call in calls:
+        if seen:
+            call(t)                                          # (its plan is there)
+        done = len(launched)
+        with pytest.raises((ValueError, RuntimeError, AssertionError, TypeError)):      # (fake tensors and symbols by PyTorch itself)
+            trace(call, t)
+        assert len(launched) == done
+        call(t)
+        assert len(launched) == done + 1
+
+
+def test_modes_that_trace_nothing_are_let_through(launched):
+    class Seen(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+    with Seen(), torch.device("cpu"):
+        M.norm_rope(torch.randn(3, 2, 8))
+    assert launched == [1]
+
+
+def test_compiled_programs_call_the_operators(launched):
+    x = torch.randn(3, 2, 8)
+    program = torch.compile(lambda x: M.norm_rope(x * 2.0) + 1.0, backend="eager")
+    for _ in range(3):
+        program(x)
+    assert len(launched) == 3
+    torch._dynamo.reset()
+
+
+def test_a_tensor_whose_memory_was_let_go_is_refused(launched):
+    x, g = torch.randn(3, 2, 8), torch.ones(8)
+    M.norm_rope(x, g)
+    g.untyped_storage().resize_(0)
+    with pytest.raises(ValueError, match="without memory"):
+        M.norm_rope(x, g)
+    assert launched == [1]
