@@ -450,7 +450,10 @@ def _load(caches, scales, pages, lengths, length, dtype, outs):
         for c in caches:
             _check(c, "cache", _CACHE, (4,))
         _check(pages, "pages", _INT, (2,), None, caches[0].device)
-    given, outs = outs, [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype) if o is None else o for c, o in zip(caches, outs)]
+        for c, o in zip(caches, outs):
+            if o is not None:
+                _check(o, "out", _FLOAT if dtype is None else (dtype,), None, (pages.shape[0], length, *c.shape[2:]), c.device)
+    given, outs = outs, [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype or torch.float32) if o is None else o for c, o in zip(caches, outs)]
     operands = [(c, s, pages, lengths, o) for c, s, o in zip(caches, scales, outs)]
     if plan is None:
         plan = _keep(key, _Plan(outs, [cache_load_task(*o) for o in operands], operands))
@@ -458,13 +461,13 @@ def _load(caches, scales, pages, lengths, length, dtype, outs):
     return tuple(outs)
 
 
-def cache_load(cache, scales, pages, lengths, length, *, dtype=torch.float32, out=None):
-    """The first lengths[b] rows (None: all `length`) of every sequence b, through pages [B, width], as [B, length, H, D];
-    zeros behind them.  Not differentiable: scales that require a gradient are refused where gradients are recorded."""
+def cache_load(cache, scales, pages, lengths, length, *, dtype=None, out=None):
+    """The first lengths[b] rows (None: all `length`) of every sequence b, through pages [B, width], as [B, length, H, D] of dtype
+    (None: out's, without one float32); zeros behind them.  Not differentiable: scales that require a gradient are refused where gradients are recorded."""
     return _load((cache,), (scales,), pages, lengths, length, dtype, (out,))[0]
 
 
-def cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, length, *, dtype=torch.float32, out=(None, None)):
+def cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, length, *, dtype=None, out=(None, None)):
     """cache_load of keys and values in one launch: (k, v)."""
     return _load((k_cache, v_cache), (k_scales, v_scales), pages, lengths, length, dtype, out)
 
