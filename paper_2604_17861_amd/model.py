@@ -338,6 +338,8 @@ def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
     eps, pairs = float(eps), bool(pairs)                    # (a key holds values, not objects)
     key = ("norm_rope", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in outs])
     plan = _plans.get(key)
+    if plan is None:
+        _need(len(outs) == len(xs), "out has %d entries (None: made here)", len(xs))
     given, outs = outs, [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
     operands = [(x, g, table, positions, o) for x, g, o in zip(xs, gammas, outs)]
     if plan is None:
@@ -447,6 +449,7 @@ def _load(caches, scales, pages, lengths, length, dtype, outs):
     key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
     plan = _plans.get(key)
     if plan is None:
+        _need(len(outs) == len(caches), "out has %d entries (None: made here)", len(caches))
         for c in caches:
             _check(c, "cache", _CACHE, (4,))
         _check(pages, "pages", _INT, (2,), None, caches[0].device)

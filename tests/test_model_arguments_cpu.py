@@ -27,3 +27,18 @@ def test_an_output_has_the_length_and_the_dtype_that_are_named(launched, seen):
     assert k.dtype == torch.float32 and v is fits
     assert M.cache_load(kc, ks, PAGES, None, 3).dtype == torch.float32 and M.cache_load(kc, ks, PAGES, None, 3, dtype=torch.bfloat16).dtype == torch.bfloat16
     assert len(launched) == done + 5
+
+
+def test_two_results_have_two_outputs(launched):
+    """One short, the second tensor was left out of the launch; one over, it was ignored."""
+    x, o = torch.randn(3, 2, 8), torch.zeros(3, 2, 8)
+    (kc, ks), (vc, vs) = a_cache(), a_cache()
+    rows = torch.zeros(1, 3, 2, 8)
+    for n in (0, 1, 3):
+        for call in (lambda: M.norm_rope_qk(x, x, out=(o,) * n), lambda: M.cache_load_kv(kc, ks, vc, vs, PAGES, None, 3, out=(rows,) * n)):
+            with pytest.raises(ValueError, match="2 entries"):
+                call()
+    assert not launched
+    M.norm_rope_qk(x, x, out=(o, None))
+    M.cache_load_kv(kc, ks, vc, vs, PAGES, None, 3, out=[rows, torch.zeros(1, 3, 2, 8)])
+    assert launched == [2, 2]
