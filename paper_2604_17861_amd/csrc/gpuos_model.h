@@ -198,6 +198,7 @@ class ModelPack {
 
  private:
   static constexpr int64_t kMost = 2147483647LL;     // rows, and elements of one dim
+  static constexpr int64_t kExtent = 1LL << 46;      // elements from an operand's first to its last
   static uint32_t size_of(uint32_t dt) { return dt >= GPUOS_I8 ? 1u : (dt == GPUOS_F32 || dt == GPUOS_I32 ? 4u : 2u); }
   static bool is_float(uint32_t dt) { return dt <= GPUOS_BF16; }
 
@@ -213,8 +214,10 @@ class ModelPack {
       if (s < 0 || s > 0xffffffffLL) return false;
       if (out && s == 0 && size[d] > 1 && !empty) return false;
       if (dense && d == nd - 1 && s != 1 && size[d] > 1) return false;
-      if (size[d] > 1) extent += (size[d] - 1) * s;          // (under 2^63 each; and all together, by the next line)
-      if (extent > (1LL << 46)) return false;
+      if (size[d] > 1) {
+        if (s > (kExtent - extent) / (size[d] - 1)) return false;      // (compared before it is added: one dim's part may be close to 2^63)
+        extent += (size[d] - 1) * s;
+      }
       st[d] = size[d] > 1 ? (uint32_t)s : 0u;
     }
     return true;
