@@ -345,7 +345,7 @@ class ModelPack {
     if (!sizes(t, 2)) return GPUOS_E_INVAL;
     const gpuos_model_operand &part = t.operand[0], &out = t.operand[1];
     uint32_t cs[2];
-    if (!part.ptr || !out.ptr || part.dtype != GPUOS_F32 || !is_float(out.dtype)) return GPUOS_E_INVAL;
+    if ((!part.ptr && t.size[1] != 0) || !out.ptr || part.dtype != GPUOS_F32 || !is_float(out.dtype)) return GPUOS_E_INVAL;
     if (!operand(part, 2, t.size, false, true, cs) || !operand(out, 1, t.size, true, false, r.os)) return GPUOS_E_INVAL;
     r.partial = (uint64_t)part.ptr;
     r.out = (uint64_t)out.ptr;

@@ -5,7 +5,7 @@ from torch.autograd import forward_ad
 from torch.fx.experimental.proxy_tensor import make_fx
 
 from paper_2604_17861_amd import model as M
-from test_gpu_model import _let_go, cache_of  # noqa: F401
+from test_gpu_model import ROUTES, _let_go, cache_of, run, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,11 @@ def test_traces_and_tangents_are_refused():
         with pytest.raises(ValueError, match="forward-mode"):
             M.norm_rope(forward_ad.make_dual(x, torch.ones_like(x)))
     assert torch.equal(M.norm_rope(x), want)
+
+
+@pytest.mark.parametrize("route", ROUTES)
+def test_the_sums_of_no_shares_are_zeros(route):
+    partial = up(torch.empty(70, 0))
+    out = torch.full((70,), 7.0, device="cuda")
+    run(route, M.gamma_sum_task(partial, out))
+    assert (out == 0).all()

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2604_17861_amd import runtime as R
-from test_model_cpu import BF16, F32, NO, op, penalty, rope
+from test_model_cpu import BF16, F32, NO, op, penalty, plan, rope
 
 MOST, STRIDE = 2 ** 31 - 1, 2 ** 32 - 1
 
@@ -22,3 +22,10 @@ def test_rows_as_far_apart_as_strides_go(sizes):
     b, s, h, d = sizes
     x = op(BF16, STRIDE, STRIDE, STRIDE, STRIDE)
     assert rope(b=b, s=s, h=h, d=d, r=0, table=NO, positions=NO, gamma=NO, x=x, out=x) == R.E_INVAL
+
+
+def test_a_sum_of_no_shares_needs_no_memory_for_them():
+    """A tensor without elements has no address."""
+    none = lambda parts, **kw: plan("GAMMA_SUM", (64, parts), (op(F32, parts, 1, ptr=0), op(BF16, 1, **kw)))
+    assert all(p["chunks"] >= 1 and p["vectors"] == 0 for p in none(0))
+    assert none(1) == R.E_INVAL and none(0, ptr=0) == R.E_INVAL
