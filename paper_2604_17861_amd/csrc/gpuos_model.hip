@@ -14,10 +14,13 @@ namespace gpuos {
 constexpr uint32_t model_lds(uint32_t v) { return v < MV_GRAD ? 1u : (v < MV_SUM ? 2048u : (v == MV_SUM ? 4u : (v < MV_PENALTY ? 1u : ModelPack::kSegment))); }
 constexpr uint32_t model_threads(uint32_t v) { return v < MV_PENALTY ? kThreads : kPenaltyThreads; }
 
-// Wavefronts of a SIMD that the compiler has to leave room for: those of the penalties need more scalar registers than eight may have, and 64 rows
-// of 100,352 in segments of eight wavefronts are 1,600 workgroups, of which the card takes 768 at once so, and 1,024 with some of them in
-// lanes: 10.6 and 10.2 us.  Rotations, 16 times a card's worth, are slower for it: 36.4 and 38.4.
-constexpr uint32_t model_waves(uint32_t v) { return v >= MV_PENALTY && v < MV_PENALTY + 3 ? 8u : 1u; }
+// Wavefronts of a SIMD that the compiler has to leave room for.  A worker of three workgroups a compute unit, the default, leaves a quarter of every
+// register file, 128 of 512 registers: a block has to fit there, or it waits until the worker leaves, which it may never do.  A block of 256
+// threads is one wavefront a SIMD, of 512 two; so four and eight.  (Unbounded, the gradient element by element took 133.)
+// The penalties gain from it besides: they need more scalar registers than eight may have, and 64 rows of 100,352 in segments of eight
+// wavefronts are 1,600 workgroups, of which the card takes 768 at once so, and 1,024 with some of them in lanes: 10.6 and 10.2 us.
+// Rotations, 16 times a card's worth, are slower with eight: 36.4 and 38.4.
+constexpr uint32_t model_waves(uint32_t v) { return 4u * model_threads(v) / kThreads; }
 
 template <uint32_t V> __global__ void __launch_bounds__(model_threads(V), model_waves(V)) gpuos_model_kernel(ModelLaunch) {
   __shared__ alignas(16) float s[model_lds(V)];

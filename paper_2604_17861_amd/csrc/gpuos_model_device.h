@@ -439,10 +439,15 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
 #pragma unroll
       for (int k = 0; k < K; ++k) { oa[k] = r * __builtin_fmaf(-xa[k], m, oa[k]); ob[k] = r * __builtin_fmaf(-xb[k], m, ob[k]); }
     }
+    // (The gradient's offsets in the output are made again for every row: kept in registers over the loop, like those of its inputs, it
+    // takes 133, and so 117, which is room for a block beside a worker's three and for a fourth on every unit: 262,144 heads of 128 bf16 and
+    // a gradient of strides of 0 312 and 202 us.)
+    uint32_t os = a.os[3];
+    if (GRAD) asm volatile("" : "+s"(os));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (in && in_a[k]) M::st_rt(op + (uint64_t)ja[k] * a.os[3] * eo, a.dtype[1], oa[k]);
-      if (in && in_b[k]) M::st_rt(op + (uint64_t)jb[k] * a.os[3] * eo, a.dtype[1], ob[k]);
+      if (in && in_a[k]) M::st_rt(op + (uint64_t)ja[k] * os * eo, a.dtype[1], oa[k]);
+      if (in && in_b[k]) M::st_rt(op + (uint64_t)jb[k] * os * eo, a.dtype[1], ob[k]);
     }
   }
   if (GRAD && a.partial != 0) {
