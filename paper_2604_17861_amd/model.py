@@ -330,6 +330,7 @@ class _NormRope(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, *douts):
         table, positions, *xs = ctx.saved_tensors
+        douts = [d.resolve_neg() for d in douts]            # (of a conjugate's imaginary part)
         dxs, dgs = _norm_rope_backward(douts, xs[0::2], xs[1::2], table, positions, ctx.eps, ctx.pairs)
         return (None, None, None, None, *(g for pair in zip(dxs, dgs) for g in pair))
 

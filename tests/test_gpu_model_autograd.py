@@ -43,3 +43,16 @@ def test_the_sums_of_no_shares_are_zeros(route):
     out = torch.full((70,), 7.0, device="cuda")
     run(route, M.gamma_sum_task(partial, out))
     assert (out == 0).all()
+
+
+def test_a_gradient_through_complex_numbers():
+    """The loss is that of the imaginary part alone, whose gradient comes back lazily negated."""
+    x, zero = torch.randn(30, 2, 64, device="cuda"), torch.zeros(30, 2, 64, device="cuda")
+    grads = []
+    for loss in (lambda z: torch.complex(zero, z).conj().abs().sum(), lambda z: z.abs().sum()):
+        leaf = x.clone().requires_grad_()
+        loss(M.norm_rope(leaf, eps=0.1)).backward()
+        grads.append(leaf.grad)
+    # The gradients at z are 1 or -1 either way, off by two half steps (of |z| and z / |z|).  dx = r (u - x r^2 mean(u x)) has terms of
+    # r (1 + |x| r mean(|x| r)) <= 10 ** 0.5 * (1 + 64 ** 0.5) < 29, and 56 roundings of them in either run.
+    torch.testing.assert_close(grads[0], grads[1], rtol=0, atol=(2 + 2 * 56) * 29 * 2.0 ** -24)

@@ -213,3 +213,10 @@ def test_a_tensor_whose_memory_was_let_go_is_refused(launched):
     with pytest.raises(ValueError, match="without memory"):
         M.norm_rope(x, g)
     assert launched == [1]
+
+
+def test_gradients_that_are_lazily_negated_go_through(launched):
+    """What autograd hands back through the imaginary part of a conjugate."""
+    x = torch.randn(3, 2, 8, requires_grad=True)
+    torch.complex(torch.zeros(3, 2, 8), M.norm_rope(x)).conj().abs().sum().backward()
+    assert launched == [1, 1] and x.grad is not None
