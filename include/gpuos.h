@@ -287,7 +287,7 @@ typedef struct gpuos_task {
 #define GPUOS_FLAG_PAIRS 4u         /* NORM_ROPE, NORM_ROPE_GRAD: neighbours are pairs      */
 #define GPUOS_MAX_OPERANDS 8
 typedef struct gpuos_model_operand {
-  void*   ptr;                      /* device address, a multiple of the element size; NULL: left out */
+  void*   ptr;                      /* device address, a multiple of the element size; NULL: left out, or no elements */
   int64_t stride[4];                /* in elements                                      */
   uint8_t dtype;                    /* enum gpuos_dtype                                 */
   uint8_t reserved[7];

@@ -202,6 +202,7 @@ class ModelPack {
   static uint32_t size_of(uint32_t dt) { return dt >= GPUOS_I8 ? 1u : (dt == GPUOS_F32 || dt == GPUOS_I32 ? 4u : 2u); }
   static bool is_float(uint32_t dt) { return dt <= GPUOS_BF16; }
 
+  // (What has no elements may have no address: a task without rows, a cache without pages.)
   // An operand of nd dims: its strides (0 where the dim has one element), or false.  `out`: no two elements share memory as far as
   // strides of 0 go; `dense`: the last dim's stride is 1.
   static bool operand(const gpuos_model_operand& o, int nd, const int64_t* size, bool out, bool dense, uint32_t* st) {
@@ -288,7 +289,8 @@ class ModelPack {
     const gpuos_model_operand *x = &t.operand[0], *gamma = &t.operand[1], *table = &t.operand[2], *pos = &t.operand[3], *out = &t.operand[4];
     const gpuos_model_operand *dz = &t.operand[grad ? 5 : 0], *part = grad ? &t.operand[6] : nullptr;
     const int64_t xz[4] = {z[0], z[1], z[2], d}, gz[1] = {d}, tz[2] = {places, rot};
-    if (!x->ptr || !out->ptr || !dz->ptr || !is_float(x->dtype) || !is_float(out->dtype) || !is_float(dz->dtype)) return GPUOS_E_INVAL;
+    const bool rows = tokens * z[2] != 0;
+    if ((rows && (!x->ptr || !out->ptr || !dz->ptr)) || !is_float(x->dtype) || !is_float(out->dtype) || !is_float(dz->dtype)) return GPUOS_E_INVAL;
     if (!operand(*x, 4, xz, false, false, r.xs) || !operand(*out, 4, xz, true, false, r.os) || !operand(*dz, 4, xz, false, false, r.zs)) return GPUOS_E_INVAL;
     if (gamma->ptr && (!is_float(gamma->dtype) || !operand(*gamma, 1, gz, false, false, &r.gs))) return GPUOS_E_INVAL;
     uint32_t ts[2] = {0, 0};
@@ -345,7 +347,7 @@ class ModelPack {
     if (!sizes(t, 2)) return GPUOS_E_INVAL;
     const gpuos_model_operand &part = t.operand[0], &out = t.operand[1];
     uint32_t cs[2];
-    if ((!part.ptr && t.size[1] != 0) || !out.ptr || part.dtype != GPUOS_F32 || !is_float(out.dtype)) return GPUOS_E_INVAL;
+    if ((!part.ptr && t.size[1] != 0 && t.size[0] != 0) || (!out.ptr && t.size[0] != 0) || part.dtype != GPUOS_F32 || !is_float(out.dtype)) return GPUOS_E_INVAL;
     if (!operand(part, 2, t.size, false, true, cs) || !operand(out, 1, t.size, true, false, r.os)) return GPUOS_E_INVAL;
     r.partial = (uint64_t)part.ptr;
     r.out = (uint64_t)out.ptr;
@@ -371,7 +373,8 @@ class ModelPack {
     const int64_t xz[4] = {z[0], z[1], z[2], d}, cz[4] = {pages, page, z[2], d}, sz[4] = {pages, page, z[2], groups};
     const int64_t pz[2] = {z[0], store ? z[1] : z[7]};
     uint32_t cs[4];
-    if (!x.ptr || !cache.ptr || !scales.ptr || !slots.ptr || !is_float(x.dtype) || cache.dtype < GPUOS_I8 || scales.dtype != GPUOS_F32 || slots.dtype != GPUOS_I32)
+    const bool rows = tokens * z[2] != 0;
+    if ((rows && (!x.ptr || !slots.ptr || (pages != 0 && (!cache.ptr || !scales.ptr)))) || !is_float(x.dtype) || cache.dtype < GPUOS_I8 || scales.dtype != GPUOS_F32 || slots.dtype != GPUOS_I32)
       return GPUOS_E_INVAL;
     if (!operand(x, 4, xz, !store, false, r.xs) || !operand(cache, 4, cz, store, true, cs) || !operand(scales, 4, sz, store, false, r.ss) ||
         !operand(slots, 2, pz, false, false, r.ps))
@@ -408,9 +411,10 @@ class ModelPack {
     const gpuos_model_operand &x = t.operand[0], &out = t.operand[1], &hist = t.operand[2], &prompt = t.operand[3], &params = t.operand[4],
                               &bias = t.operand[5], &allowed = t.operand[6];
     const int64_t xz[2] = {b, v}, hz[2] = {b, n}, pz[2] = {b, 3}, az[2] = {b, (v + 31) / 32};
-    if (!x.ptr || !out.ptr || !is_float(x.dtype) || !is_float(out.dtype) || !operand(x, 2, xz, false, false, r.xs) || !operand(out, 2, xz, true, false, r.os))
+    const bool rows = b * v != 0;
+    if ((rows && (!x.ptr || !out.ptr)) || !is_float(x.dtype) || !is_float(out.dtype) || !operand(x, 2, xz, false, false, r.xs) || !operand(out, 2, xz, true, false, r.os))
       return GPUOS_E_INVAL;
-    if ((hist.ptr == nullptr) != (params.ptr == nullptr) || (!hist.ptr && (n != 0 || prompt.ptr))) return GPUOS_E_INVAL;
+    if (rows && ((hist.ptr == nullptr) != (params.ptr == nullptr) || (!hist.ptr && (n != 0 || prompt.ptr)))) return GPUOS_E_INVAL;
     if (hist.ptr && (hist.dtype != GPUOS_I32 || params.dtype != GPUOS_F32 || !operand(hist, 2, hz, false, false, r.hs) || !operand(params, 2, pz, false, false, r.ms)))
       return GPUOS_E_INVAL;
     if (prompt.ptr && (prompt.dtype != GPUOS_I32 || !operand(prompt, 1, xz, false, false, &r.ps))) return GPUOS_E_INVAL;

@@ -1,4 +1,5 @@
-"""Model operators and autograd on the GPU: what they write counts as written, and what would lose a derivative is refused."""
+"""Model operators on the GPU round their arithmetic: what they write counts as written for autograd, what would lose a derivative is refused,
+tensors without elements are nothing to do."""
 import pytest
 import torch
 from torch.autograd import forward_ad
@@ -56,3 +57,21 @@ def test_a_gradient_through_complex_numbers():
     # The gradients at z are 1 or -1 either way, off by two half steps (of |z| and z / |z|).  dx = r (u - x r^2 mean(u x)) has terms of
     # r (1 + |x| r mean(|x| r)) <= 10 ** 0.5 * (1 + 64 ** 0.5) < 29, and 56 roundings of them in either run.
     torch.testing.assert_close(grads[0], grads[1], rtol=0, atol=(2 + 2 * 56) * 29 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("route", ROUTES)
+def test_empty_tensors_in_descriptors(route):
+    e, x, out = up(torch.empty(0, 2, 64)), up(torch.randn(5, 2, 64)), up(torch.zeros(5, 2, 64))
+    none, some = up(torch.empty(0, dtype=torch.int32)), up(torch.zeros(3, 2, dtype=torch.int32))
+    cache, scales = up(torch.empty(0, 4, 2, 64, dtype=torch.int8)), up(torch.empty(0, 4, 2, 1))
+    back = up(torch.zeros(3, 7, 2, 64))
+    lengths = up(torch.tensor([7, 0, 3], dtype=torch.int32))
+    run(route, M.norm_rope_task(e, None, None, None, e), M.norm_rope_task(x, None, None, None, out), M.cache_store_task(e, none, cache, scales),
+        M.penalty_task(up(torch.empty(0, 9)), up(torch.empty(0, 9))),
+        # a cache without pages: nothing is stored, and what is read back is in no page
+        M.cache_store_task(x, up(torch.arange(5, dtype=torch.int32)), cache, scales), M.cache_load_task(cache, scales, some, lengths, back))
+    assert torch.equal(out, M.norm_rope(x))
+    for b, n in enumerate((7, 0, 3)):
+        assert torch.isnan(back[b, :n]).all() and (back[b, n:] == 0).all()
+    M.cache_store(x, up(torch.arange(5, dtype=torch.int32)), cache, scales)
+    assert torch.isnan(M.cache_load(cache, scales, some, None, 7)).all()

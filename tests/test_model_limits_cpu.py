@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2604_17861_amd import runtime as R
-from test_model_cpu import BF16, F32, NO, op, penalty, plan, rope
+from test_model_cpu import BF16, F16, F32, I8, I32, NO, grad, load, op, penalty, plan, rope, store
 
 MOST, STRIDE = 2 ** 31 - 1, 2 ** 32 - 1
 
@@ -29,3 +29,22 @@ def test_a_sum_of_no_shares_needs_no_memory_for_them():
     none = lambda parts, **kw: plan("GAMMA_SUM", (64, parts), (op(F32, parts, 1, ptr=0), op(BF16, 1, **kw)))
     assert all(p["chunks"] >= 1 and p["vectors"] == 0 for p in none(0))
     assert none(1) == R.E_INVAL and none(0, ptr=0) == R.E_INVAL
+
+
+def test_what_has_no_elements_needs_no_address():
+    """Tasks without rows, and caches without pages, as empty tensors describe them."""
+    at = lambda dtype, *stride: op(dtype, *stride, ptr=0)
+    rows = at(BF16, 768, 256, 64, 1)
+    empty = [plans for n in (dict(b=0), dict(s=0), dict(h=0)) for plans in (
+        rope(x=rows, out=rows, positions=NO, **n), grad(x=rows, dx=rows, dout=rows, partial=NO, positions=NO, **n))]
+    empty += [store(s=0, x=at(BF16, 256, 128, 64, 1), slots=at(I32, 1, 1)), load(b=0, table=at(I32, 2, 1), lengths=NO, out=at(F16, 3840, 128, 64, 1)), load(l=0, out=at(F16, 128, 128, 64, 1)),
+              store(h=0, x=at(BF16, 64, 64, 64, 1), cache=at(I8, 64, 64, 64, 1), scales=at(F32, 1, 1, 1, 1)),
+              penalty(b=0, x=at(F32, 1000, 1), out=at(F32, 1000, 1), history=NO, prompts=NO, params=NO), penalty(v=0, x=at(F32, 1, 1), out=at(F32, 1, 1)),
+              plan("GAMMA_SUM", (0, 5), (at(F32, 5, 1), at(BF16, 1)))]
+    assert all(p["vectors"] == 2 and p["chunks"] == 1 for plans in empty for p in plans)
+    none = dict(pages=0, cache=at(I8, 2048, 128, 64, 1), scales=at(F32, 32, 2, 1, 1))
+    assert isinstance(store(**none), tuple) and isinstance(load(**none), tuple)
+    # with elements they do
+    for bad in (store(cache=at(I8, 2048, 128, 64, 1)), load(scales=at(F32, 32, 2, 1, 1)), load(pages=0, table=NO, **{k: none[k] for k in ("cache", "scales")}),
+                store(pages=0, x=NO), load(pages=0, out=NO), rope(x=rows), rope(out=rows), penalty(x=at(F32, 1000, 1))):
+        assert bad == R.E_INVAL
