@@ -101,24 +101,6 @@ template <int POL> struct Glob {
       for (int k = 0; k < 8; ++k) f[k] = Elem<DT>::get(q, k);
     }
   }
-  template <int DT> static DEV void st4e(uint64_t p, const float* f) {
-    v4i q = {0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) Elem<DT>::put(q, k, f[k]);
-    if (Elem<DT>::ES == 4) st16(p, q);
-    else st8(p, v2i{q[0], q[1]});
-  }
-  template <int DT> static DEV void st8e(uint64_t p, const float* f) {
-    if (Elem<DT>::ES == 4) {
-      st4e<DT>(p, f);
-      st4e<DT>(p + 16, f + 4);
-    } else {
-      v4i q = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) Elem<DT>::put(q, k, f[k]);
-      st16(p, q);
-    }
-  }
 };
 DEV uint32_t float_size(uint32_t dt) { return dt == GPUOS_F32 ? 4u : 2u; }
 DEV uint32_t ceil_log2(uint32_t n) { return n <= 1 ? 0u : 32u - (uint32_t)__builtin_clz(n - 1); }
@@ -460,7 +442,7 @@ DEV void rope_elements(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid
   }
 }
 
-// GAMMA_SUM: the workgroup a row of the partial sums (4 KB at most), always in the same order.
+// GAMMA_SUM: the workgroup a row of the partial sums (of any length; 4 KB at most as NORM_ROPE_GRAD makes them), always in the same order.
 template <int POL> DEV void gamma_sum(const RopeArgs& a, uint32_t chunk, float* s, uint32_t tid) {
   typedef Glob<POL> M;
   for (uint32_t row = chunk; row < a.items; row += a.chunks) {
