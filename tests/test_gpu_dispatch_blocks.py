@@ -1,8 +1,11 @@
 """The dispatch filter and kernels that are launched between its blocks."""
+import threading
+
 import pytest
 import torch
 
 from paper_2604_17861_amd import model as M
+from paper_2604_17861_amd import runtime as R
 from paper_2604_17861_amd.dispatch import GpuosMode
 
 pytestmark = pytest.mark.gpu
@@ -44,5 +47,22 @@ def test_a_block_that_begins_behind_a_kernel_in_flight_reads_its_result(launch):
                 y = torch.relu(last)
             assert torch.equal(y.cpu(), want)
         assert mode.stats["redirected"] == 6, mode.stats
+    finally:
+        mode.close()
+
+
+def test_a_call_from_another_thread_passes_a_filter_by_and_ends():
+    x = torch.randn(40, 4, 64, device="cuda")
+    want = M.norm_rope(x)
+    torch.cuda.synchronize()
+    mode, got = GpuosMode(idle_exit_ms=50), []
+    try:
+        with mode:
+            other = threading.Thread(target=lambda: got.append(M.norm_rope(x)))
+            other.start()
+            other.join(60)
+            assert not other.is_alive() and len(got) == 1 and mode in R.active_filters
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want)
     finally:
         mode.close()
