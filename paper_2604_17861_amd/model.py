@@ -18,11 +18,11 @@ sequence.  int32 is the only integer type.  Everything here is checking of shape
 """
 import struct
 from array import array
+from itertools import chain, repeat
 
 import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
-from torch.autograd.graph import increment_version
 from torch.fx import _symbolic_trace
 from torch.utils._python_dispatch import _get_current_dispatch_mode_stack
 
@@ -68,23 +68,26 @@ def _sig(t):
 
 class _Plan:
     """The descriptors of one or more tasks, without those that have nothing to do (an empty tensor has no address).
-    rows: what tells which those are; operands: of every task, in the descriptor's order (None: left out)."""
+    rows: what tells which those are; operands: of every task, in the descriptor's order (None: left out); places: where each of them is in what
+    _run is given (None: all tasks' operands, one after the other)."""
     __slots__ = ("words", "n", "device", "at")
 
-    def __init__(self, rows, tasks, operands):
+    def __init__(self, rows, tasks, operands, places=None):
         tasks = [t for x, t in zip(rows, tasks) if x.numel() != 0]
         self.words = array("Q", b"".join(tasks))
         self.n, self.device = len(tasks), rows[0].get_device()
         _need(all(x.get_device() == self.device for x in rows), "the tensors of one call are on one device")
-        self.at = []                                        # (word, which of all the operands)
-        first, place = 0, 0
-        for x, mine in zip(rows, operands):
+        if places is None:
+            count = iter(range(8 * len(operands)))
+            places = [[next(count) for _ in mine] for mine in operands]
+        self.at = []                                        # (word, which of what _run is given)
+        first = 0
+        for x, mine, at in zip(rows, operands, places):
             if x.numel() != 0:
                 for o in range(8):
                     self.words[first + _POINTER + 6 * o] = 0
-                self.at += [(first + _POINTER + 6 * o, place + o) for o, t in enumerate(mine) if t is not None]
+                self.at += [(first + _POINTER + 6 * o, at[o]) for o, t in enumerate(mine) if t is not None]
                 first += _WORDS
-            place += len(mine)
 
 
 def _keep(key, plan):
@@ -95,8 +98,8 @@ def _keep(key, plan):
 
 
 def _run(plan, operands, written=()):
-    """Launch with these addresses: the operands of all tasks, one after the other.  written: tensors of the caller's among
-    them (None: left out) that the call writes; what autograd has saved of those is no longer what it was."""
+    """Launch with these addresses: the operands of all tasks, one after the other (or as the plan's `places` say).  written: tensors of the caller's among
+    them that the call writes; what autograd has saved of those is no longer what it was."""
     if plan.n:
         if forward_ad._current_level >= 0:
             _no_tangent(operands)
@@ -105,12 +108,14 @@ def _run(plan, operands, written=()):
         words = plan.words[:]
         for word, k in plan.at:
             words[word] = at = operands[k].data_ptr()
-            if at == 0:
+            if not at:
                 _need(operands[k].numel() == 0, "a tensor without memory (of a trace, say)")
         R.launch_model_at(words.buffer_info()[0], plan.n, plan.device, _stream_of(plan.device))
-        for o in written:
-            if o is not None and not o.is_inference():
-                increment_version(o)
+        if written:
+            try:
+                torch._C._increment_version(written)        # (torch.autograd.graph.increment_version, 0.4 us less)
+            except RuntimeError:                            # tensors of inference mode have no versions
+                torch._C._increment_version([o for o in written if not o.is_inference()])
 
 
 def _no_tangent(operands):
@@ -337,21 +342,21 @@ class _NormRope(torch.autograd.Function):
 
 def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):
     eps, pairs = float(eps), bool(pairs)                    # (a key holds values, not objects)
-    key = ("norm_rope", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in outs])
+    key = ("norm_rope", eps, pairs, *map(_sig, (table, positions, *xs, *gammas, *outs)))
     plan = _plans.get(key)
     if plan is None:
         _need(len(outs) == len(xs), "out has %d entries (None: made here)", len(xs))
-    given, outs = outs, [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
-    operands = [(x, g, table, positions, o) for x, g, o in zip(xs, gammas, outs)]
+    given, outs = [o for o in outs if o is not None], [_empty_like(x) if o is None else o for x, o in zip(xs, outs)]
+    operands = list(zip(xs, gammas, repeat(table), repeat(positions), outs))
     if plan is None:
         plan = _keep(key, _Plan(xs, [norm_rope_task(*o, eps=eps, pairs=pairs) for o in operands], operands))
-    _run(plan, sum(operands, ()), given)
+    _run(plan, list(chain.from_iterable(operands)), given)
     return tuple(outs)
 
 
 def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
     eps, pairs = float(eps), bool(pairs)
-    key = ("backward", eps, pairs, _sig(table), _sig(positions), *[_sig(t) for t in xs], *[_sig(t) for t in gammas], *[_sig(t) for t in douts])
+    key = ("backward", eps, pairs, *map(_sig, (table, positions, *xs, *gammas, *douts)))
     plan = _plans.get(key)
     dxs, dgs, grads, sums = [], [], [], []
     for dout, x, gamma in zip(douts, xs, gammas):
@@ -368,12 +373,17 @@ def _norm_rope_backward(douts, xs, gammas, table, positions, eps, pairs):
     if plan is None:                                        # (a sum is another operator than what it adds up, so a launch behind it)
         tasks = [norm_rope_grad_task(o[5], *o[:5], o[6], eps=eps, pairs=pairs) for o in grads] + [gamma_sum_task(*o) for o in sums]
         plan = _keep(key, _Plan([o[0] for o in grads + sums], tasks, grads + sums))
-    _run(plan, sum(grads + sums, ()))
+    _run(plan, list(chain.from_iterable(grads + sums)))
     return dxs, dgs
 
 
 def _differentiable(xs, outs):
-    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in xs):
+    if not torch.is_grad_enabled():
+        return False
+    for t in xs:
+        if t is not None and t.requires_grad:
+            break
+    else:
         return False
     _need(all(o is None for o in outs), "out does not go with gradients")
     if forward_ad._current_level >= 0:                      # (the function itself is given them without their tangents)
@@ -383,7 +393,9 @@ def _differentiable(xs, outs):
 
 def _no_gradient(what, *xs):
     if torch.is_grad_enabled():
-        _need(not any(t is not None and t.requires_grad for t in xs), "%s has no gradient here", what)
+        for t in xs:
+            if t is not None and t.requires_grad:
+                raise ValueError("%s has no gradient here" % what)
 
 
 def norm_rope(x, gamma=None, table=None, positions=None, *, eps=1e-6, pairs=False, out=None):
@@ -424,12 +436,13 @@ def norm_rope_qk_backward(dq, dk, q, k, gamma_q=None, gamma_k=None, table=None, 
 
 def _store(xs, slots, caches, scales):
     _no_gradient("cache_store", *xs, *scales)
-    key = ("store", _sig(slots), *[_sig(t) for t in xs], *[_sig(t) for t in caches], *[_sig(t) for t in scales])
-    plan = _plans.get(key)
-    operands = [(x, slots, c, s) for x, c, s in zip(xs, caches, scales)]
+    given = (slots, *xs, *caches, *scales)
+    key = ("store", *map(_sig, given))
+    plan, n = _plans.get(key), len(xs)
     if plan is None:
-        plan = _keep(key, _Plan(xs, [cache_store_task(*o) for o in operands], operands))
-    _run(plan, sum(operands, ()), (*caches, *scales))
+        operands = list(zip(xs, repeat(slots), caches, scales))
+        plan = _keep(key, _Plan(xs, [cache_store_task(*o) for o in operands], operands, [(1 + i, 0, 1 + n + i, 1 + 2 * n + i) for i in range(n)]))
+    _run(plan, given, given[1 + n:])
 
 
 def cache_store(x, slots, cache, scales):
@@ -447,21 +460,23 @@ def cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales):
 def _load(caches, scales, pages, lengths, length, dtype, outs):
     length = int(length)
     _no_gradient("cache_load", *scales, *outs)
-    key = ("load", length, dtype, _sig(pages), _sig(lengths), *[_sig(t) for t in caches], *[_sig(t) for t in scales], *[_sig(t) for t in outs])
-    plan = _plans.get(key)
+    given = (pages, lengths, *caches, *scales)
+    key = ("load", length, dtype, *map(_sig, (*given, *outs)))
+    plan, n = _plans.get(key), len(caches)
     if plan is None:
-        _need(len(outs) == len(caches), "out has %d entries (None: made here)", len(caches))
+        _need(len(outs) == n, "out has %d entries (None: made here)", n)
         for c in caches:
             _check(c, "cache", _CACHE, (4,))
         _check(pages, "pages", _INT, (2,), None, caches[0].device)
         for c, o in zip(caches, outs):
             if o is not None:
                 _check(o, "out", _FLOAT if dtype is None else (dtype,), None, (pages.shape[0], length, *c.shape[2:]), c.device)
-    given, outs = outs, [c.new_empty((pages.shape[0], length, c.shape[2], c.shape[3]), dtype=dtype or torch.float32) if o is None else o for c, o in zip(caches, outs)]
-    operands = [(c, s, pages, lengths, o) for c, s, o in zip(caches, scales, outs)]
+    written, rows, dtype = [o for o in outs if o is not None], pages.shape[0], dtype or torch.float32
+    outs = [c.new_empty((rows, length, *c.shape[2:]), dtype=dtype) if o is None else o for c, o in zip(caches, outs)]
     if plan is None:
-        plan = _keep(key, _Plan(outs, [cache_load_task(*o) for o in operands], operands))
-    _run(plan, sum(operands, ()), given)
+        operands = list(zip(caches, scales, repeat(pages), repeat(lengths), outs))
+        plan = _keep(key, _Plan(outs, [cache_load_task(*o) for o in operands], operands, [(2 + i, 2 + n + i, 0, 1, 2 + 2 * n + i) for i in range(n)]))
+    _run(plan, (*given, *outs), written)
     return tuple(outs)
 
 
@@ -483,16 +498,16 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
     repetition penalty only) by params [B, 3] = repetition, frequency, presence; bias; -inf where a bit of allowed is
     not set.  out may be x.  Not differentiable: logits that require a gradient are refused where gradients are recorded."""
     _no_gradient("penalize_logits", x, params, bias, out)
-    key = ("penalty", _sig(x), _sig(history), _sig(prompt_lengths), _sig(params), _sig(bias), _sig(allowed), _sig(out))
+    key = ("penalty", *map(_sig, (x, history, prompt_lengths, params, bias, allowed, out)))
     plan = _plans.get(key)
     if plan is None:
         _check(x, "x", _FLOAT, (2,))
-    given, out = out, _empty_like(x) if out is None else out
+    given, out = () if out is None else (out,), _empty_like(x) if out is None else out
     operands = (x, out, history, prompt_lengths, params, bias, allowed)
     if plan is None:
         task = penalty_task(*operands)
         if history is not None and history.shape[1] == 0:   # (nothing is counted: as without one)
             operands = (x, out, None, None, None, bias, allowed)
         plan = _keep(key, _Plan((x,), (task,), (operands,)))
-    _run(plan, operands, (given,))
+    _run(plan, operands, given)
     return out
