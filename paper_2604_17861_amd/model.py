@@ -11,7 +11,7 @@ launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as ta
 `register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  include/gpuos.h says what every operator computes and takes.
 
 PyTorch sees no operators here: norm_rope and norm_rope_qk are autograd functions; what has no derivative is refused where gradients are
-recorded, so are forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a call.
+recorded, so are second derivatives, forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a call.
 
 Shapes: rows of heads are [T, H, D] or [B, S, H, D] of any strides, with one position, slot or length for each token or
 sequence.  int32 is the only integer type.  Everything here is checking of shapes and marshalling.
@@ -22,7 +22,6 @@ from itertools import chain, repeat
 
 import torch
 from torch.autograd import forward_ad
-from torch.autograd.function import once_differentiable
 from torch.fx import _symbolic_trace
 from torch.utils._python_dispatch import _get_current_dispatch_mode_stack
 
@@ -332,12 +331,29 @@ class _NormRope(torch.autograd.Function):
         return _norm_rope(xs[0::2], xs[1::2], table, positions, eps, pairs, [None] * (len(xs) // 2))
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, *douts):
         table, positions, *xs = ctx.saved_tensors
         douts = [d.resolve_neg() for d in douts]            # (of a conjugate's imaginary part)
+        if torch.is_grad_enabled():                         # (create_graph)
+            return (None, None, None, None, *_NormRopeGrad.apply(table, positions, ctx.eps, ctx.pairs, len(douts), *douts, *xs))
         dxs, dgs = _norm_rope_backward(douts, xs[0::2], xs[1::2], table, positions, ctx.eps, ctx.pairs)
         return (None, None, None, None, *(g for pair in zip(dxs, dgs) for g in pair))
+
+
+class _NormRopeGrad(torch.autograd.Function):
+    """The gradients as results that know what they come from, so that whoever differentiates them again is told.  (once_differentiable marks
+    them only where dout requires a gradient, and by a node that leads to none of their sources: a second derivative on the way to another
+    is then left out in silence.)"""
+
+    @staticmethod
+    def forward(ctx, table, positions, eps, pairs, n, *tensors):
+        xs = tensors[n:]
+        dxs, dgs = _norm_rope_backward(tensors[:n], xs[0::2], xs[1::2], table, positions, eps, pairs)
+        return tuple(g for pair in zip(dxs, dgs) for g in pair)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of norm_rope are not differentiable themselves")
 
 
 def _norm_rope(xs, gammas, table, positions, eps, pairs, outs):

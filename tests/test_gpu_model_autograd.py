@@ -6,7 +6,7 @@ from torch.autograd import forward_ad
 from torch.fx.experimental.proxy_tensor import make_fx
 
 from paper_2604_17861_amd import model as M
-from test_gpu_model import ROUTES, _let_go, cache_of, run, up  # noqa: F401
+from test_gpu_model import BF16, F32, ROUTES, _let_go, cache_of, normal, rope_inputs, run, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,14 @@ def test_empty_tensors_in_descriptors(route):
         assert torch.isnan(back[b, :n]).all() and (back[b, n:] == 0).all()
     M.cache_store(x, up(torch.arange(5, dtype=torch.int32)), cache, scales)
     assert torch.isnan(M.cache_load(cache, scales, some, None, 7)).all()
+
+
+def test_gradients_that_keep_their_graph_are_the_same_and_are_not_differentiated_again():
+    gen, x, g, table, p = rope_inputs((33, 4, 64), 64, BF16, F32, "each", 4)
+    leaves = [x.cuda().requires_grad_(), g.cuda().requires_grad_()]
+    table, p, dz = table.cuda(), p.cuda(), normal(gen, 33, 4, 64, dtype=BF16).cuda()
+    want = torch.autograd.grad(M.norm_rope(*leaves, table, p), leaves, dz)
+    got = torch.autograd.grad(M.norm_rope(*leaves, table, p), leaves, dz, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(RuntimeError, match="not differentiable themselves"):
+        (leaves[1].sum() + got[0].float().square().sum()).backward()

@@ -220,3 +220,27 @@ def test_gradients_that_are_lazily_negated_go_through(launched):
     x = torch.randn(3, 2, 8, requires_grad=True)
     torch.complex(torch.zeros(3, 2, 8), M.norm_rope(x)).conj().abs().sum().backward()
     assert launched == [1, 1] and x.grad is not None
+
+
+@pytest.mark.filterwarnings("ignore:Using backward")
+def test_second_derivatives_raise_also_on_the_way_to_others(launched):
+    x, g = torch.randn(3, 2, 8, requires_grad=True), torch.ones(8, requires_grad=True)
+    other = torch.randn(3, requires_grad=True)
+    dz = torch.randn(3, 2, 8)
+    for leaves in ((x,), (x, g), (g,)):
+        z = M.norm_rope(x, g)
+        grads = torch.autograd.grad(z, leaves, dz, create_graph=True)
+        assert all(t.requires_grad for t in grads)
+        with pytest.raises(RuntimeError, match="not differentiable themselves"):
+            (other.sum() + sum(t.square().sum() for t in grads)).backward()
+    with pytest.raises(RuntimeError, match="not differentiable themselves"):      # by way of dout
+        torch.autograd.functional.jvp(lambda t: M.norm_rope(t), x.detach(), dz)
+    # the first ones are there all the same, and what does not need the second goes its way
+    x.grad = g.grad = other.grad = None                      # (of the passes that ended on their way)
+    z = M.norm_rope(x, g)
+    (z.sum() + other.square().sum()).backward(create_graph=True)
+    assert x.grad.shape == x.shape and g.grad.shape == g.shape and torch.equal(other.grad, 2 * other)
+    x.grad = g.grad = other.grad = None
+    q, k = M.norm_rope_qk(x, torch.randn(3, 1, 8), None, g)
+    grads = torch.autograd.grad((q, k), (x, g), (dz, torch.ones(3, 1, 8)), create_graph=True)
+    assert [t.shape for t in grads] == [x.shape, g.shape]
