@@ -252,7 +252,8 @@ typedef struct gpuos_task {
  *   (2j, 2j + 1), j < R/2: the first of a pair becomes y c - y' s, the second y' c + y s,
  *   with c = table[p, j], s = table[p, R/2 + j] of the token's position p.  A position
  *   outside 0 .. places - 1 makes the token's rows NaN.  (The squares of a row are summed in
- *   fp32: rows with elements of over 1e18 leave its range.)
+ *   fp32: rows with elements of over 1e18 leave its range, and so do, where epsilon is 0, rows
+ *   with none of over 1e-19.)
  * NORM_ROPE_GRAD  size = {B, S, H, D, R, places, parts}; operands 0-3 as above,
  *   4 dx [B,S,H,D]  5 dout [B,S,H,D]  6 partial [D, parts], F32, dense, or none
  *   The gradient of x, and in each column of `partial` what one of `parts` shares of
@@ -533,7 +534,8 @@ int gpuos_submit_model(gpuos_ctx* ctx, const gpuos_model_task* tasks, uint32_t n
  * refused nothing is launched.  Up to eight tasks of one operator that follow each other and do not
  * depend on an earlier task of their launch (dep, GPUOS_FLAG_FENCE) are one launch and run at the
  * same time; launches run in order, and a back-distance past the first task is met by the
- * stream's order. */
+ * stream's order.  Each of these kernels has room on a compute unit beside a resident worker of
+ * three workgroups, the default, and of fewer. */
 int gpuos_launch_model(int32_t device, const gpuos_model_task* tasks, uint32_t n, const uint32_t* impl_of_op, void* stream);
 
 /* How such a task is run (no GPU needed), out[0..3] as a task of the ring, out[4..7] as a kernel: 1 for

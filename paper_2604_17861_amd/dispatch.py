@@ -45,7 +45,8 @@ HIP worker kernel through the C ABI (Runtime.submit).  Ordering rules that keep 
     task has completed (host wait on its ticket); view operations only pass the storage along;
   * before the first redirected operation after PyTorch launched work of its own, and before the first
     of every `with` block (what ran outside was not seen), the current stream is synchronised once
-    (its kernels may still be writing the inputs);
+    (its kernels may still be writing the inputs).  What other threads launch, or this one on other streams, is
+    not seen: the caller waits for it before its results go into redirected operations;
   * every tensor a pending task names is kept alive until the task has completed, so the caching
     allocator cannot hand its memory to somebody else;
   * leaving the `with` block (or `synchronize()`) drains everything.

@@ -10,8 +10,9 @@ wait for nothing, and may be captured into a graph.  The `*_task` functions make
 launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as tasks of the ring (bind the operators with
 `register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  include/gpuos.h says what every operator computes and takes.
 
-PyTorch sees no operators here: norm_rope and norm_rope_qk are autograd functions; what has no derivative is refused where gradients are
-recorded, so are second derivatives, forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a call.
+PyTorch sees no operators here.  norm_rope and norm_rope_qk are autograd functions; everything else is refused where a gradient would be
+lost, and so are second derivatives, forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a
+call.  What a descriptor writes, autograd does not hear of.
 
 Shapes: rows of heads are [T, H, D] or [B, S, H, D] of any strides, with one position, slot or length for each token or
 sequence.  int32 is the only integer type.  Everything here is checking of shapes and marshalling.
@@ -310,7 +311,8 @@ def penalty_task(x, out, history=None, prompt_lengths=None, params=None, bias=No
 # ---- norm and rotation -----------------------------------------------------------------------------
 
 def _parts(x, tensors=1):
-    """Shares of gamma's gradient, a workgroup each: as many as there are passes of one (32 rows of 128), at most PARTS_MAX, and of all tensors of
+    """Shares of gamma's gradient, a workgroup each: one for 32 rows, which is a workgroup's pass over rows of 128 elements of 16 bits (of 64 it
+    takes twice as many rows, and half of the shares of a short call are empty; of 512 a quarter), at most PARTS_MAX, and of all tensors of
     a launch no more than the card's 256 units take at once by their registers (five of 16 bits each, four of 32).  Two of 8,192 x 16 heads
     of 128 bf16 with 1,024 / 768 / 640 / 512 shares each: 52, 46, 47, 48 us; 8,192 x 32 of fp32 153, 165, 155, 152; one alone 26 to 29."""
     rows = x.numel() // x.shape[-1]

@@ -5,8 +5,9 @@ import torch
 from torch.autograd import forward_ad
 from torch.fx.experimental.proxy_tensor import make_fx
 
+import model_reference as ref
 from paper_2604_17861_amd import model as M
-from test_gpu_model import BF16, F32, ROUTES, _let_go, cache_of, normal, rope_inputs, run, up  # noqa: F401
+from test_gpu_model import BF16, F32, ROUTES, _let_go, cache_of, check, normal, rope_inputs, run, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +87,29 @@ def test_gradients_that_keep_their_graph_are_the_same_and_are_not_differentiated
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(RuntimeError, match="not differentiable themselves"):
         (leaves[1].sum() + got[0].float().square().sum()).backward()
+
+
+@pytest.mark.parametrize("frozen", ("gamma", "x", "k"))
+def test_gradients_of_some_inputs_only(frozen):
+    gen, q, g, table, p = rope_inputs((70, 4, 64), 64, BF16, F32, "each", 31)
+    k, dq, dk = (normal(gen, 70, n, 64, dtype=BF16) for n in (2, 4, 2))
+    leaves = [t.cuda() for t in (q, k, g)]
+    if frozen != "gamma":
+        leaves[2].requires_grad_()
+    if frozen != "x":
+        leaves[0].requires_grad_()
+        if frozen != "k":
+            leaves[1].requires_grad_()
+    zq, zk = M.norm_rope_qk(leaves[0], leaves[1], leaves[2], leaves[2], table.cuda(), p.cuda())
+    torch.autograd.backward((zq, zk), (dq.cuda(), dk.cuda()))
+    dgs = 0.0
+    size = 0.0
+    for leaf, dz, x in ((leaves[0], dq, q), (leaves[1], dk, k)):
+        dx, s, dg, gs = ref.norm_rope_grad(dz, x, g, table, p, 1e-6, False)
+        dgs, size = dgs + dg, size + gs
+        assert (leaf.grad is None) == (not leaf.requires_grad)
+        if leaf.requires_grad:
+            check(leaf.grad, dx, s, 56)
+    assert (leaves[2].grad is None) == (frozen == "gamma")
+    if frozen != "gamma":                                    # (two sums of at most 280 rows, and their sum)
+        check(leaves[2].grad, dgs, size, 56 + 280 + 256 + 8 + 4 + 1)
