@@ -1,7 +1,7 @@
 """Model operators on PyTorch tensors: the memory-bound steps that stand round a model's matrix products.
 
     q, k = norm_rope_qk(q, k, gamma_q, gamma_k, table, positions)      # norm of every head and rotation, differentiable
-    cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales)  # into a paged cache of 8-bit values
+    cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales)  # into a paged cache of 8-bit values (this and on: no gradients)
     k, v = cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, dtype=q.dtype)
     x = penalize_logits(x, history=tokens, params=params, allowed=bits)
 
