@@ -82,8 +82,10 @@ enum gpuos_status {
 
 /* ---- element types ------------------------------------------------------ */
 enum gpuos_dtype { GPUOS_F32 = 0, GPUOS_F16 = 1, GPUOS_BF16 = 2, GPUOS_I32 = 3,
-                   GPUOS_I8 = 4, GPUOS_E4M3 = 5 };   /* the last two: the values of a quantised cache (gpuos_model_task) only;
-                                                        E4M3 is the OCP format without infinities (largest 448) */
+                   GPUOS_I8 = 4, GPUOS_E4M3 = 5,     /* these two: the values of a quantised cache (gpuos_model_task, gpuos_cache_task)
+                                                        only; E4M3 is the OCP format without infinities (largest 448) */
+                   GPUOS_E2M1 = 6 };                 /* of a gpuos_cache_task only: two a byte, the earlier one in the lower half;
+                                                        by the lower three bits 0 .5 1 1.5 2 3 4 6, the fourth is the sign */
 
 /* ---- built-in device implementations an operator-table entry can name -----
  * (operator library, paper Section 5.2: elementwise add / mul / ReLU / GELU and
@@ -304,6 +306,44 @@ typedef struct gpuos_model_task {
   uint16_t dep[3];                  /* as in gpuos_task                                 */
   uint16_t reserved[3];
 } gpuos_model_task;                 /* 472 bytes */
+
+/* ---- cache operators ------------------------------------------------------
+ * What goes into a paged cache of 4 or 8 bits and the attention that reads it as it is held: kernels on a stream of
+ * the caller's (gpuos_launch_cache).  They have more operands than a gpuos_model_task and matrix instructions, which the worker's
+ * executors have not, and are no tasks of the ring; there a NORM_ROPE and CACHE_STORE, and CACHE_LOAD, do the same
+ * steps by themselves for 8 bits.  Operands, strides and aliasing are as for a gpuos_model_task.  A cache is [pages, page, Hk, D], dense,
+ * I8, E4M3 or (two elements a byte, D even; strides are in bytes) E2M1; its scales are [pages, page, Hk, groups], F32; those
+ * of keys and values have one dtype.
+ *
+ * GPUOS_CACHE_APPEND  size = {B, S, Hq, Hk, D, R, places, pages, page, groups}, 1 <= D <= 512, R even, R <= D
+ *   0 q [B,S,Hq,D]  1 k  2 v [B,S,Hk,D], one float dtype  3 table [places, R], F32, dense (none if R = 0)
+ *   4 positions [B,S], I32 (none: index in S)  5 slots [B,S], I32  6 out [B,S,Hq,D] (may be q)  7 keys' cache  8 their
+ *   scales  9 values' cache  10 their scales
+ *   The first R elements of every head of q and k are rotated as by NORM_ROPE, without a norm, products and sums each
+ *   rounded to 32 bits: a pair (y, y') becomes fl(fl(y c) - fl(y' s)), fl(fl(y' c) + fl(y s)).  q goes to out, rounded once more;
+ *   k, and v as it is, are quantised into their caches as by CACHE_STORE, with qmax = 6 for E2M1 (groups: D, or a power of two
+ *   from 8 on; a zero keeps its sign).  Hq = 0: keys and values only.
+ * GPUOS_CACHE_ATTENTION  size = {B, S, Hq, Hk, D, pages, page, groups, width, longest, window}, D a multiple of 8, D <= 256, Hq a
+ *   multiple of Hk; alpha multiplies the scores.  groups: D, or a power of two from 32 on
+ *   0 q [B,S,Hq,D]  1 keys' cache  2 their scales  3 values' cache  4 their scales  5 table [B, width], I32: page indexes,
+ *   longest <= width * page  6 lengths [B], I32 (none: longest; one over longest counts as it, one below 0 as 0)  7 out [B,S,Hq,D], q's dtype
+ *   Sequence b has lengths[b] rows in the cache, the S queries' own last: query s is at n = lengths[b] - S + s and sees the rows t <= n,
+ *   with a window above 0 of those the t > n - window.  out = softmax(alpha q . k_t) v_t over these; zeros where there are none.  Head h of
+ *   the queries goes with head h / (Hq / Hk) of the cache.  Sums and the softmax are held in fp32, the result is
+ *   rounded once.  A row in a page that is not in the cache is NaN, and so is what a query that sees it gets; what a query does not see
+ *   changes nothing, nor does a row whose weight is below fp32's range.  A code of E4M3 that is no number makes its row NaN.
+ *   No result depends on the order in which anything runs.
+ */
+enum gpuos_cache_op { GPUOS_CACHE_APPEND = 1, GPUOS_CACHE_ATTENTION = 2 };
+#define GPUOS_MAX_CACHE_OPERANDS 11
+typedef struct gpuos_cache_task {
+  uint32_t op;                      /* enum gpuos_cache_op                              */
+  uint32_t flags;                   /* GPUOS_FLAG_PAIRS (GPUOS_CACHE_APPEND)            */
+  int64_t  size[12];                /* as listed above; entries past those are ignored  */
+  gpuos_model_operand operand[GPUOS_MAX_CACHE_OPERANDS];
+  float    alpha;
+  uint32_t reserved;
+} gpuos_cache_task;                 /* 640 bytes */
 
 /* per-ticket completion record (paper Section 5.3 tracepoint fields: task id,
  * operator-table version; timestamps are host steady_clock nanoseconds) */
@@ -542,6 +582,14 @@ int gpuos_launch_model(int32_t device, const gpuos_model_task* tasks, uint32_t n
  * rows in vectors, 0 element by element, 2 nothing to do; work units; items in a unit at most; what an item
  * is: that many heads of a token at most (LOGIT_PENALTY: elements of a row; GAMMA_SUM: 1, a row). */
 int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t out[8]);
+
+/* A cache operator on `stream`, as gpuos_launch_model: nothing is allocated or waited for, and the call may be captured.
+ * workspace: device memory, 16-byte aligned, of as many bytes as gpuos_cache_workspace says (GPUOS_E_NOMEM: fewer); it
+ * belongs to the call until its kernels have run, so two calls that may run at a time need one each. */
+int gpuos_launch_cache(int32_t device, const gpuos_cache_task* task, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The workspace that a task needs, in bytes; 0 for most.  It depends on sizes alone.  No GPU needed. */
+int gpuos_cache_workspace(const gpuos_cache_task* task, uint64_t* bytes);
 
 /* Flush, then block until `ticket` and every earlier ticket completed
  * (GPUOS_ALL: everything submitted).  timeout_ns == 0 uses wait_timeout_ms.

@@ -6,8 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgpuos.so")
-SOURCES = ["gpuos_kernels.hip", "gpuos_model.hip", "gpuos_runtime.cpp", "gpuos_model.cpp", "gpuos_jit.cpp"]
-HEADERS = ["gpuos_internal.h", "gpuos_device.h", "gpuos_model.h", "gpuos_model_device.h", os.path.join("..", "..", "include", "gpuos.h")]
+SOURCES = ["gpuos_kernels.hip", "gpuos_model.hip", "gpuos_cache.hip", "gpuos_runtime.cpp", "gpuos_model.cpp", "gpuos_cache.cpp", "gpuos_jit.cpp"]
+HEADERS = ["gpuos_internal.h", "gpuos_device.h", "gpuos_model.h", "gpuos_model_device.h", "gpuos_cache.h", "gpuos_on_device.h", os.path.join("..", "..", "include", "gpuos.h")]
 
 # -ffp-contract=off: only the FMA operator fuses.  The -packed-fp32-ops target feature switch
 # keeps the compiler from forming packed fp32 instructions.

@@ -1,0 +1,194 @@
+// gpuos_cache.h -- cache operators (gpuos_cache_task): what their kernels are given and, for the host, the check of a
+// descriptor and its packing.
+#pragma once
+#include "gpuos_model.h"
+
+namespace gpuos {
+
+enum CacheFormat : uint32_t { CF_E2M1 = 0, CF_I8 = 1, CF_E4M3 = 2 };
+
+// A cache of keys or of values: where it lies, what a page, a place and a head are apart (bytes; floats for the scales).
+struct CachePart {
+  uint64_t cache, scales;
+  uint32_t cs[3], ss[4];           // page, place, head (, group)
+};
+struct AppendArgs {
+  uint64_t x[3], out, table, positions, slots;       // x: queries, keys, values
+  CachePart kv[2];
+  uint32_t xs[3][4], os[4], ps[2], ls[2], ts;        // strides: B, S, H, D; of positions, slots; of the table's rows
+  uint32_t hq, hk, seq, d, half, places, pages, page, group;
+  uint32_t blocks_q, blocks_k, blocks;               // blocks of heads: of queries, of keys (as many of values), of a token
+  uint32_t items, chunks;
+  Div by_blocks, by_seq, by_page;
+  uint32_t dtype, format;
+  uint32_t vec, pairs;                               // rows in vectors (the rules are at the packing); neighbours are rotated together
+};
+struct AttendArgs {
+  uint64_t q, out, table, lengths, part, stats;      // part, stats: the pieces' sums [pieces, rows, D] and [pieces, rows, 2]
+  CachePart kv[2];
+  uint32_t qs[4], os[4], ps[2], ls;                  // strides: B, S, H, D; of the page table, the lengths
+  uint32_t b, s, hq, hk, per, d, pages, page, group, longest, window;      // per: heads of queries that share one of keys
+  uint32_t rows, tiles, pieces;                      // rows: queries of a head of keys, per * S; tiles of them, and of parts of results; pieces of a sequence
+  uint32_t lg_parts;                                 // parts of a result that are a workgroup each: 1 or 2
+  Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_hk;
+  uint32_t dtype;
+  float scale;                                       // of the scores, in powers of two
+};
+
+constexpr uint32_t kAppendBlock = 2;       // heads of an item
+constexpr uint32_t kTileRows = 16;         // queries of a tile: a side of a matrix instruction's result
+constexpr uint32_t kTileTokens = 64;       // rows of the cache that a wavefront takes at once
+constexpr uint32_t kPiecesMost = 256;
+
+int launch_append(const AppendArgs& a, void* stream);       // gpuos_cache.hip
+int launch_attend(const AttendArgs& a, uint32_t format, void* stream);
+
+// Checks and packs one descriptor.
+class CachePack : ModelPack {
+ public:
+  static constexpr uint32_t kHead = 256;   // elements of a head that attention takes
+  static constexpr uint64_t kBlocksMost = (1ull << 24) - 1;      // workgroups of a launch: a grid has fewer than 2^32 threads
+
+  static int append(const gpuos_cache_task& t, AppendArgs* a, bool* empty) {
+    memset(a, 0, sizeof(*a));
+    if (t.op != GPUOS_CACHE_APPEND || (t.flags & ~GPUOS_FLAG_PAIRS)) return GPUOS_E_INVAL;
+    if (!in_range(t, 10)) return GPUOS_E_INVAL;
+    const int64_t *z = t.size, b = z[0], s = z[1], hq = z[2], hk = z[3], d = z[4], rot = z[5], places = z[6], pages = z[7], page = z[8], groups = z[9];
+    if (!fits(b, s, hq + 2 * hk, d) || d < 1 || d > (int64_t)kModelRow || rot > d || rot % 2 != 0) return GPUOS_E_INVAL;
+    const gpuos_model_operand *q = &t.operand[0], *k = &t.operand[1], *v = &t.operand[2], *table = &t.operand[3], *pos = &t.operand[4], *slots = &t.operand[5],
+                              *out = &t.operand[6];
+    const bool some = b * s != 0, keys = some && hk != 0, queries = some && hq != 0;
+    *empty = !keys && !queries;
+    const int64_t qz[4] = {b, s, hq, d}, kz[4] = {b, s, hk, d}, tz[2] = {places, rot};
+    if ((keys && (!k->ptr || !v->ptr || !slots->ptr)) || (queries && (!q->ptr || !out->ptr))) return GPUOS_E_INVAL;
+    const uint32_t dt = k->dtype;
+    if (!is_float(dt) || v->dtype != dt || (hq != 0 && (q->dtype != dt || out->dtype != dt))) return GPUOS_E_INVAL;
+    if (hq != 0 && (!operand(*q, 4, qz, false, false, a->xs[0]) || !operand(*out, 4, qz, true, false, a->os))) return GPUOS_E_INVAL;
+    if (!operand(*k, 4, kz, false, false, a->xs[1]) || !operand(*v, 4, kz, false, false, a->xs[2])) return GPUOS_E_INVAL;
+    if (slots->dtype != GPUOS_I32 || !operand(*slots, 2, kz, false, false, a->ls)) return GPUOS_E_INVAL;
+    uint32_t ts[2] = {0, 0};
+    if (rot > 0) {
+      if (places < 1 || !table->ptr || table->dtype != GPUOS_F32 || !operand(*table, 2, tz, false, true, ts)) return GPUOS_E_INVAL;
+      if (pos->ptr && (pos->dtype != GPUOS_I32 || !operand(*pos, 2, kz, false, false, a->ps))) return GPUOS_E_INVAL;
+    }
+    const int rc = caches(t, 7, hk, d, pages, page, groups, true, keys && pages != 0, 8, a->kv, &a->format);
+    if (rc != GPUOS_OK) return rc;
+    a->x[0] = (uint64_t)q->ptr; a->x[1] = (uint64_t)k->ptr; a->x[2] = (uint64_t)v->ptr;
+    a->out = (uint64_t)out->ptr;
+    a->table = rot > 0 ? (uint64_t)table->ptr : 0;
+    a->positions = rot > 0 ? (uint64_t)pos->ptr : 0;
+    a->slots = (uint64_t)slots->ptr;
+    a->ts = ts[0];
+    a->hq = (uint32_t)hq; a->hk = (uint32_t)hk; a->seq = (uint32_t)s; a->d = (uint32_t)d;
+    a->half = (uint32_t)(rot / 2); a->places = (uint32_t)places;
+    a->pages = (uint32_t)pages; a->page = (uint32_t)page; a->group = (uint32_t)(d / groups);
+    a->dtype = dt;
+    a->pairs = (t.flags & GPUOS_FLAG_PAIRS) ? 1u : 0u;
+    // Vectors: a lane takes eight elements that are all rotated by the same half of the pairs, or not rotated.
+    const bool dense = (hq == 0 || (a->xs[0][3] == 1 && a->os[3] == 1)) && a->xs[1][3] == 1 && a->xs[2][3] == 1;
+    a->vec = dense && d % 8 == 0 && (a->pairs ? rot : rot / 2) % 8 == 0 ? 1u : 0u;
+    const uint32_t block = a->vec ? kAppendBlock : 1;
+    a->blocks_q = (a->hq + block - 1) / block;
+    a->blocks_k = (a->hk + block - 1) / block;
+    a->blocks = a->blocks_q + 2 * a->blocks_k;
+    if (*empty) return GPUOS_OK;
+    a->items = (uint32_t)(b * s * a->blocks);
+    a->by_blocks = make_div(a->blocks);
+    a->by_seq = make_div(a->seq);
+    a->by_page = make_div(a->page);
+    uint32_t lanes = 1;
+    while (lanes < (a->d + 7) / 8) lanes *= 2;
+    const uint32_t pass = kThreads / lanes;
+    const uint64_t passes = ((uint64_t)a->items + pass - 1) / pass;
+    a->chunks = passes < 65536 ? (uint32_t)passes : 65536u;
+    return GPUOS_OK;
+  }
+
+  // *bytes: what the pieces' sums take, 0 if there is one piece
+  static int attend(const gpuos_cache_task& t, AttendArgs* a, uint32_t* format, uint64_t* bytes, bool* empty) {
+    memset(a, 0, sizeof(*a));
+    *bytes = 0;
+    if (t.op != GPUOS_CACHE_ATTENTION || t.flags != 0 || !in_range(t, 11)) return GPUOS_E_INVAL;
+    const int64_t *z = t.size, b = z[0], s = z[1], hq = z[2], hk = z[3], d = z[4], pages = z[5], page = z[6], groups = z[7], width = z[8], longest = z[9], window = z[10];
+    if (!fits(b, s, hq, d) || d < 8 || d > (int64_t)kHead || d % 8 != 0) return GPUOS_E_INVAL;
+    *empty = b * s * hq == 0;
+    if (hk < 1 || hq % hk != 0 || hk > kMost / (b > 0 ? b : 1)) return GPUOS_E_INVAL;
+    if (!*empty && pages < 1) return GPUOS_E_INVAL;
+    const gpuos_model_operand *q = &t.operand[0], *table = &t.operand[5], *lengths = &t.operand[6], *out = &t.operand[7];
+    const int64_t qz[4] = {b, s, hq, d}, pz[2] = {b, width};
+    if (!*empty && (!q->ptr || !out->ptr || (longest != 0 && !table->ptr))) return GPUOS_E_INVAL;
+    if (!is_float(q->dtype) || out->dtype != q->dtype || !operand(*q, 4, qz, false, false, a->qs) || !operand(*out, 4, qz, true, false, a->os)) return GPUOS_E_INVAL;
+    if (table->dtype != GPUOS_I32 || !operand(*table, 2, pz, false, false, a->ps)) return GPUOS_E_INVAL;
+    if (lengths->ptr && (lengths->dtype != GPUOS_I32 || !operand(*lengths, 1, pz, false, false, &a->ls))) return GPUOS_E_INVAL;
+    const int rc = caches(t, 1, hk, d, pages, page, groups, false, !*empty, 32, a->kv, format);
+    if (rc != GPUOS_OK) return rc;
+    if (longest > width * page) return GPUOS_E_INVAL;           // the table names every row there may be
+    if (!(t.alpha == t.alpha)) return GPUOS_E_INVAL;
+    a->q = (uint64_t)q->ptr; a->out = (uint64_t)out->ptr; a->table = (uint64_t)table->ptr; a->lengths = (uint64_t)lengths->ptr;
+    a->b = (uint32_t)b; a->s = (uint32_t)s; a->hq = (uint32_t)hq; a->hk = (uint32_t)hk; a->per = (uint32_t)(hq / hk); a->d = (uint32_t)d;
+    a->pages = (uint32_t)pages; a->page = (uint32_t)page; a->group = (uint32_t)(d / groups); a->longest = (uint32_t)longest; a->window = (uint32_t)window;
+    a->dtype = q->dtype;
+    a->scale = t.alpha * 1.44269504088896340736f;
+    if (*empty) return GPUOS_OK;
+    a->rows = a->per * a->s;
+    a->lg_parts = d > 128 ? 1u : 0u;
+    a->tiles = ((a->rows + kTileRows - 1) / kTileRows) << a->lg_parts;
+    const uint64_t pairs = (uint64_t)b * hk * a->tiles;
+    // what a tile of queries sees, at most
+    const int64_t seen = window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
+    a->pieces = pieces(pairs, (uint64_t)seen);
+    if (((uint64_t)b * a->pieces + 7) / 8 * 8 * hk * a->tiles > kBlocksMost) return GPUOS_E_INVAL;
+    a->by_page = make_div(a->page);
+    a->by_per = make_div(a->per);
+    a->by_tiles = make_div(a->tiles);
+    a->by_inner = make_div(a->hk * a->tiles);
+    a->by_pieces = make_div(a->pieces);
+    a->by_rows = make_div(a->rows);
+    a->by_hk = make_div(a->hk);
+    if (a->pieces > 1) *bytes = (uint64_t)a->pieces * b * s * hq * (d + 2) * 4;
+    return GPUOS_OK;
+  }
+
+  // Pieces that a sequence's rows are cut into, each a workgroup's; a second launch joins them.
+  static uint32_t pieces(uint64_t pairs, uint64_t seen) {
+    uint64_t n = (1024 + pairs - 1) / pairs;
+    const uint64_t most = (seen + 255) / 256;
+    if (n > most) n = most;
+    if (n > kPiecesMost) n = kPiecesMost;
+    return n < 1 ? 1u : (uint32_t)n;
+  }
+
+ private:
+  static bool in_range(const gpuos_cache_task& t, int n) {
+    for (int k = 0; k < n; ++k)
+      if (t.size[k] < 0 || t.size[k] > kMost) return false;
+    return true;
+  }
+  static bool fits(int64_t b, int64_t s, int64_t h, int64_t d) { return b * s <= kMost && h <= kMost && (b * s == 0 || h <= kMost / (b * s)) && d <= kMost; }
+  // keys' cache and scales, values' cache and scales: operands `first` to first + 3
+  static int caches(const gpuos_cache_task& t, int first, int64_t hk, int64_t d, int64_t pages, int64_t page, int64_t groups, bool out, bool used, int64_t least,
+                    CachePart* kv, uint32_t* format) {
+    if (groups < 1 || d % groups != 0 || page < 1 || pages > kMost / page) return GPUOS_E_INVAL;
+    const int64_t group = d / groups;
+    if (groups > 1 && (group < least || (group & (group - 1)) != 0)) return GPUOS_E_INVAL;
+    const uint32_t dt = t.operand[first].dtype;
+    if (dt != GPUOS_I8 && dt != GPUOS_E4M3 && dt != GPUOS_E2M1) return GPUOS_E_INVAL;
+    if (dt == GPUOS_E2M1 && d % 2 != 0) return GPUOS_E_INVAL;
+    *format = dt == GPUOS_E2M1 ? CF_E2M1 : (dt == GPUOS_I8 ? CF_I8 : CF_E4M3);
+    const int64_t cz[4] = {pages, page, hk, dt == GPUOS_E2M1 ? d / 2 : d}, sz[4] = {pages, page, hk, groups};
+    for (int k = 0; k < 2; ++k) {
+      gpuos_model_operand cache = t.operand[first + 2 * k];
+      const gpuos_model_operand& scales = t.operand[first + 2 * k + 1];
+      uint32_t cs[4];
+      if (cache.dtype != dt || scales.dtype != GPUOS_F32 || (used && (!cache.ptr || !scales.ptr))) return GPUOS_E_INVAL;
+      cache.dtype = GPUOS_I8;                        // (bytes, as far as strides go)
+      if (!operand(cache, 4, cz, out, true, cs) || !operand(scales, 4, sz, out, false, kv[k].ss)) return GPUOS_E_INVAL;
+      for (int i = 0; i < 3; ++i) kv[k].cs[i] = cs[i];
+      kv[k].cache = (uint64_t)cache.ptr;
+      kv[k].scales = (uint64_t)scales.ptr;
+    }
+    return GPUOS_OK;
+  }
+};
+
+}  // namespace gpuos

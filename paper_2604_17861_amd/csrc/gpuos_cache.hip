@@ -1,0 +1,777 @@
+// gpuos_cache.hip -- the kernels of the cache operators: appending rotated keys and values, attention over a cache.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gpuos_cache.h"
+
+namespace gpuos {
+
+#define DEV __device__ __forceinline__
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+template <class T> using G = __attribute__((address_space(1))) T;
+typedef u4 __attribute__((aligned(2))) u4_any;
+typedef u2 __attribute__((aligned(1))) u2_any;
+typedef u4 __attribute__((aligned(1))) u4_byte;
+typedef uint32_t __attribute__((aligned(1))) u1_any;
+template <class T> DEV T ld(uint64_t p) { return *(const G<T>*)p; }
+template <class T> DEV void st(uint64_t p, T v) { *(G<T>*)p = v; }
+DEV float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
+DEV uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }
+constexpr uint32_t size_of(uint32_t dt) { return dt == GPUOS_F32 ? 4u : 2u; }
+template <uint32_t DT> DEV float ld_elem(uint64_t p) {
+  if (DT == GPUOS_F32) return ld<float>(p);
+  const uint16_t h = ld<uint16_t>(p);
+  return DT == GPUOS_F16 ? (float)__builtin_bit_cast(_Float16, h) : as_f((uint32_t)h << 16);
+}
+template <uint32_t DT> DEV uint32_t half_bits(float f) {
+  asm("" : "+v"(f));                       // (or a product and its rounding to 16 bits become one instruction, with one rounding)
+  return DT == GPUOS_F16 ? (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)f) : (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f);
+}
+template <uint32_t DT> DEV void st_elem(uint64_t p, float f) {
+  if (DT == GPUOS_F32) st<float>(p, f);
+  else st<uint16_t>(p, (uint16_t)half_bits<DT>(f));
+}
+// eight elements that follow each other
+template <uint32_t DT> DEV void ld8(uint64_t p, float* f) {
+  const u4 a = ld<u4_any>(p);
+  if (DT == GPUOS_F32) {
+    const u4 b = ld<u4_any>(p + 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] = as_f(a[i]); f[4 + i] = as_f(b[i]); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t h = i & 1 ? a[i / 2] >> 16 : a[i / 2] & 0xffffu;
+      f[i] = DT == GPUOS_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)h) : as_f(h << 16);
+    }
+  }
+}
+template <uint32_t DT> DEV void st8(uint64_t p, const float* f) {
+  if (DT == GPUOS_F32) {
+    st<u4_any>(p, u4{as_u(f[0]), as_u(f[1]), as_u(f[2]), as_u(f[3])});
+    st<u4_any>(p + 16, u4{as_u(f[4]), as_u(f[5]), as_u(f[6]), as_u(f[7])});
+  } else {
+    u4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = half_bits<DT>(f[2 * i]) | (half_bits<DT>(f[2 * i + 1]) << 16);
+    st<u4_any>(p, w);
+  }
+}
+
+template <uint32_t DT> DEV void st4(uint64_t p, f4 f) {
+  if (DT == GPUOS_F32) st<u4_any>(p, __builtin_bit_cast(u4, f));
+  else st<u2_any>(p, u2{half_bits<DT>(f[0]) | (half_bits<DT>(f[1]) << 16), half_bits<DT>(f[2]) | (half_bits<DT>(f[3]) << 16)});
+}
+
+// ---------------------------------------------------------------------------
+// GPUOS_CACHE_APPEND
+//
+// Bound by memory: rows are read once (a rotation reads its other half a second time, out of the line that a neighbouring lane has asked
+// for), and written once, in 16 or 32 bits or as codes.  A power of two of lanes holds a row, eight elements each; what goes over
+// lanes is a group's maximum.  Products and sums of the rotation are rounded by themselves (no fused multiply-add), so that the codes
+// are those of the definition.
+// ---------------------------------------------------------------------------
+DEV uint64_t pick(uint32_t kind, uint64_t a, uint64_t b, uint64_t c) { return kind == 0 ? a : (kind == 1 ? b : c); }
+DEV uint32_t pick(uint32_t kind, uint32_t a, uint32_t b, uint32_t c) { return kind == 0 ? a : (kind == 1 ? b : c); }
+
+// eight codes of |y| <= qmax (1 + 2^-23): to the nearest, to the even one of two
+DEV u2 encode(const float* y, uint32_t format) {
+  u2 w = {0, 0};
+  if (format == CF_E2M1) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], 1.0f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], 1.0f, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], 1.0f, 3);
+    w[0] = c;
+  } else if (format == CF_I8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)(int32_t)__builtin_rintf(y[i]) & 0xffu) << (8 * (i % 4));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
+      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], c, true);
+    }
+  }
+  return w;
+}
+
+// VEC: rows in vectors of eight, each all first, all second or all not rotated elements (neighbours: all rotated or none), last dims dense;
+// else element by element, a head at a time.
+template <uint32_t DT, bool VEC> __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_append_kernel(const AppendArgs a) {
+  constexpr uint32_t ES = size_of(DT);
+  constexpr int U = VEC ? kAppendBlock : 1;
+  const uint32_t units = (a.d + 7u) / 8u, lg = units <= 1u ? 0u : 32u - (uint32_t)__builtin_clz(units - 1u), lanes = 1u << lg;
+  const uint32_t u = threadIdx.x & (lanes - 1u), row = threadIdx.x >> lg, step = kThreads >> lg, j0 = 8u * u;
+  const uint32_t lg_width = a.group == a.d ? lg : 28u - (uint32_t)__builtin_clz(a.group), width = 1u << lg_width;      // lanes of a group
+  const uint32_t n = a.half;
+  const uint32_t left = u < units ? (VEC || a.d - j0 >= 8u ? 8u : a.d - j0) : 0u;      // elements that the lane has
+  const bool first = j0 < n;                                                 // (of a vector's: all)
+  for (uint32_t base = blockIdx.x * step; base < a.items; base += a.chunks * step) {
+    const uint32_t item = base + row < a.items ? base + row : a.items - 1u;
+    const bool there = base + row < a.items && u < units;
+    const uint32_t token = divided(item, a.by_blocks), blk = item - token * a.blocks;
+    const uint32_t b = divided(token, a.by_seq), s = token - b * a.seq;
+    const uint32_t kind = blk < a.blocks_q ? 0u : (blk < a.blocks_q + a.blocks_k ? 1u : 2u);
+    const uint32_t h = (blk - pick(kind, 0u, a.blocks_q, a.blocks_q + a.blocks_k)) * U, count = kind == 0 ? a.hq : a.hk;
+    const uint32_t heads = there ? (count - h < (uint32_t)U ? count - h : (uint32_t)U) : 0u;
+    const uint32_t sb = pick(kind, a.xs[0][0], a.xs[1][0], a.xs[2][0]), ss = pick(kind, a.xs[0][1], a.xs[1][1], a.xs[2][1]);
+    const uint32_t sh = pick(kind, a.xs[0][2], a.xs[1][2], a.xs[2][2]), sd = VEC ? 1u : pick(kind, a.xs[0][3], a.xs[1][3], a.xs[2][3]);
+    const uint64_t xp = pick(kind, a.x[0], a.x[1], a.x[2]) + ((uint64_t)b * sb + (uint64_t)s * ss + (uint64_t)h * sh) * ES;
+    const bool turns = kind != 2u && n != 0u, turned = turns && j0 < 2u * n;
+    uint32_t place = 0;
+    bool has = true;
+    if (turns) {
+      place = a.positions != 0 ? ld<uint32_t>(a.positions + ((uint64_t)b * a.ps[0] + (uint64_t)s * a.ps[1]) * 4u) : s;
+      has = place < a.places;
+    }
+    const uint64_t cosines = a.table + (uint64_t)(has ? place : 0u) * a.ts * 4u, sines = cosines + (uint64_t)n * 4u;
+    const uint32_t slot = kind != 0u ? ld<uint32_t>(a.slots + ((uint64_t)b * a.ls[0] + (uint64_t)s * a.ls[1]) * 4u) : 0xffffffffu;
+    // the elements, the other ones of their pairs, cosines and signed sines: z = x c + p s
+    float z[U][8];
+    if constexpr (VEC) {
+      float x[U][8], p[U][8], c[8], sn[8];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[k][i] = p[k][i] = 0.0f;
+        if ((uint32_t)k < heads) {
+          const uint64_t at = xp + (uint64_t)k * sh * ES;
+          ld8<DT>(at + (uint64_t)j0 * ES, x[k]);
+          if (turned && a.pairs == 0) ld8<DT>(at + (uint64_t)(first ? j0 + n : j0 - n) * ES, p[k]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = sn[i] = 0.0f;
+      if (turned && heads != 0u) {
+        if (a.pairs != 0) {
+          const u4 cc = ld<u4_any>(cosines + (j0 / 2u) * 4u), sc = ld<u4_any>(sines + (j0 / 2u) * 4u);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) { c[i] = as_f(cc[i / 2]); sn[i] = i & 1 ? as_f(sc[i / 2]) : -as_f(sc[i / 2]); }
+        } else {
+          ld8<GPUOS_F32>(cosines + (first ? j0 : j0 - n) * 4u, c);
+          ld8<GPUOS_F32>(sines + (first ? j0 : j0 - n) * 4u, sn);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sn[i] = first ? -sn[i] : sn[i];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[k][i] = turned ? x[k][i] * c[i] + (a.pairs != 0 ? x[k][i ^ 1] : p[k][i]) * sn[i] : x[k][i];
+      }
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t j = j0 + i;
+        z[0][i] = 0.0f;
+        if (heads != 0u && i < left) {
+          z[0][i] = ld_elem<DT>(xp + (uint64_t)j * sd * ES);
+          if (turns && j < 2u * n) {
+            const uint32_t o = a.pairs != 0 ? j ^ 1u : (j < n ? j + n : j - n), at = a.pairs != 0 ? j / 2u : (j < n ? j : j - n);
+            const float c = ld<float>(cosines + (uint64_t)at * 4u), sn = ld<float>(sines + (uint64_t)at * 4u), p = ld_elem<DT>(xp + (uint64_t)o * sd * ES);
+            z[0][i] = z[0][i] * c + p * ((a.pairs != 0 ? (j & 1u) == 0u : j < n) ? -sn : sn);
+          }
+        }
+      }
+    }
+    const bool kept = slot < a.pages * a.page;
+    const uint32_t page = divided(kept ? slot : 0u, a.by_page), in = slot - page * a.page;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (__builtin_amdgcn_ballot_w64((uint32_t)k < heads) == 0) continue;       // (the same in every lane: the maxima need them all)
+      if (!has) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[k][i] = (uint32_t)i < left ? __builtin_nanf("") : 0.0f;
+      }
+      const bool here = (uint32_t)k < heads;
+      if (kind == 0u && here) {
+        const uint64_t to = a.out + ((uint64_t)b * a.os[0] + (uint64_t)s * a.os[1] + (uint64_t)(h + k) * a.os[2]) * ES;
+        if (VEC) st8<DT>(to + (uint64_t)j0 * ES, z[k]);
+        else {
+#pragma unroll
+          for (uint32_t i = 0; i < 8; ++i) {
+            if (i < left) st_elem<DT>(to + (uint64_t)(j0 + i) * a.os[3] * ES, z[k][i]);
+          }
+        }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t m = as_u(z[k][i]) & 0x7fffffffu;
+        top = m > top ? m : top;
+      }
+      for (uint32_t w = 1; w < width; w *= 2) {
+        const uint32_t m = (uint32_t)__shfl_xor((int)top, (int)w, 64);
+        top = m > top ? m : top;
+      }
+      if (kind != 0u && here && kept) {
+        const float qmax = a.format == CF_E2M1 ? 6.0f : (a.format == CF_I8 ? 127.0f : 448.0f);
+        const float m = __builtin_fmaxf(as_f(top), 0x1p-100f), inv = qmax / m;
+        const bool bad = top >= 0x7f800000u;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = bad ? 0.0f : z[k][i] * inv;
+        const u2 w = encode(y, a.format);
+        const bool v = kind == 2u;
+        const uint64_t to = (v ? a.kv[1].cache : a.kv[0].cache) + (uint64_t)page * (v ? a.kv[1].cs[0] : a.kv[0].cs[0]) +
+                            (uint64_t)in * (v ? a.kv[1].cs[1] : a.kv[0].cs[1]) + (uint64_t)(h + k) * (v ? a.kv[1].cs[2] : a.kv[0].cs[2]);
+        if (a.format == CF_E2M1) {
+          if (VEC || left == 8u) st<u1_any>(to + j0 / 2u, w[0]);
+          else for (uint32_t i = 0; i < left / 2u; ++i) st<uint8_t>(to + j0 / 2u + i, (uint8_t)(w[0] >> (8u * i)));
+        } else {
+          if (VEC || left == 8u) st<u2_any>(to + j0, w);
+          else for (uint32_t i = 0; i < left; ++i) st<uint8_t>(to + j0 + i, (uint8_t)((i < 4u ? w[0] : w[1]) >> (8u * (i & 3u))));
+        }
+        if ((u & (width - 1u)) == 0u) {
+          const uint64_t at = (v ? a.kv[1].scales : a.kv[0].scales) + ((uint64_t)page * (v ? a.kv[1].ss[0] : a.kv[0].ss[0]) + (uint64_t)in * (v ? a.kv[1].ss[1] : a.kv[0].ss[1]) +
+                              (uint64_t)(h + k) * (v ? a.kv[1].ss[2] : a.kv[0].ss[2]) + (uint64_t)(u >> lg_width) * (v ? a.kv[1].ss[3] : a.kv[0].ss[3])) * 4u;
+          st<float>(at, bad ? __builtin_nanf("") : m / qmax);
+        }
+      }
+    }
+  }
+}
+
+int launch_append(const AppendArgs& a, void* stream) {
+  const void* const kernels[] = {(const void*)gpuos_cache_append_kernel<GPUOS_F32, true>,   (const void*)gpuos_cache_append_kernel<GPUOS_F16, true>,
+                                 (const void*)gpuos_cache_append_kernel<GPUOS_BF16, true>,  (const void*)gpuos_cache_append_kernel<GPUOS_F32, false>,
+                                 (const void*)gpuos_cache_append_kernel<GPUOS_F16, false>, (const void*)gpuos_cache_append_kernel<GPUOS_BF16, false>};
+  void* args[] = {(void*)&a};
+  return (int)hipLaunchKernel(kernels[a.dtype + (a.vec ? 0u : 3u)], dim3(a.chunks), dim3(kThreads), args, 0, (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------------------
+// GPUOS_CACHE_ATTENTION
+//
+// o_r = sum_t p_rt v_t / sum_t p_rt,  p_rt = 2^(x_rt - m_r),  x_rt = scale log2(e) q_r . k_t, over the t that query r sees; m_r is a running
+// maximum that is followed only when it has grown by 8 (then p < 2^8, and nothing is scaled again for every small step).
+//
+// A workgroup has up to 16 queries that share a head of keys and a piece of the sequence; each of its four wavefronts takes 64 rows of the
+// cache at a time.  Both products are matrix instructions of 16 x 16 x 32 on bf16.  Codes of all formats are bf16 numbers as they stand,
+// so what is multiplied is exact: a row's scale goes onto the sum of a group's products (keys) or onto p (values), in fp32; p and q of
+// more than 8 bits go in as two or three bf16 numbers that add up to them.
+// The first product is K Q^T: lane (n, g) then holds the scores of query n and rows 4 g .. 4 g + 3 of either half, and these eight are the
+// inputs of its part of the second, V^T P^T, if the rows are summed in that order: scores never change lanes, and a query's maximum, sum and
+// results are all in lanes of its number.  64 rows go at a time, four tiles of the first product, two steps of the second.
+// ---------------------------------------------------------------------------
+template <uint32_t FMT> struct Code { static constexpr uint32_t BITS = FMT == CF_E2M1 ? 4u : 8u; };
+
+DEV uint32_t bits_of(bf2 v) { return __builtin_bit_cast(uint32_t, v); }
+// elements 2 I, 2 I + 1 of a word of codes as bf16; int8: of the word's bytes
+template <uint32_t FMT, int I> DEV uint32_t pair_of(uint32_t w) {
+  if constexpr (FMT == CF_E2M1) return bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, I));
+  else if constexpr (FMT == CF_E4M3) return bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, I != 0));
+  else {
+    const float a = (float)(int8_t)(w >> (16 * I)), b = (float)(int8_t)(w >> (16 * I + 8));
+    return __builtin_amdgcn_perm(as_u(b), as_u(a), 0x07060302u);      // (of so few bits the upper half is all)
+  }
+}
+DEV uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+DEV bf8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf8, u4{a, b, c, d}); }
+DEV f4 mfma(bf8 a, bf8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// f's upper 16 bits are the first of its parts, the rest is exact
+DEV float upper(float f) { return as_f(as_u(f) & 0xffff0000u); }
+DEV float rest_of(float f) {
+  const float hi = upper(f), r = f - hi;
+  return (as_u(f) & 0x7f800000u) == 0x7f800000u ? 0.0f : r;
+}
+// over the four lanes of a query
+DEV float max4(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+  v = __builtin_fmaxf(as_f(r[0]), as_f(r[1]));
+  auto q = __builtin_amdgcn_permlane16_swap(as_u(v), as_u(v), false, false);
+  return __builtin_fmaxf(as_f(q[0]), as_f(q[1]));
+}
+DEV float sum4(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(as_u(v), as_u(v), false, false);
+  v = as_f(r[0]) + as_f(r[1]);
+  auto q = __builtin_amdgcn_permlane16_swap(as_u(v), as_u(v), false, false);
+  return as_f(q[0]) + as_f(q[1]);
+}
+DEV void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+// 0 times anything is 0: a row of the cache that a query does not see adds nothing, whatever its scale is.  (Not as inline asm: the compiler does
+// not see there that a result of the exponential is waited for.)
+extern "C" __device__ float legacy_mul(float, float) __asm("llvm.amdgcn.fmul.legacy");
+
+struct AttendPlace { uint32_t b, hk, tile, piece, part; bool there; };
+DEV AttendPlace attend_place(const AttendArgs& a) {
+  // Workgroups go to the eight dies in turn.  All heads of a piece (and all its tiles of queries) go to one die, one behind the other:
+  // heads that lie together share lines of the cache and of its scales there.
+  AttendPlace p;
+  const uint32_t die = blockIdx.x & 7u, k = blockIdx.x >> 3, o = divided(k, a.by_inner), inner = k - o * (a.hk * a.tiles), outer = o * 8u + die;
+  p.there = outer < a.b * a.pieces;
+  p.b = divided(outer, a.by_pieces);
+  p.piece = outer - p.b * a.pieces;
+  p.hk = divided(inner, a.by_tiles);
+  const uint32_t tile = inner - p.hk * a.tiles;
+  p.tile = tile >> a.lg_parts;
+  p.part = tile - (p.tile << a.lg_parts);
+  return p;
+}
+
+// A wavefront's codes go by way of LDS, 64 rows by 64 bytes at a time (a slab): read from memory in pieces of 16 bytes, four lanes a row, the
+// next slab on its way while one is worked on.  Piece c of row t lies in place c ^ swizzle(t), so that neither product's reads meet in a
+// bank: for the first a lane reads its row's codes, for the second a column's of 16 rows (4 bits) or eight, which the LDS transposes.
+DEV uint32_t swizzle(uint32_t t) { return ((t >> 2) ^ (t >> 4)) & 3u; }
+constexpr uint32_t kSlab = 4096;
+typedef int i2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i2* lds_i2;
+
+// DP: elements of a head that there is room for; FULL: a head has as many; MULTI: more than one scale a row.  Of 256 elements a workgroup has
+// all of the scores but one half of the results: with all of those it would not fit into 128 registers (below).
+template <uint32_t FMT, uint32_t DP, bool FULL, uint32_t DT, bool MULTI>
+__global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(128))) gpuos_cache_attend_kernel(const AttendArgs a) {
+  constexpr uint32_t BITS = Code<FMT>::BITS, ROW = DP * BITS / 8u, NS = ROW < 64u ? 1u : ROW / 64u, DS = DP / NS;      // slabs; elements of one
+  constexpr uint32_t DV = DP < 128u ? DP : 128u, NV = NS * DV / DP;            // elements of a result that a workgroup has; slabs of them
+  constexpr uint32_t CH = ROW < 64u ? ROW / 16u : 4u, IT = CH, KS = DS / 32u, MT = DS / 16u;      // pieces of a row; loads of a lane; steps, tiles of a slab
+  constexpr uint32_t NQ = DT == GPUOS_BF16 ? 1u : (DT == GPUOS_F16 ? 2u : 3u), NP = DT == GPUOS_F32 ? 3u : 2u;
+  constexpr uint32_t GROUPS = MULTI ? DP / 32u : 1u;
+  constexpr uint32_t WAVE_LDS = kSlab + 2048u + GROUPS * 512u, Q_LDS = NQ * (DP / 32u) * 1024u, JOIN_LDS = 2u * 16u * DV * 4u + 512u;
+  constexpr uint32_t LDS = Q_LDS + 4u * WAVE_LDS > JOIN_LDS ? Q_LDS + 4u * WAVE_LDS : JOIN_LDS;
+  __shared__ alignas(16) uint8_t lds[LDS];
+  const AttendPlace at = attend_place(a);
+  if (!at.there) return;
+  const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u, n = lane & 15u, g = lane >> 4;
+  const uint32_t d = FULL ? DP : a.d;
+
+  // what the tile's queries see: rows [from, end) of the sequence, and of that this piece's [t0, t1)
+  int32_t len = (int32_t)a.longest;
+  if (a.lengths != 0) {
+    const int32_t l = ld<int32_t>(a.lengths + (uint64_t)at.b * a.ls * 4u);
+    len = l < 0 ? 0 : (l < len ? l : len);
+  }
+  len = __builtin_amdgcn_readfirstlane(len);
+  const uint32_t r0 = at.tile * kTileRows, rl = (r0 + kTileRows < a.rows ? r0 + kTileRows : a.rows) - 1u;      // the tile's first and last query
+  const int32_t past = len - (int32_t)a.s;                                     // rows before the first query's own
+  const int32_t pos_first = past + (int32_t)divided(r0, a.by_per), pos_last = past + (int32_t)divided(rl, a.by_per);
+  const uint32_t row = r0 + n;
+  const bool has_row = row < a.rows;
+  const uint32_t qs = divided(has_row ? row : r0, a.by_per), qh = (has_row ? row : r0) - qs * a.per;
+  const int32_t pos = past + (int32_t)qs;
+  const int32_t see_from = a.window != 0 ? pos - (int32_t)a.window + 1 : 0;      // this lane's query sees [see_from, pos]
+  int32_t from = a.window != 0 ? pos_first - (int32_t)a.window + 1 : 0;
+  from = from < 0 ? 0 : from;
+  const int32_t end = pos_last + 1;
+  const int32_t all_from = a.window != 0 ? pos_last - (int32_t)a.window + 1 : 0;      // all of them see [all_from, pos_first]
+  int32_t t0 = from, t1 = end;
+  if (a.pieces > 1u) {
+    const int32_t blocks = end > from ? (end - from + 63) / 64 : 0, per = (int32_t)divided((uint32_t)blocks + a.pieces - 1u, a.by_pieces);
+    t0 = from + (int32_t)at.piece * per * 64;
+    t1 = t0 + per * 64 < end ? t0 + per * 64 : end;
+  }
+
+  // the queries, as the parts of the second operand of K Q^T
+  bf8* const qf = (bf8*)lds;
+  if (t0 < t1) {
+    for (uint32_t j = wave; j < DP / 32u; j += 4u) {
+      const uint32_t e0 = 32u * j + 8u * g;
+      const uint64_t qp = a.q + ((uint64_t)at.b * a.qs[0] + (uint64_t)qs * a.qs[1] + (uint64_t)(at.hk * a.per + qh) * a.qs[2]) * size_of(DT);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+      if (has_row && e0 < d) {
+        if (a.qs[3] == 1u) ld8<DT>(qp + (uint64_t)e0 * size_of(DT), f);
+        else {
+#pragma unroll
+          for (uint32_t i = 0; i < 8; ++i) f[i] = ld_elem<DT>(qp + (uint64_t)(e0 + i) * a.qs[3] * size_of(DT));
+        }
+      }
+#pragma unroll
+      for (uint32_t t = 0; t < NQ; ++t) {
+        u4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1]));
+        qf[(t * (DP / 32u) + j) * 64u + lane] = __builtin_bit_cast(bf8, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = rest_of(f[i]);
+      }
+    }
+  }
+  __syncthreads();
+
+  uint8_t* const slab = lds + Q_LDS + wave * WAVE_LDS;
+  uint64_t* const offs = (uint64_t*)(slab + kSlab);                // [2][keys, values][64]
+  float* const sc = (float*)(slab + kSlab + 2048u);                // [GROUPS][keys, values][64]
+  const uint64_t table = a.table + (uint64_t)at.b * a.ps[0] * 4u;
+  float ks[GROUPS], vs[GROUPS];                                    // scales of row t + lane
+  u4 r[IT];                                                        // a slab's pieces
+
+  const auto look = [&](int32_t t) -> uint32_t {                   // the entry of the page table for row t + lane (behind the last: for that)
+    const int32_t k = t + (int32_t)lane < t1 ? t + (int32_t)lane : t1 - 1;
+    return ld<uint32_t>(table + (uint64_t)divided((uint32_t)k, a.by_page) * a.ps[1] * 4u);
+  };
+  const auto find = [&](int32_t t, uint32_t entry, uint32_t buf) {      // where the row lies, and its scales
+    const uint32_t k = (uint32_t)(t + (int32_t)lane < t1 ? t + (int32_t)lane : t1 - 1), in = k - divided(k, a.by_page) * a.page;
+    const bool known = entry < a.pages;
+    const uint64_t e = known ? entry : 0u;
+#pragma unroll
+    for (uint32_t v = 0; v < 2; ++v) {
+      offs[(buf * 2u + v) * 64u + lane] = a.kv[v].cache + (uint64_t)at.hk * a.kv[v].cs[2] + e * a.kv[v].cs[0] + (uint64_t)in * a.kv[v].cs[1];
+      const uint64_t sp = a.kv[v].scales + ((uint64_t)at.hk * a.kv[v].ss[2] + e * a.kv[v].ss[0] + (uint64_t)in * a.kv[v].ss[1]) * 4u;
+#pragma unroll
+      for (uint32_t q = 0; q < GROUPS; ++q) {
+        float f = !MULTI || q * a.group < d ? ld<float>(sp + (uint64_t)q * a.kv[v].ss[3] * 4u) : 0.0f;
+        if (!known) f = __builtin_nanf("");                        // a page that is not in the cache
+        (v ? vs : ks)[q] = f;
+      }
+    }
+  };
+  const auto ask = [&](uint32_t buf, uint32_t v, uint32_t s) {
+#pragma unroll
+    for (uint32_t i = 0; i < IT; ++i) {
+      const uint32_t c = lane & (CH - 1u);
+      const uint64_t p = offs[(buf * 2u + v) * 64u + i * (64u / CH) + lane / CH] + 64u * s + 16u * c;
+      if (FULL) r[i] = ld<u4_byte>(p);
+      else {
+        const uint32_t row_bytes = d * BITS / 8u, e = 64u * s + 16u * c;
+        r[i] = u4{0, 0, 0, 0};
+        if (e + 16u <= row_bytes) r[i] = ld<u4_byte>(p);
+        else {
+#pragma unroll
+          for (uint32_t w = 0; w < 4; ++w) {
+            if (e + 4u * w < row_bytes) r[i][w] = ld<u1_any>(p + 4u * w);
+          }
+        }
+      }
+    }
+  };
+  // Places in LDS: of piece c of row t, 64 t + 16 (c ^ swizzle(t)).  Those of a lane differ by an exclusive or and a constant from the first,
+  // which is hidden from the compiler: it would keep them all in registers.
+  const auto hidden = [](uint32_t v) { asm("" : "+v"(v)); return v; };
+  const auto slab_at = [&](uint32_t t, uint32_t c, uint32_t more) { return 64u * t + 16u * (c ^ swizzle(t)) + more; };
+  const uint32_t put_at = slab_at(lane / CH, lane & (CH - 1u), 0);
+  const uint32_t key_at = BITS == 4u ? slab_at(n, 0, 4u * g) : slab_at(n, g >> 1, 8u * (g & 1u));
+  const uint32_t value_at = BITS == 4u ? slab_at(16u * (n >> 2) + 4u * g + (n & 3u), 0, 0) : slab_at(16u * (n >> 3) + 4u * g + ((n >> 1) & 3u), 0, 8u * (n & 1u));
+  const auto put = [&]() {
+    const uint32_t o = hidden(put_at);
+#pragma unroll
+    for (uint32_t i = 0; i < IT; ++i) *(u4*)(slab + i * (64u / CH) * 64u + (o ^ (swizzle(i * (64u / CH)) << 4))) = r[i];
+  };
+
+  const uint32_t first_slab = at.part * NV, first_e = at.part * DV;      // of the values that the workgroup has
+  f4 acc[NV * MT];
+#pragma unroll
+  for (uint32_t j = 0; j < NV * MT; ++j) acc[j] = f4{0, 0, 0, 0};
+  float m = -__builtin_inff(), l = 0.0f;
+  int32_t t = t0 + (int32_t)wave * 64;
+  uint32_t entry = 0, buf = 0;
+  if (t < t1) {
+    entry = look(t);
+    find(t, entry, 0);
+    wave_sync();
+    ask(0, 0, 0);
+    entry = look(t + 256);
+  }
+  for (; t < t1; t += 256, buf ^= 1u) {
+#pragma unroll
+    for (uint32_t q = 0; q < GROUPS; ++q) {
+      sc[(2u * q) * 64u + lane] = ks[q];
+      sc[(2u * q + 1u) * 64u + lane] = vs[q];
+    }
+    // scores: of query n, rows 16 T + 4 g + i
+    f4 x[4], c[4];
+#pragma unroll
+    for (int T = 0; T < 4; ++T) x[T] = c[T] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t s = 0; s < NS; ++s) {
+      put();
+      wave_sync();
+      if (s + 1u < NS) ask(buf, 0, s + 1u);
+      else ask(buf, 1, first_slab);
+      const uint32_t ko = hidden(key_at);
+#pragma unroll
+      for (uint32_t j = 0; j < KS; ++j) {
+        const uint32_t e = s * DS + 32u * j;                       // the step's first element
+        if (FULL || e < d) {
+          bf8 q[NQ];
+#pragma unroll
+          for (uint32_t k = 0; k < NQ; ++k) q[k] = qf[(k * (DP / 32u) + e / 32u) * 64u + lane];
+#pragma unroll
+          for (uint32_t T = 0; T < 4; ++T) {
+            bf8 k;
+            const uint8_t* const kp = slab + 1024u * T + (ko ^ (((j * (BITS / 4u)) ^ T) << 4));
+            if constexpr (BITS == 4u) {
+              const uint32_t w = *(const uint32_t*)kp;
+              k = frag(pair_of<FMT, 0>(w), pair_of<FMT, 1>(w), pair_of<FMT, BITS == 4u ? 2 : 0>(w), pair_of<FMT, BITS == 4u ? 3 : 0>(w));
+            } else {
+              const u2 w = *(const u2*)kp;
+              k = frag(pair_of<FMT, 0>(w[0]), pair_of<FMT, 1>(w[0]), pair_of<FMT, 0>(w[1]), pair_of<FMT, 1>(w[1]));
+            }
+#pragma unroll
+            for (uint32_t z = 0; z < NQ; ++z) c[T] = mfma(k, q[z], c[T]);
+          }
+          if (MULTI && (e + 32u) % a.group == 0u) {
+#pragma unroll
+            for (uint32_t T = 0; T < 4; ++T) {
+              const f4 f = *(const f4*)(sc + (2u * (e / a.group)) * 64u + 16u * T + 4u * g);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[T][i] = __builtin_fmaf(c[T][i], f[i], x[T][i]);
+              c[T] = f4{0, 0, 0, 0};
+            }
+          }
+        }
+      }
+      wave_sync();
+    }
+    const bool next = t + 256 < t1;
+    if (next) find(t + 256, entry, buf ^ 1u);                      // (these scales go into LDS at the top)
+#pragma unroll
+    for (uint32_t T = 0; T < 4; ++T) {
+      if (!MULTI) x[T] = c[T] * *(const f4*)(sc + 16u * T + 4u * g);
+      x[T] *= a.scale;
+    }
+    if (t < all_from || t + 63 > pos_first || t + 64 > t1) {       // some query does not see all of these
+#pragma unroll
+      for (int T = 0; T < 4; ++T) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t k = t + 16 * T + (int32_t)(4u * g) + i;
+          x[T][i] = k < t1 && k <= pos && k >= see_from ? x[T][i] : -__builtin_inff();
+        }
+      }
+    }
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int T = 0; T < 4; ++T) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, x[T][i]);
+    }
+    top = max4(top);
+    if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
+      const float to = __builtin_fmaxf(m, top), by = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);      // (1 also where both are -inf)
+      m = to;
+      l *= by;
+#pragma unroll
+      for (uint32_t j = 0; j < NV * MT; ++j) acc[j] *= by;
+    }
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+    for (int T = 0; T < 4; ++T) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[T][i] = __builtin_amdgcn_exp2f(x[T][i] - base);
+      l += (x[T][0] + x[T][1]) + (x[T][2] + x[T][3]);
+    }
+
+    // weights: 2^(x - m) times the scale of the row's group, in parts
+    bf8 w[NP][2];
+    const auto weights = [&](uint32_t group) {
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u) {
+        float f[8];
+#pragma unroll
+        for (uint32_t T = 0; T < 2; ++T) {
+          const f4 v = *(const f4*)(sc + (2u * group + 1u) * 64u + 16u * (2u * u + T) + 4u * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[4 * T + i] = legacy_mul(x[2u * u + T][i], v[i]);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < NP; ++k) {
+          u4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            v[i] = k + 1u < NP ? high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1])) : bits_of(__builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), bf2));
+          }
+          w[k][u] = __builtin_bit_cast(bf8, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = f[i] - upper(f[i]);
+        }
+      }
+    };
+#pragma unroll
+    for (uint32_t s = 0; s < NV; ++s) {
+      if constexpr (FMT == CF_E4M3) {
+        // A code that is no number makes its row none: the code becomes 0, the row's scale a NaN.
+        uint32_t any = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < IT; ++i) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) any |= (r[i][k] & 0x7f7f7f7fu) + 0x01010101u;
+        }
+        if (__builtin_amdgcn_ballot_w64((any & 0x80808080u) != 0u) != 0) {
+#pragma unroll
+          for (uint32_t i = 0; i < IT; ++i) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t y = ((r[i][k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+              bad |= y;
+              r[i][k] &= ~((y >> 7) * 0xffu);
+            }
+            if (bad != 0u) {
+#pragma unroll
+              for (uint32_t q = 0; q < GROUPS; ++q) sc[(2u * q + 1u) * 64u + i * (64u / CH) + lane / CH] = __builtin_nanf("");
+            }
+          }
+        }
+      }
+      put();
+      wave_sync();
+      if (s + 1u < NV) ask(buf, 1, first_slab + s + 1u);
+      else if (next) {
+        ask(buf ^ 1u, 0, 0);
+        entry = look(t + 512);
+      }
+      if (!MULTI && s == 0u) weights(0);
+      const uint32_t vo = hidden(value_at);
+#pragma unroll
+      for (uint32_t j = 0; j < MT; ++j) {
+        const uint32_t e = first_e + s * DS + 16u * j;             // the tile's first element
+        if (FULL || e < d) {
+          if (MULTI && e % a.group == 0u) weights(e / a.group);
+          f4& o = acc[s * MT + j];
+          bf8 v[2];
+          if constexpr (BITS == 4u) {
+            const i2 y = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2)(slab + (vo ^ ((j >> 1) << 4)) + 8u * (j & 1u)));
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              v[u] = frag(pair_of<FMT, 0>((uint32_t)y[u]), pair_of<FMT, 1>((uint32_t)y[u]), pair_of<FMT, BITS == 4u ? 2 : 0>((uint32_t)y[u]), pair_of<FMT, BITS == 4u ? 3 : 0>((uint32_t)y[u]));
+          } else {
+#pragma unroll
+            for (uint32_t u = 0; u < 2; ++u) {
+              const i2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2)(slab + 2048u * u + (vo ^ ((j ^ (2u * u)) << 4))));
+              v[u] = frag(pair_of<FMT, 0>((uint32_t)y[0]), pair_of<FMT, 1>((uint32_t)y[0]), pair_of<FMT, 0>((uint32_t)y[1]), pair_of<FMT, 1>((uint32_t)y[1]));
+            }
+          }
+#pragma unroll
+          for (uint32_t k = 0; k < NP; ++k) {
+            o = mfma(v[0], w[k][0], o);
+            o = mfma(v[1], w[k][1], o);
+          }
+        }
+      }
+      wave_sync();
+    }
+  }
+
+  // the four wavefronts' sums
+  l = sum4(l);
+  __syncthreads();
+  float* const stats = (float*)lds;                                // [4][16][2]
+  float* const sums = (float*)(lds + 512u);                        // [2][16][DP]
+  if (g == 0u) {
+    stats[(wave * 16u + n) * 2u] = m;
+    stats[(wave * 16u + n) * 2u + 1u] = l;
+  }
+  __syncthreads();
+  float most = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) most = __builtin_fmaxf(most, stats[(k * 16u + n) * 2u]);
+  const float ref = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) total += stats[(k * 16u + n) * 2u + 1u] * __builtin_amdgcn_exp2f(stats[(k * 16u + n) * 2u] - ref);
+  const float by = __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+  for (uint32_t j = 0; j < NV * MT; ++j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[j][i] *= by;
+  }
+  // (two and two, then the two: always in this order)
+  for (uint32_t k = 2; k >= 1u; k /= 2u) {
+    if (wave >= k && wave < 2u * k) {
+#pragma unroll
+      for (uint32_t j = 0; j < NV * MT; ++j) *(f4*)(sums + ((wave - k) * NV * MT + j) * 256u + lane * 4u) = acc[j];
+    }
+    __syncthreads();
+    if (wave < k) {
+#pragma unroll
+      for (uint32_t j = 0; j < NV * MT; ++j) acc[j] += *(const f4*)(sums + (wave * NV * MT + j) * 256u + lane * 4u);
+    }
+    __syncthreads();
+  }
+  if (wave != 0u || !has_row) return;
+  const bool last = a.pieces == 1u;
+  const float inv = last ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
+  const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(at.hk * a.per + qh) * a.os[2]) * size_of(DT);
+  const uint64_t all = (uint64_t)a.b * a.hk * a.rows, mine = ((uint64_t)at.b * a.hk + at.hk) * a.rows + row, slice = (uint64_t)at.piece * all + mine;
+  if (!last && g == 0u && at.part == 0u) {
+    st<float>(a.stats + slice * 8u, most);
+    st<float>(a.stats + slice * 8u + 4u, total);
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < NV * MT; ++j) {
+    const uint32_t e = first_e + 16u * j + 4u * g;                 // (a head has a multiple of eight)
+    if (FULL || e < d) {
+      if (!last) st<u4_any>(a.part + (slice * d + e) * 4u, __builtin_bit_cast(u4, acc[j]));
+      else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) acc[j][i] *= inv;
+        if (a.os[3] == 1u) st4<DT>(op + (uint64_t)e * size_of(DT), acc[j]);
+        else {
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) st_elem<DT>(op + (uint64_t)(e + i) * a.os[3] * size_of(DT), acc[j][i]);
+        }
+      }
+    }
+  }
+}
+
+// The pieces' sums: a workgroup has a query; each of its wavefronts adds every fourth piece.
+template <uint32_t DT> __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_join_kernel(const AttendArgs a) {
+  __shared__ alignas(16) float lds[4 * 260];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u, mine = blockIdx.x;
+  const uint64_t all = (uint64_t)a.b * a.hk * a.rows;
+  float most = -__builtin_inff();
+  for (uint32_t k = lane; k < a.pieces; k += 64u) most = __builtin_fmaxf(most, ld<float>(a.stats + (k * all + mine) * 8u));
+  for (int w = 32; w >= 1; w /= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w, 64));
+  const float ref = most == -__builtin_inff() ? 0.0f : most;
+  float sum[4] = {0, 0, 0, 0}, total = 0.0f;
+  for (uint32_t k = wave; k < a.pieces; k += 4u) {
+    const uint64_t slice = k * all + mine;
+    const float l = ld<float>(a.stats + slice * 8u + 4u), by = __builtin_amdgcn_exp2f(ld<float>(a.stats + slice * 8u) - ref);
+    if (l == 0.0f) continue;                                       // (an empty piece: its sums were not written)
+    total += l * by;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      if (lane + 64u * i < a.d) sum[i] += ld<float>(a.part + (slice * a.d + lane + 64u * i) * 4u) * by;
+    }
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) lds[wave * 260u + lane + 64u * i] = sum[i];
+  if (lane == 0u) lds[wave * 260u + 256u] = total;
+  __syncthreads();
+  total = (lds[256] + lds[260 + 256]) + (lds[520 + 256] + lds[780 + 256]);
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const uint32_t pair = divided(mine, a.by_rows), row = mine - pair * a.rows, b = divided(pair, a.by_hk), hk = pair - b * a.hk;
+  const uint32_t qs = divided(row, a.by_per), qh = row - qs * a.per;
+  const uint64_t op = a.out + ((uint64_t)b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(hk * a.per + qh) * a.os[2]) * size_of(DT);
+  const uint32_t e = threadIdx.x;
+  if (e < a.d) st_elem<DT>(op + (uint64_t)e * a.os[3] * size_of(DT), ((lds[e] + lds[260 + e]) + (lds[520 + e] + lds[780 + e])) * inv);
+}
+
+template <uint32_t FMT, uint32_t DT, bool MULTI> const void* attend_kernel(uint32_t d) {
+  if constexpr (DT != GPUOS_F32) {
+    if (d == 64u) return (const void*)gpuos_cache_attend_kernel<FMT, 64, true, DT, MULTI>;
+    if (d == 128u) return (const void*)gpuos_cache_attend_kernel<FMT, 128, true, DT, MULTI>;
+    if (d == 256u) return (const void*)gpuos_cache_attend_kernel<FMT, 256, true, DT, MULTI>;
+  }
+  if (d <= 128u) return (const void*)gpuos_cache_attend_kernel<FMT, 128, false, DT, MULTI>;
+  return (const void*)gpuos_cache_attend_kernel<FMT, 256, false, DT, MULTI>;
+}
+template <uint32_t FMT> const void* attend_kernel(uint32_t dt, uint32_t d, bool multi) {
+  if (dt == GPUOS_F32) return multi ? attend_kernel<FMT, GPUOS_F32, true>(d) : attend_kernel<FMT, GPUOS_F32, false>(d);
+  if (dt == GPUOS_F16) return multi ? attend_kernel<FMT, GPUOS_F16, true>(d) : attend_kernel<FMT, GPUOS_F16, false>(d);
+  return multi ? attend_kernel<FMT, GPUOS_BF16, true>(d) : attend_kernel<FMT, GPUOS_BF16, false>(d);
+}
+
+int launch_attend(const AttendArgs& a, uint32_t format, void* stream) {
+  const bool multi = a.group != a.d;
+  const void* kernel = format == CF_E2M1 ? attend_kernel<CF_E2M1>(a.dtype, a.d, multi) : (format == CF_I8 ? attend_kernel<CF_I8>(a.dtype, a.d, multi) : attend_kernel<CF_E4M3>(a.dtype, a.d, multi));
+  void* args[] = {(void*)&a};
+  const uint32_t outer = (a.b * a.pieces + 7u) / 8u * 8u;
+  const int rc = (int)hipLaunchKernel(kernel, dim3(outer * a.hk * a.tiles), dim3(kThreads), args, 0, (hipStream_t)stream);
+  if (rc != (int)hipSuccess || a.pieces == 1u) return rc;
+  const void* const joins[] = {(const void*)gpuos_cache_join_kernel<GPUOS_F32>, (const void*)gpuos_cache_join_kernel<GPUOS_F16>, (const void*)gpuos_cache_join_kernel<GPUOS_BF16>};
+  return (int)hipLaunchKernel(joins[a.dtype], dim3(a.b * a.hk * a.rows), dim3(kThreads), args, 0, (hipStream_t)stream);
+}
+
+}  // namespace gpuos

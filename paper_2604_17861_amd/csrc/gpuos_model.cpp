@@ -1,38 +1,15 @@
 // gpuos_model.cpp -- model operators as ordinary kernels on a caller's stream (gpuos_launch_model), and how
 // their tasks are cut (gpuos_model_plan).  Their checks and packing are in gpuos_model.h.
 
-#include <hip/hip_runtime_api.h>
-
 #include <new>
 #include <vector>
 
 #include "../../include/gpuos.h"
 #include "gpuos_internal.h"
 #include "gpuos_model.h"
+#include "gpuos_on_device.h"
 
 using namespace gpuos;
-
-namespace {
-
-// The device that a call works on, and the caller's again when it ends.
-class OnDevice {
- public:
-  explicit OnDevice(int device) {
-    int e = (int)hipGetDevice(&before_);
-    if (e == (int)hipSuccess && before_ != device) {
-      e = (int)hipSetDevice(device);
-      changed_ = e == (int)hipSuccess;
-    }
-    status = hip_status(e, "hipSetDevice");
-  }
-  ~OnDevice() { if (changed_) (void)hipSetDevice(before_); }
-  int status;
- private:
-  int before_ = 0;
-  bool changed_ = false;
-};
-
-}  // namespace
 
 extern "C" {
 

@@ -196,7 +196,7 @@ class ModelPack {
     return rc;
   }
 
- private:
+ protected:
   static constexpr int64_t kMost = 2147483647LL;     // rows, and elements of one dim
   static constexpr int64_t kExtent = 1LL << 46;      // elements from an operand's first to its last
   static uint32_t size_of(uint32_t dt) { return dt >= GPUOS_I8 ? 1u : (dt == GPUOS_F32 || dt == GPUOS_I32 ? 4u : 2u); }

@@ -529,3 +529,7 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
         plan = _keep(key, _Plan((x,), (task,), (operands,)))
     _run(plan, operands, given)
     return out
+
+
+# ---- a cache of 4 or 8 bits and the attention that reads it ------------------------------------------
+from ._cache import cache_append_qkv, cache_attention  # noqa: E402,F401

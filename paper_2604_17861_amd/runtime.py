@@ -84,6 +84,8 @@ def lib():
         "gpuos_submit_model": (ctypes.c_int, [vp, vp, u32, P(u64)]),
         "gpuos_launch_model": (ctypes.c_int, [i32, vp, u32, vp, vp]),
         "gpuos_model_plan": (ctypes.c_int, [vp, u32, vp]),
+        "gpuos_launch_cache": (ctypes.c_int, [i32, vp, vp, u64, vp]),
+        "gpuos_cache_workspace": (ctypes.c_int, [vp, P(u64)]),
         "gpuos_flush": (ctypes.c_int, [vp]),
         "gpuos_wait": (ctypes.c_int, [vp, u64, u64]),
         "gpuos_get_completions": (ctypes.c_int, [vp, u64, u32, vp]),
@@ -453,6 +455,33 @@ def launch_model_at(tasks, n, device, stream):
     rc = _launch_model(device, tasks, n, _model_table, stream)
     if rc != OK:
         raise GpuosError(rc, "gpuos_launch_model")
+
+
+_launch_cache = None
+
+
+def cache_workspace(task):
+    """gpuos_cache_workspace of a cache operator's descriptor (bytes): the bytes that its launch needs."""
+    assert isinstance(task, bytes) and len(task) == S.CACHE_TASK_BYTES
+    n = ctypes.c_uint64()
+    _check(lib().gpuos_cache_workspace(task, ctypes.byref(n)), "gpuos_cache_workspace")
+    return n.value
+
+
+def launch_cache(task, workspace=0, workspace_bytes=0, device=0, stream=0):
+    """gpuos_launch_cache: a cache operator's descriptor (bytes) on `stream` (a stream's handle); workspace: a device address."""
+    assert isinstance(task, bytes) and len(task) == S.CACHE_TASK_BYTES
+    launch_cache_at(task, device, workspace, workspace_bytes, stream)
+
+
+def launch_cache_at(task, device, workspace, workspace_bytes, stream):
+    """launch_cache of a descriptor at an address."""
+    global _launch_cache
+    if _launch_cache is None:
+        _launch_cache = lib().gpuos_launch_cache
+    rc = _launch_cache(device, task, workspace, workspace_bytes, stream)
+    if rc != OK:
+        raise GpuosError(rc, "gpuos_launch_cache")
 
 
 def _impl_table(table):

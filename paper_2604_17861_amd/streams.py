@@ -56,6 +56,7 @@ FLAG_FENCE, FLAG_KEEPDIM = 1, 2
 MODEL_IMPL = dict(NORM_ROPE=20, NORM_ROPE_GRAD=21, GAMMA_SUM=22, CACHE_STORE=23, CACHE_LOAD=24, LOGIT_PENALTY=25)
 MODEL_OP = {name: code + 32 for name, code in MODEL_IMPL.items()}
 MODEL_TASK_BYTES = 472
+CACHE_TASK_BYTES = 640
 
 # Operator programs (elementwise operators defined at run time as instruction lists): impl ids from
 # PROGRAM_BASE name the programs a context (or a test) has defined.  Eight fp32 registers: r0..r2 the
