@@ -1,6 +1,7 @@
 // gpuos_cache.h -- cache operators (gpuos_cache_task): what their kernels are given and, for the host, the check of a
 // descriptor and its packing.
 #pragma once
+#include <stdlib.h>
 #include "gpuos_model.h"
 
 namespace gpuos {
@@ -30,7 +31,8 @@ struct AttendArgs {
   uint32_t b, s, hq, hk, per, d, pages, page, group, longest, window;      // per: heads of queries that share one of keys
   uint32_t rows, tiles, pieces;                      // rows: queries of a head of keys, per * S; tiles of them, and of parts of results; pieces of a sequence
   uint32_t lg_parts;                                 // parts of a result that are a workgroup each: 1 or 2
-  Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_hk;
+  uint32_t blocks, inner;                            // workgroups, and how many that follow each other go to one die
+  Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_hk, by_group;
   uint32_t dtype;
   float scale;                                       // of the scores, in powers of two
 };
@@ -47,7 +49,7 @@ int launch_attend(const AttendArgs& a, uint32_t format, void* stream);
 class CachePack : ModelPack {
  public:
   static constexpr uint32_t kHead = 256;   // elements of a head that attention takes
-  static constexpr uint64_t kBlocksMost = (1ull << 24) - 1;      // workgroups of a launch: a grid has fewer than 2^32 threads
+  static constexpr uint64_t kBlocksMost = 14000000;      // workgroups of a launch: a grid, an eighth larger, has fewer than 2^32 threads
 
   static int append(const gpuos_cache_task& t, AppendArgs* a, bool* empty) {
     memset(a, 0, sizeof(*a));
@@ -137,11 +139,20 @@ class CachePack : ModelPack {
     // what a tile of queries sees, at most
     const int64_t seen = window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
     a->pieces = pieces(pairs, (uint64_t)seen);
-    if (((uint64_t)b * a->pieces + 7) / 8 * 8 * hk * a->tiles > kBlocksMost) return GPUOS_E_INVAL;
+    if (pairs * a->pieces > kBlocksMost) return GPUOS_E_INVAL;
+    a->blocks = (uint32_t)(pairs * a->pieces);
+    // All heads of a piece of a sequence go to one die, if the dies then have about as much to do; else all queries of a head; else each workgroup to the next.
+    const uint32_t inners[2] = {a->hk * a->tiles, a->tiles};
+    a->inner = 1;
+    for (uint32_t n : inners) {
+      const uint32_t outer = a->blocks / n;
+      if ((outer + 7) / 8 * 8 * 8 <= outer * 9) { a->inner = n; break; }
+    }
     a->by_page = make_div(a->page);
     a->by_per = make_div(a->per);
+    a->by_group = make_div(a->group);
     a->by_tiles = make_div(a->tiles);
-    a->by_inner = make_div(a->hk * a->tiles);
+    a->by_inner = make_div(a->inner);
     a->by_pieces = make_div(a->pieces);
     a->by_rows = make_div(a->rows);
     a->by_hk = make_div(a->hk);
@@ -151,8 +162,9 @@ class CachePack : ModelPack {
 
   // Pieces that a sequence's rows are cut into, each a workgroup's; a second launch joins them.
   static uint32_t pieces(uint64_t pairs, uint64_t seen) {
-    uint64_t n = (1024 + pairs - 1) / pairs;
-    const uint64_t most = (seen + 255) / 256;
+    static const uint64_t T = getenv("GT") ? atoi(getenv("GT")) : 1024, MN = getenv("GM") ? atoi(getenv("GM")) : 512;
+    uint64_t n = (T + pairs - 1) / pairs;
+    const uint64_t most = (seen + MN - 1) / MN;
     if (n > most) n = most;
     if (n > kPiecesMost) n = kPiecesMost;
     return n < 1 ? 1u : (uint32_t)n;

@@ -274,12 +274,27 @@ template <uint32_t FMT, int I> DEV uint32_t pair_of(uint32_t w) {
 }
 DEV uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 DEV bf8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf8, u4{a, b, c, d}); }
+// eight codes that follow each other: a word of 4 bits each, two of 8
+template <uint32_t FMT> DEV bf8 eight_of(uint32_t a, uint32_t b) {
+  if constexpr (FMT == CF_E2M1) return frag(pair_of<FMT, 0>(a), pair_of<FMT, 1>(a), pair_of<FMT, 2>(a), pair_of<FMT, 3>(a));
+  else return frag(pair_of<FMT, 0>(a), pair_of<FMT, 1>(a), pair_of<FMT, 0>(b), pair_of<FMT, 1>(b));
+}
 DEV f4 mfma(bf8 a, bf8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // f's upper 16 bits are the first of its parts, the rest is exact
 DEV float upper(float f) { return as_f(as_u(f) & 0xffff0000u); }
 DEV float rest_of(float f) {
   const float hi = upper(f), r = f - hi;
   return (as_u(f) & 0x7f800000u) == 0x7f800000u ? 0.0f : r;
+}
+// v, of which the compiler does not know where it is from: it computes what depends on it here, and does not keep it; and the same, not before f is
+// there: or it begins everything that does not depend on anything before it finishes something.  Either way it runs out of registers.
+DEV uint32_t hidden(uint32_t v) {
+  asm("" : "+v"(v));
+  return v;
+}
+DEV uint32_t behind(uint32_t v, f4 f) {
+  asm("" : "+v"(v) : "v"(f));
+  return v;
 }
 // over the four lanes of a query
 DEV float max4(float v) {
@@ -304,15 +319,16 @@ extern "C" __device__ float legacy_mul(float, float) __asm("llvm.amdgcn.fmul.leg
 
 struct AttendPlace { uint32_t b, hk, tile, piece, part; bool there; };
 DEV AttendPlace attend_place(const AttendArgs& a) {
-  // Workgroups go to the eight dies in turn.  All heads of a piece (and all its tiles of queries) go to one die, one behind the other:
-  // heads that lie together share lines of the cache and of its scales there.
+  // Workgroups go to the eight dies in turn; `inner` that follow each other here go to one (the rule is at the packing): heads that lie
+  // together share lines of the cache and of its scales, queries of a head all of it.
   AttendPlace p;
-  const uint32_t die = blockIdx.x & 7u, k = blockIdx.x >> 3, o = divided(k, a.by_inner), inner = k - o * (a.hk * a.tiles), outer = o * 8u + die;
-  p.there = outer < a.b * a.pieces;
-  p.b = divided(outer, a.by_pieces);
-  p.piece = outer - p.b * a.pieces;
-  p.hk = divided(inner, a.by_tiles);
-  const uint32_t tile = inner - p.hk * a.tiles;
+  const uint32_t die = blockIdx.x & 7u, k = blockIdx.x >> 3, o = divided(k, a.by_inner), outer = o * 8u + die;
+  const uint32_t id = outer * a.inner + (k - o * a.inner), head = divided(id, a.by_tiles), part = divided(head, a.by_hk);
+  p.there = id < a.blocks;
+  p.b = divided(part, a.by_pieces);
+  p.piece = part - p.b * a.pieces;
+  p.hk = head - part * a.hk;
+  const uint32_t tile = id - head * a.tiles;
   p.tile = tile >> a.lg_parts;
   p.part = tile - (p.tile << a.lg_parts);
   return p;
@@ -326,18 +342,29 @@ constexpr uint32_t kSlab = 4096;
 typedef int i2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i2* lds_i2;
 
+// LDS: the queries' parts; for each wavefront a slab, where rows lie (two tiles, keys and values), scales; or, in their place, sums to be joined.
+// Dynamic, because the compiler goes by what it knows of LDS when it chooses how many registers to take: with 45 KB it took 168, and a
+// workgroup has to fit into the 128 (and the 69,808 bytes) that a worker of three workgroups a compute unit leaves.
+constexpr uint32_t attend_wave_lds(uint32_t dp, bool multi) { return kSlab + 2048u + (multi ? dp / 32u : 1u) * 512u; }
+constexpr uint32_t attend_q_lds(uint32_t dp, uint32_t dt) { return (dt == GPUOS_BF16 ? 1u : (dt == GPUOS_F16 ? 2u : 3u)) * (dp / 32u) * 1024u; }
+constexpr uint32_t attend_lds(uint32_t dp, uint32_t dt, bool multi) {
+  const uint32_t loop = attend_q_lds(dp, dt) + 4u * attend_wave_lds(dp, multi), join = 2u * 16u * (dp < 128u ? dp : 128u) * 4u + 512u;
+  return loop > join ? loop : join;
+}
+static_assert(attend_lds(256, GPUOS_F32, true) <= 65536u, "what a launch may ask for");
+
 // DP: elements of a head that there is room for; FULL: a head has as many; MULTI: more than one scale a row.  Of 256 elements a workgroup has
 // all of the scores but one half of the results: with all of those it would not fit into 128 registers (below).
 template <uint32_t FMT, uint32_t DP, bool FULL, uint32_t DT, bool MULTI>
-__global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(128))) gpuos_cache_attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const AttendArgs a) {
   constexpr uint32_t BITS = Code<FMT>::BITS, ROW = DP * BITS / 8u, NS = ROW < 64u ? 1u : ROW / 64u, DS = DP / NS;      // slabs; elements of one
   constexpr uint32_t DV = DP < 128u ? DP : 128u, NV = NS * DV / DP;            // elements of a result that a workgroup has; slabs of them
   constexpr uint32_t CH = ROW < 64u ? ROW / 16u : 4u, IT = CH, KS = DS / 32u, MT = DS / 16u;      // pieces of a row; loads of a lane; steps, tiles of a slab
   constexpr uint32_t NQ = DT == GPUOS_BF16 ? 1u : (DT == GPUOS_F16 ? 2u : 3u), NP = DT == GPUOS_F32 ? 3u : 2u;
   constexpr uint32_t GROUPS = MULTI ? DP / 32u : 1u;
-  constexpr uint32_t WAVE_LDS = kSlab + 2048u + GROUPS * 512u, Q_LDS = NQ * (DP / 32u) * 1024u, JOIN_LDS = 2u * 16u * DV * 4u + 512u;
-  constexpr uint32_t LDS = Q_LDS + 4u * WAVE_LDS > JOIN_LDS ? Q_LDS + 4u * WAVE_LDS : JOIN_LDS;
-  __shared__ alignas(16) uint8_t lds[LDS];
+  constexpr bool STEPS = MULTI || BITS == 8u || NP == 3u;
+  constexpr uint32_t WAVE_LDS = attend_wave_lds(DP, MULTI), Q_LDS = attend_q_lds(DP, DT);
+  extern __shared__ uint8_t lds[];                                 // attend_lds(DP, DT, MULTI) bytes
   const AttendPlace at = attend_place(a);
   if (!at.there) return;
   const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u, n = lane & 15u, g = lane >> 4;
@@ -355,9 +382,14 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
   const int32_t pos_first = past + (int32_t)divided(r0, a.by_per), pos_last = past + (int32_t)divided(rl, a.by_per);
   const uint32_t row = r0 + n;
   const bool has_row = row < a.rows;
-  const uint32_t qs = divided(has_row ? row : r0, a.by_per), qh = (has_row ? row : r0) - qs * a.per;
+  const auto query = [&](uint32_t& qs, uint32_t& qh) {             // the lane's query: of S, of the heads that share one of keys
+    const uint32_t r = hidden(has_row ? row : r0);
+    qs = divided(r, a.by_per);
+    qh = r - qs * a.per;
+  };
+  uint32_t qs, qh;
+  query(qs, qh);
   const int32_t pos = past + (int32_t)qs;
-  const int32_t see_from = a.window != 0 ? pos - (int32_t)a.window + 1 : 0;      // this lane's query sees [see_from, pos]
   int32_t from = a.window != 0 ? pos_first - (int32_t)a.window + 1 : 0;
   from = from < 0 ? 0 : from;
   const int32_t end = pos_last + 1;
@@ -419,9 +451,11 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
       const uint64_t sp = a.kv[v].scales + ((uint64_t)at.hk * a.kv[v].ss[2] + e * a.kv[v].ss[0] + (uint64_t)in * a.kv[v].ss[1]) * 4u;
 #pragma unroll
       for (uint32_t q = 0; q < GROUPS; ++q) {
-        float f = !MULTI || q * a.group < d ? ld<float>(sp + (uint64_t)q * a.kv[v].ss[3] * 4u) : 0.0f;
+        float f = 0.0f;                                            // (of more than one scale: that of each 32 elements)
+        if (FULL || !MULTI || 32u * q < d) f = ld<float>(sp + (uint64_t)(MULTI ? divided(32u * q, a.by_group) : 0u) * a.kv[v].ss[3] * 4u);
         if (!known) f = __builtin_nanf("");                        // a page that is not in the cache
-        (v ? vs : ks)[q] = f;
+        if (v) vs[q] = f;
+        else ks[q] = f;
       }
     }
   };
@@ -446,7 +480,6 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
   };
   // Places in LDS: of piece c of row t, 64 t + 16 (c ^ swizzle(t)).  Those of a lane differ by an exclusive or and a constant from the first,
   // which is hidden from the compiler: it would keep them all in registers.
-  const auto hidden = [](uint32_t v) { asm("" : "+v"(v)); return v; };
   const auto slab_at = [&](uint32_t t, uint32_t c, uint32_t more) { return 64u * t + 16u * (c ^ swizzle(t)) + more; };
   const uint32_t put_at = slab_at(lane / CH, lane & (CH - 1u), 0);
   const uint32_t key_at = BITS == 4u ? slab_at(n, 0, 4u * g) : slab_at(n, g >> 1, 8u * (g & 1u));
@@ -487,36 +520,33 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
       wave_sync();
       if (s + 1u < NS) ask(buf, 0, s + 1u);
       else ask(buf, 1, first_slab);
-      const uint32_t ko = hidden(key_at);
+      uint32_t ko = hidden(key_at);
 #pragma unroll
       for (uint32_t j = 0; j < KS; ++j) {
-        const uint32_t e = s * DS + 32u * j;                       // the step's first element
-        if (FULL || e < d) {
-          bf8 q[NQ];
+        const uint32_t e = s * DS + 32u * j;                       // the step's first element (behind the head's last, all are 0)
+        bf8 q[NQ];
 #pragma unroll
-          for (uint32_t k = 0; k < NQ; ++k) q[k] = qf[(k * (DP / 32u) + e / 32u) * 64u + lane];
+        for (uint32_t k = 0; k < NQ; ++k) q[k] = qf[(k * (DP / 32u) + e / 32u) * 64u + lane];
+#pragma unroll
+        for (uint32_t T = 0; T < 4; ++T) {
+          bf8 k;
+          const uint8_t* const kp = slab + 1024u * T + (ko ^ (((j * (BITS / 4u)) ^ T) << 4));
+          if constexpr (BITS == 4u) k = eight_of<FMT>(*(const uint32_t*)kp, 0u);
+          else {
+            const u2 w = *(const u2*)kp;
+            k = eight_of<FMT>(w[0], w[1]);
+          }
+#pragma unroll
+          for (uint32_t z = 0; z < NQ; ++z) c[T] = mfma(k, q[z], c[T]);
+        }
+        if (MULTI) {
 #pragma unroll
           for (uint32_t T = 0; T < 4; ++T) {
-            bf8 k;
-            const uint8_t* const kp = slab + 1024u * T + (ko ^ (((j * (BITS / 4u)) ^ T) << 4));
-            if constexpr (BITS == 4u) {
-              const uint32_t w = *(const uint32_t*)kp;
-              k = frag(pair_of<FMT, 0>(w), pair_of<FMT, 1>(w), pair_of<FMT, BITS == 4u ? 2 : 0>(w), pair_of<FMT, BITS == 4u ? 3 : 0>(w));
-            } else {
-              const u2 w = *(const u2*)kp;
-              k = frag(pair_of<FMT, 0>(w[0]), pair_of<FMT, 1>(w[0]), pair_of<FMT, 0>(w[1]), pair_of<FMT, 1>(w[1]));
-            }
+            const f4 f = *(const f4*)(sc + (2u * (e / 32u)) * 64u + 16u * T + 4u * g);
 #pragma unroll
-            for (uint32_t z = 0; z < NQ; ++z) c[T] = mfma(k, q[z], c[T]);
-          }
-          if (MULTI && (e + 32u) % a.group == 0u) {
-#pragma unroll
-            for (uint32_t T = 0; T < 4; ++T) {
-              const f4 f = *(const f4*)(sc + (2u * (e / a.group)) * 64u + 16u * T + 4u * g);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) x[T][i] = __builtin_fmaf(c[T][i], f[i], x[T][i]);
-              c[T] = f4{0, 0, 0, 0};
-            }
+            for (int i = 0; i < 4; ++i) x[T][i] = __builtin_fmaf(c[T][i], f[i], x[T][i]);
+            c[T] = f4{0, 0, 0, 0};
+            ko = behind(ko, x[T]);
           }
         }
       }
@@ -530,12 +560,13 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
       x[T] *= a.scale;
     }
     if (t < all_from || t + 63 > pos_first || t + 64 > t1) {       // some query does not see all of these
+      const int32_t see_from = a.window != 0 ? pos - (int32_t)a.window + 1 : 0;
 #pragma unroll
       for (int T = 0; T < 4; ++T) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int32_t k = t + 16 * T + (int32_t)(4u * g) + i;
-          x[T][i] = k < t1 && k <= pos && k >= see_from ? x[T][i] : -__builtin_inff();
+          x[T][i] = k < t1 && k <= pos && k >= see_from ? x[T][i] : -__builtin_inff();      // (its query sees [see_from, pos])
         }
       }
     }
@@ -562,29 +593,26 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
     }
 
     // weights: 2^(x - m) times the scale of the row's group, in parts
-    bf8 w[NP][2];
-    const auto weights = [&](uint32_t group) {
+    bf8 w[2][NP];
+    const auto weights = [&](uint32_t group, uint32_t u, uint32_t g4, bf8 (&to)[NP]) {
+      float f[8];
 #pragma unroll
-      for (uint32_t u = 0; u < 2; ++u) {
-        float f[8];
+      for (uint32_t T = 0; T < 2; ++T) {
+        const f4 v = *(const f4*)(sc + (2u * group + 1u) * 64u + 16u * (2u * u + T) + g4);
 #pragma unroll
-        for (uint32_t T = 0; T < 2; ++T) {
-          const f4 v = *(const f4*)(sc + (2u * group + 1u) * 64u + 16u * (2u * u + T) + 4u * g);
+        for (int i = 0; i < 4; ++i) f[4 * T + i] = legacy_mul(x[2u * u + T][i], v[i]);
+      }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[4 * T + i] = legacy_mul(x[2u * u + T][i], v[i]);
+      for (uint32_t k = 0; k < NP; ++k) {
+        u4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          typedef float f2 __attribute__((ext_vector_type(2)));
+          v[i] = k + 1u < NP ? high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1])) : bits_of(__builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), bf2));
         }
+        to[k] = __builtin_bit_cast(bf8, v);
 #pragma unroll
-        for (uint32_t k = 0; k < NP; ++k) {
-          u4 v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            typedef float f2 __attribute__((ext_vector_type(2)));
-            v[i] = k + 1u < NP ? high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1])) : bits_of(__builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), bf2));
-          }
-          w[k][u] = __builtin_bit_cast(bf8, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = f[i] - upper(f[i]);
-        }
+        for (int i = 0; i < 8; ++i) f[i] = f[i] - upper(f[i]);
       }
     };
 #pragma unroll
@@ -621,31 +649,43 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
         ask(buf ^ 1u, 0, 0);
         entry = look(t + 512);
       }
-      if (!MULTI && s == 0u) weights(0);
-      const uint32_t vo = hidden(value_at);
+      // The two steps of a tile of results together, two tiles at a time, as one waits for the other; or (STEPS) one step after the other, so that
+      // only one step's weights are held.
+      if (!MULTI && !STEPS && s == 0u) {
+        weights(0, 0, 4u * g, w[0]);
+        weights(0, 1, 4u * g, w[1]);
+      }
 #pragma unroll
-      for (uint32_t j = 0; j < MT; ++j) {
-        const uint32_t e = first_e + s * DS + 16u * j;             // the tile's first element
-        if (FULL || e < d) {
-          if (MULTI && e % a.group == 0u) weights(e / a.group);
-          f4& o = acc[s * MT + j];
-          bf8 v[2];
-          if constexpr (BITS == 4u) {
-            const i2 y = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2)(slab + (vo ^ ((j >> 1) << 4)) + 8u * (j & 1u)));
+      for (uint32_t uu = 0; uu < (STEPS ? 2u : 1u); ++uu) {
+        const uint32_t vo = STEPS && uu == 1u ? behind(value_at, acc[s * MT + MT - 1u]) : hidden(value_at);
+        if (!MULTI && STEPS) weights(0, uu, uu == 1u ? behind(4u * g, acc[s * MT + MT - 1u]) : hidden(4u * g), w[0]);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-              v[u] = frag(pair_of<FMT, 0>((uint32_t)y[u]), pair_of<FMT, 1>((uint32_t)y[u]), pair_of<FMT, BITS == 4u ? 2 : 0>((uint32_t)y[u]), pair_of<FMT, BITS == 4u ? 3 : 0>((uint32_t)y[u]));
-          } else {
+        for (uint32_t j = 0; j < MT; j += 2) {
+          const uint32_t e = first_e + s * DS + 16u * j;           // the tile's first element
+          if constexpr (MULTI) weights(e / 32u, uu, j >= 2u ? behind(4u * g, acc[s * MT + j - 1u]) : hidden(4u * g), w[0]);
+          bf8 v[2][2];                                           // [tile][step]
 #pragma unroll
-            for (uint32_t u = 0; u < 2; ++u) {
-              const i2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2)(slab + 2048u * u + (vo ^ ((j ^ (2u * u)) << 4))));
-              v[u] = frag(pair_of<FMT, 0>((uint32_t)y[0]), pair_of<FMT, 1>((uint32_t)y[0]), pair_of<FMT, 0>((uint32_t)y[1]), pair_of<FMT, 1>((uint32_t)y[1]));
+          for (uint32_t i = 0; i < 2; ++i) {
+            if constexpr (BITS == 4u) {
+              const i2 y = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2)(slab + (vo ^ ((j >> 1) << 4)) + 8u * i));
+#pragma unroll
+              for (uint32_t u = 0; u < (STEPS ? 1u : 2u); ++u) v[i][u] = eight_of<FMT>((uint32_t)y[STEPS ? uu : u], 0u);
+            } else {
+#pragma unroll
+              for (uint32_t u = 0; u < (STEPS ? 1u : 2u); ++u) {
+                const uint32_t step = STEPS ? uu : u;
+                const i2 y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2)(slab + 2048u * step + (vo ^ (((j + i) ^ (2u * step)) << 4))));
+                v[i][u] = eight_of<FMT>((uint32_t)y[0], (uint32_t)y[1]);
+              }
             }
           }
 #pragma unroll
           for (uint32_t k = 0; k < NP; ++k) {
-            o = mfma(v[0], w[k][0], o);
-            o = mfma(v[1], w[k][1], o);
+#pragma unroll
+            for (uint32_t u = 0; u < (STEPS ? 1u : 2u); ++u) {
+#pragma unroll
+              for (uint32_t i = 0; i < 2; ++i) acc[s * MT + j + i] = mfma(v[i][u], w[u][k], acc[s * MT + j + i]);
+            }
           }
         }
       }
@@ -690,6 +730,7 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
   }
   if (wave != 0u || !has_row) return;
   const bool last = a.pieces == 1u;
+  query(qs, qh);
   const float inv = last ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
   const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(at.hk * a.per + qh) * a.os[2]) * size_of(DT);
   const uint64_t all = (uint64_t)a.b * a.hk * a.rows, mine = ((uint64_t)at.b * a.hk + at.hk) * a.rows + row, slice = (uint64_t)at.piece * all + mine;
@@ -715,49 +756,78 @@ __global__ void __launch_bounds__(kThreads, 4) __attribute__((amdgpu_num_vgpr(12
   }
 }
 
-// The pieces' sums: a workgroup has a query; each of its wavefronts adds every fourth piece.
-template <uint32_t DT> __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_join_kernel(const AttendArgs a) {
-  __shared__ alignas(16) float lds[4 * 260];
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u, mine = blockIdx.x;
+// The pieces' sums: a workgroup has a query, each of its wavefronts adds every so many pieces, eight on their way at a time.
+constexpr uint32_t kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
+template <uint32_t DT> __global__ void __launch_bounds__(kJoinThreads, 8) gpuos_cache_join_kernel(const AttendArgs a) {
+  __shared__ alignas(16) float weight[kPiecesMost], sums[kJoinWaves][256], tops[kJoinWaves], totals[kJoinWaves];
+  const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u, mine = blockIdx.x;
   const uint64_t all = (uint64_t)a.b * a.hk * a.rows;
-  float most = -__builtin_inff();
-  for (uint32_t k = lane; k < a.pieces; k += 64u) most = __builtin_fmaxf(most, ld<float>(a.stats + (k * all + mine) * 8u));
-  for (int w = 32; w >= 1; w /= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w, 64));
-  const float ref = most == -__builtin_inff() ? 0.0f : most;
-  float sum[4] = {0, 0, 0, 0}, total = 0.0f;
-  for (uint32_t k = wave; k < a.pieces; k += 4u) {
-    const uint64_t slice = k * all + mine;
-    const float l = ld<float>(a.stats + slice * 8u + 4u), by = __builtin_amdgcn_exp2f(ld<float>(a.stats + slice * 8u) - ref);
-    if (l == 0.0f) continue;                                       // (an empty piece: its sums were not written)
-    total += l * by;
+  static_assert(kPiecesMost <= kJoinThreads, "a thread for each piece");
+  float m = -__builtin_inff(), l = 0.0f;
+  if (tid < a.pieces) {
+    const u2 v = ld<u2_any>(a.stats + (tid * all + mine) * 8u);
+    m = as_f(v[0]);
+    l = as_f(v[1]);
+  }
+  float top = m;
+  for (int w = 32; w >= 1; w /= 2) top = __builtin_fmaxf(top, __shfl_xor(top, w, 64));
+  if (lane == 0u) tops[wave] = top;
+  __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      if (lane + 64u * i < a.d) sum[i] += ld<float>(a.part + (slice * a.d + lane + 64u * i) * 4u) * by;
+  for (uint32_t k = 0; k < kJoinWaves; ++k) top = __builtin_fmaxf(top, tops[k]);
+  const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
+  float total = l == 0.0f ? 0.0f : l * by;
+  if (tid < kPiecesMost) weight[tid] = l == 0.0f ? -1.0f : by;       // (an empty piece: its sums were not written)
+  for (int w = 32; w >= 1; w /= 2) total += __shfl_xor(total, w, 64);
+  if (lane == 0u) totals[wave] = total;
+  __syncthreads();
+  total = 0.0f;
+#pragma unroll
+  for (uint32_t k = 0; k < kJoinWaves; ++k) total += totals[k];
+  f4 sum = {0, 0, 0, 0};
+  const bool has = 4u * lane < a.d;
+  const uint64_t from = a.part + ((uint64_t)mine * a.d + (has ? 4u * lane : 0u)) * 4u;
+  for (uint32_t k0 = wave; k0 < a.pieces; k0 += 8u * kJoinWaves) {
+    f4 v[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      v[i] = f4{0, 0, 0, 0};
+      const uint32_t k = k0 + i * kJoinWaves;
+      if (has && k < a.pieces) v[i] = __builtin_bit_cast(f4, ld<u4_any>(from + (uint64_t)k * all * a.d * 4u));
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t k = k0 + i * kJoinWaves;
+      const float w = k < a.pieces ? weight[k] : -1.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += w < 0.0f ? 0.0f : v[i][e] * w;
     }
   }
-#pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) lds[wave * 260u + lane + 64u * i] = sum[i];
-  if (lane == 0u) lds[wave * 260u + 256u] = total;
+  *(f4*)&sums[wave][4u * lane] = sum;
   __syncthreads();
-  total = (lds[256] + lds[260 + 256]) + (lds[520 + 256] + lds[780 + 256]);
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   const uint32_t pair = divided(mine, a.by_rows), row = mine - pair * a.rows, b = divided(pair, a.by_hk), hk = pair - b * a.hk;
   const uint32_t qs = divided(row, a.by_per), qh = row - qs * a.per;
   const uint64_t op = a.out + ((uint64_t)b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(hk * a.per + qh) * a.os[2]) * size_of(DT);
-  const uint32_t e = threadIdx.x;
-  if (e < a.d) st_elem<DT>(op + (uint64_t)e * a.os[3] * size_of(DT), ((lds[e] + lds[260 + e]) + (lds[520 + e] + lds[780 + e])) * inv);
+  if (tid < a.d) {
+    float o = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < kJoinWaves; ++k) o += sums[k][tid];
+    st_elem<DT>(op + (uint64_t)tid * a.os[3] * size_of(DT), o * inv);
+  }
 }
 
-template <uint32_t FMT, uint32_t DT, bool MULTI> const void* attend_kernel(uint32_t d) {
+struct AttendKernel { const void* kernel; uint32_t lds; };
+template <uint32_t FMT, uint32_t DT, bool MULTI> AttendKernel attend_kernel(uint32_t d) {
   if constexpr (DT != GPUOS_F32) {
-    if (d == 64u) return (const void*)gpuos_cache_attend_kernel<FMT, 64, true, DT, MULTI>;
-    if (d == 128u) return (const void*)gpuos_cache_attend_kernel<FMT, 128, true, DT, MULTI>;
-    if (d == 256u) return (const void*)gpuos_cache_attend_kernel<FMT, 256, true, DT, MULTI>;
+    if (d == 64u) return {(const void*)gpuos_cache_attend_kernel<FMT, 64, true, DT, MULTI>, attend_lds(64, DT, MULTI)};
+    if (d == 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, true, DT, MULTI>, attend_lds(128, DT, MULTI)};
+    if (d == 256u) return {(const void*)gpuos_cache_attend_kernel<FMT, 256, true, DT, MULTI>, attend_lds(256, DT, MULTI)};
   }
-  if (d <= 128u) return (const void*)gpuos_cache_attend_kernel<FMT, 128, false, DT, MULTI>;
-  return (const void*)gpuos_cache_attend_kernel<FMT, 256, false, DT, MULTI>;
+  if (d <= 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, false, DT, MULTI>, attend_lds(128, DT, MULTI)};
+  return {(const void*)gpuos_cache_attend_kernel<FMT, 256, false, DT, MULTI>, attend_lds(256, DT, MULTI)};
 }
-template <uint32_t FMT> const void* attend_kernel(uint32_t dt, uint32_t d, bool multi) {
+template <uint32_t FMT> AttendKernel attend_kernel(uint32_t dt, uint32_t d, bool multi) {
   if (dt == GPUOS_F32) return multi ? attend_kernel<FMT, GPUOS_F32, true>(d) : attend_kernel<FMT, GPUOS_F32, false>(d);
   if (dt == GPUOS_F16) return multi ? attend_kernel<FMT, GPUOS_F16, true>(d) : attend_kernel<FMT, GPUOS_F16, false>(d);
   return multi ? attend_kernel<FMT, GPUOS_BF16, true>(d) : attend_kernel<FMT, GPUOS_BF16, false>(d);
@@ -765,13 +835,13 @@ template <uint32_t FMT> const void* attend_kernel(uint32_t dt, uint32_t d, bool 
 
 int launch_attend(const AttendArgs& a, uint32_t format, void* stream) {
   const bool multi = a.group != a.d;
-  const void* kernel = format == CF_E2M1 ? attend_kernel<CF_E2M1>(a.dtype, a.d, multi) : (format == CF_I8 ? attend_kernel<CF_I8>(a.dtype, a.d, multi) : attend_kernel<CF_E4M3>(a.dtype, a.d, multi));
+  const AttendKernel k = format == CF_E2M1 ? attend_kernel<CF_E2M1>(a.dtype, a.d, multi) : (format == CF_I8 ? attend_kernel<CF_I8>(a.dtype, a.d, multi) : attend_kernel<CF_E4M3>(a.dtype, a.d, multi));
   void* args[] = {(void*)&a};
-  const uint32_t outer = (a.b * a.pieces + 7u) / 8u * 8u;
-  const int rc = (int)hipLaunchKernel(kernel, dim3(outer * a.hk * a.tiles), dim3(kThreads), args, 0, (hipStream_t)stream);
+  const uint32_t outer = (a.blocks / a.inner + 7u) / 8u * 8u;
+  const int rc = (int)hipLaunchKernel(k.kernel, dim3(outer * a.inner), dim3(kThreads), args, k.lds, (hipStream_t)stream);
   if (rc != (int)hipSuccess || a.pieces == 1u) return rc;
   const void* const joins[] = {(const void*)gpuos_cache_join_kernel<GPUOS_F32>, (const void*)gpuos_cache_join_kernel<GPUOS_F16>, (const void*)gpuos_cache_join_kernel<GPUOS_BF16>};
-  return (int)hipLaunchKernel(joins[a.dtype], dim3(a.b * a.hk * a.rows), dim3(kThreads), args, 0, (hipStream_t)stream);
+  return (int)hipLaunchKernel(joins[a.dtype], dim3(a.b * a.hk * a.rows), dim3(kJoinThreads), args, 0, (hipStream_t)stream);
 }
 
 }  // namespace gpuos

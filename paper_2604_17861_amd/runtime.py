@@ -123,7 +123,7 @@ def lib():
 
 
 EXPORTS = ["gpuos_default_config", "gpuos_init", "gpuos_init_static", "gpuos_register_op", "gpuos_swap_op", "gpuos_submit", "gpuos_submit_flush",
-           "gpuos_submit_model", "gpuos_launch_model", "gpuos_model_plan", "gpuos_flush", "gpuos_wait", "gpuos_get_completions", "gpuos_peek_queue",
+           "gpuos_submit_model", "gpuos_launch_model", "gpuos_model_plan", "gpuos_launch_cache", "gpuos_cache_workspace", "gpuos_flush", "gpuos_wait", "gpuos_get_completions", "gpuos_peek_queue",
            "gpuos_worker_alive", "gpuos_set_yield_every", "gpuos_shutdown", "gpuos_stop_worker", "gpuos_start_worker",
            "gpuos_worker_elapsed_ms", "gpuos_worker_stats", "gpuos_run_serial", "gpuos_launch_per_op", "gpuos_task_bytes", "gpuos_task_plan", "gpuos_device_info", "gpuos_define_program", "gpuos_native_info", "gpuos_submit_from_threads", "gpuos_get_trace", "gpuos_op_counts",
            "gpuos_trace_origin", "gpuos_kill_op", "gpuos_audit_log", "gpuos_strerror",
