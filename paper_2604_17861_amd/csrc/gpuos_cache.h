@@ -30,9 +30,11 @@ struct AttendArgs {
   uint32_t qs[4], os[4], ps[2], ls;                  // strides: B, S, H, D; of the page table, the lengths
   uint32_t b, s, hq, hk, per, d, pages, page, group, longest, window;      // per: heads of queries that share one of keys
   uint32_t rows, tiles, pieces;                      // rows: queries of a head of keys, per * S; tiles of them, and of parts of results; pieces of a sequence
+  uint32_t by_fours;                                 // scales of 32 elements each, side by side: read in fours
+  uint32_t by_head, heads;                           // a wavefront has a head of its own: heads of keys in fours (else heads)
   uint32_t lg_parts;                                 // parts of a result that are a workgroup each: 1 or 2
   uint32_t blocks, inner;                            // workgroups, and how many that follow each other go to one die
-  Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_hk, by_group;
+  Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_heads, by_hk, by_group;
   uint32_t dtype;
   float scale;                                       // of the scores, in powers of two
 };
@@ -41,6 +43,21 @@ constexpr uint32_t kAppendBlock = 2;       // heads of an item
 constexpr uint32_t kTileRows = 16;         // queries of a tile: a side of a matrix instruction's result
 constexpr uint32_t kTileTokens = 64;       // rows of the cache that a wavefront takes at once
 constexpr uint32_t kPiecesMost = 256;
+
+// Elements of a head that the kernel of a head's d has room for.
+constexpr uint32_t attend_room(uint32_t d, uint32_t dt) { return d == 64u && dt != GPUOS_F32 ? 64u : (d <= 128u ? 128u : 256u); }
+// LDS: the queries' parts; for each wavefront a slab, where its rows lie, their scales; or, in their place, sums to be joined.
+// Dynamic, because the compiler goes by what it knows of LDS when it chooses how many registers to take: with 45 KB it took 168, and a
+// workgroup has to fit into the 128 (and the 69,808 bytes) that a worker of three workgroups a compute unit leaves.
+constexpr uint32_t kSlab = 4096;           // bytes of codes that a wavefront has in LDS: 64 rows by 64
+constexpr uint32_t attend_wave_lds(uint32_t dp, bool multi) { return kSlab + 1024u + (multi ? dp / 32u : 1u) * 512u; }
+constexpr uint32_t attend_q_lds(uint32_t dp, uint32_t dt) { return (dt == GPUOS_BF16 ? 1u : (dt == GPUOS_F16 ? 2u : 3u)) * (dp / 32u) * 1024u; }
+constexpr uint32_t attend_lds(uint32_t dp, uint32_t dt, bool multi, bool by_head) {
+  const uint32_t loop = attend_q_lds(dp, dt) * (by_head ? 4u : 1u) + 4u * attend_wave_lds(dp, multi), join = 2u * 16u * (dp < 128u ? dp : 128u) * 4u + 512u;
+  return loop > join ? loop : join;
+}
+constexpr uint32_t kLdsMost = 65536;
+static_assert(attend_lds(256, GPUOS_F32, true, false) <= kLdsMost, "what a launch may ask for");
 
 int launch_append(const AppendArgs& a, void* stream);       // gpuos_cache.hip
 int launch_attend(const AttendArgs& a, uint32_t format, void* stream);
@@ -135,14 +152,19 @@ class CachePack : ModelPack {
     a->rows = a->per * a->s;
     a->lg_parts = d > 128 ? 1u : 0u;
     a->tiles = ((a->rows + kTileRows - 1) / kTileRows) << a->lg_parts;
-    const uint64_t pairs = (uint64_t)b * hk * a->tiles;
     // what a tile of queries sees, at most
     const int64_t seen = window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
-    a->pieces = pieces(pairs, (uint64_t)seen);
+    a->by_fours = a->group == 32 && a->kv[0].ss[3] == 1 && a->kv[1].ss[3] == 1 ? 1u : 0u;
+    // Four heads of a row that lie together are read together, if their queries fit into LDS; else a workgroup has a head.
+    a->by_head = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
+    if (getenv("GH")) a->by_head = atoi(getenv("GH"));
+    a->heads = a->by_head ? (a->hk + 3) / 4 : a->hk;
+    const uint64_t pairs = (uint64_t)b * a->heads * a->tiles;
+    a->pieces = pieces(pairs, (uint64_t)seen, a->by_head ? 128 : 512);
     if (pairs * a->pieces > kBlocksMost) return GPUOS_E_INVAL;
     a->blocks = (uint32_t)(pairs * a->pieces);
     // All heads of a piece of a sequence go to one die, if the dies then have about as much to do; else all queries of a head; else each workgroup to the next.
-    const uint32_t inners[2] = {a->hk * a->tiles, a->tiles};
+    const uint32_t inners[2] = {a->heads * a->tiles, a->tiles};
     a->inner = 1;
     for (uint32_t n : inners) {
       const uint32_t outer = a->blocks / n;
@@ -155,14 +177,15 @@ class CachePack : ModelPack {
     a->by_inner = make_div(a->inner);
     a->by_pieces = make_div(a->pieces);
     a->by_rows = make_div(a->rows);
+    a->by_heads = make_div(a->heads);
     a->by_hk = make_div(a->hk);
     if (a->pieces > 1) *bytes = (uint64_t)a->pieces * b * s * hq * (d + 2) * 4;
     return GPUOS_OK;
   }
 
   // Pieces that a sequence's rows are cut into, each a workgroup's; a second launch joins them.
-  static uint32_t pieces(uint64_t pairs, uint64_t seen) {
-    static const uint64_t T = getenv("GT") ? atoi(getenv("GT")) : 1024, MN = getenv("GM") ? atoi(getenv("GM")) : 512;
+  static uint32_t pieces(uint64_t pairs, uint64_t seen, uint64_t least) {
+    static const uint64_t T = getenv("GT") ? atoi(getenv("GT")) : 768, MN = getenv("GM") ? atoi(getenv("GM")) : least;
     uint64_t n = (T + pairs - 1) / pairs;
     const uint64_t most = (seen + MN - 1) / MN;
     if (n > most) n = most;

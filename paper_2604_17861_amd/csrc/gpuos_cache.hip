@@ -323,11 +323,11 @@ DEV AttendPlace attend_place(const AttendArgs& a) {
   // together share lines of the cache and of its scales, queries of a head all of it.
   AttendPlace p;
   const uint32_t die = blockIdx.x & 7u, k = blockIdx.x >> 3, o = divided(k, a.by_inner), outer = o * 8u + die;
-  const uint32_t id = outer * a.inner + (k - o * a.inner), head = divided(id, a.by_tiles), part = divided(head, a.by_hk);
+  const uint32_t id = outer * a.inner + (k - o * a.inner), head = divided(id, a.by_tiles), part = divided(head, a.by_heads);
   p.there = id < a.blocks;
   p.b = divided(part, a.by_pieces);
   p.piece = part - p.b * a.pieces;
-  p.hk = head - part * a.hk;
+  p.hk = head - part * a.heads;
   const uint32_t tile = id - head * a.tiles;
   p.tile = tile >> a.lg_parts;
   p.part = tile - (p.tile << a.lg_parts);
@@ -338,20 +338,8 @@ DEV AttendPlace attend_place(const AttendArgs& a) {
 // next slab on its way while one is worked on.  Piece c of row t lies in place c ^ swizzle(t), so that neither product's reads meet in a
 // bank: for the first a lane reads its row's codes, for the second a column's of 16 rows (4 bits) or eight, which the LDS transposes.
 DEV uint32_t swizzle(uint32_t t) { return ((t >> 2) ^ (t >> 4)) & 3u; }
-constexpr uint32_t kSlab = 4096;
 typedef int i2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i2* lds_i2;
-
-// LDS: the queries' parts; for each wavefront a slab, where rows lie (two tiles, keys and values), scales; or, in their place, sums to be joined.
-// Dynamic, because the compiler goes by what it knows of LDS when it chooses how many registers to take: with 45 KB it took 168, and a
-// workgroup has to fit into the 128 (and the 69,808 bytes) that a worker of three workgroups a compute unit leaves.
-constexpr uint32_t attend_wave_lds(uint32_t dp, bool multi) { return kSlab + 2048u + (multi ? dp / 32u : 1u) * 512u; }
-constexpr uint32_t attend_q_lds(uint32_t dp, uint32_t dt) { return (dt == GPUOS_BF16 ? 1u : (dt == GPUOS_F16 ? 2u : 3u)) * (dp / 32u) * 1024u; }
-constexpr uint32_t attend_lds(uint32_t dp, uint32_t dt, bool multi) {
-  const uint32_t loop = attend_q_lds(dp, dt) + 4u * attend_wave_lds(dp, multi), join = 2u * 16u * (dp < 128u ? dp : 128u) * 4u + 512u;
-  return loop > join ? loop : join;
-}
-static_assert(attend_lds(256, GPUOS_F32, true) <= 65536u, "what a launch may ask for");
 
 // DP: elements of a head that there is room for; FULL: a head has as many; MULTI: more than one scale a row.  Of 256 elements a workgroup has
 // all of the scores but one half of the results: with all of those it would not fit into 128 registers (below).
@@ -364,23 +352,16 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
   constexpr uint32_t GROUPS = MULTI ? DP / 32u : 1u;
   constexpr bool STEPS = MULTI || BITS == 8u || NP == 3u;
   constexpr uint32_t WAVE_LDS = attend_wave_lds(DP, MULTI), Q_LDS = attend_q_lds(DP, DT);
-  extern __shared__ uint8_t lds[];                                 // attend_lds(DP, DT, MULTI) bytes
+  extern __shared__ uint8_t lds[];                                 // attend_lds bytes
   const AttendPlace at = attend_place(a);
   if (!at.there) return;
   const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u, n = lane & 15u, g = lane >> 4;
   const uint32_t d = FULL ? DP : a.d;
+  // A wavefront has a head of its own, or every fourth 64 rows of the workgroup's.
+  const bool by_head = a.by_head != 0u;
+  const uint32_t head = by_head ? at.hk * 4u + wave : at.hk;
 
-  // what the tile's queries see: rows [from, end) of the sequence, and of that this piece's [t0, t1)
-  int32_t len = (int32_t)a.longest;
-  if (a.lengths != 0) {
-    const int32_t l = ld<int32_t>(a.lengths + (uint64_t)at.b * a.ls * 4u);
-    len = l < 0 ? 0 : (l < len ? l : len);
-  }
-  len = __builtin_amdgcn_readfirstlane(len);
-  const uint32_t r0 = at.tile * kTileRows, rl = (r0 + kTileRows < a.rows ? r0 + kTileRows : a.rows) - 1u;      // the tile's first and last query
-  const int32_t past = len - (int32_t)a.s;                                     // rows before the first query's own
-  const int32_t pos_first = past + (int32_t)divided(r0, a.by_per), pos_last = past + (int32_t)divided(rl, a.by_per);
-  const uint32_t row = r0 + n;
+  const uint32_t r0 = at.tile * kTileRows, row = r0 + n;
   const bool has_row = row < a.rows;
   const auto query = [&](uint32_t& qs, uint32_t& qh) {             // the lane's query: of S, of the heads that share one of keys
     const uint32_t r = hidden(has_row ? row : r0);
@@ -389,6 +370,48 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
   };
   uint32_t qs, qh;
   query(qs, qh);
+  // the queries are asked for first: where the rows of the cache lie is four more trips to memory
+  constexpr uint32_t QL = DP / 32u;                                // pieces of eight elements in lanes
+  const bf8* const qf = (const bf8*)(lds + (by_head ? wave * Q_LDS : 0u));
+  float qv[2][8];                                                  // (a fourth of them; or half of them at a time)
+  const uint64_t qp = a.q + ((uint64_t)at.b * a.qs[0] + (uint64_t)qs * a.qs[1] + (uint64_t)(head * a.per + qh) * a.qs[2]) * size_of(DT);
+  const auto ask_queries = [&](uint32_t j, float (&f)[8]) {
+    const uint32_t e0 = 32u * j + 8u * g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+    if (j < QL && has_row && e0 < d && head < a.hk) {
+      if (a.qs[3] == 1u) ld8<DT>(qp + (uint64_t)e0 * size_of(DT), f);
+      else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) f[i] = ld_elem<DT>(qp + (uint64_t)(e0 + i) * a.qs[3] * size_of(DT));
+      }
+    }
+  };
+  const auto put_queries = [&](uint32_t j, float (&f)[8]) {        // as the parts of the second operand of K Q^T
+    if (j >= QL) return;
+#pragma unroll
+    for (uint32_t t = 0; t < NQ; ++t) {
+      u4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1]));
+      ((bf8*)qf)[(t * QL + j) * 64u + lane] = __builtin_bit_cast(bf8, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = rest_of(f[i]);
+    }
+  };
+  ask_queries(by_head ? 0u : wave, qv[0]);
+  ask_queries(by_head ? 1u : wave + 4u, qv[1]);
+
+  // what the tile's queries see: rows [from, end) of the sequence, and of that this piece's [t0, t1)
+  int32_t len = (int32_t)a.longest;
+  if (a.lengths != 0) {
+    const int32_t l = ld<int32_t>(a.lengths + (uint64_t)at.b * a.ls * 4u);
+    len = l < 0 ? 0 : (l < len ? l : len);
+  }
+  len = __builtin_amdgcn_readfirstlane(len);
+  const uint32_t rl = (r0 + kTileRows < a.rows ? r0 + kTileRows : a.rows) - 1u;      // the tile's first and last query
+  const int32_t past = len - (int32_t)a.s;                                     // rows before the first query's own
+  const int32_t pos_first = past + (int32_t)divided(r0, a.by_per), pos_last = past + (int32_t)divided(rl, a.by_per);
   const int32_t pos = past + (int32_t)qs;
   int32_t from = a.window != 0 ? pos_first - (int32_t)a.window + 1 : 0;
   from = from < 0 ? 0 : from;
@@ -401,38 +424,11 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     t1 = t0 + per * 64 < end ? t0 + per * 64 : end;
   }
 
-  // the queries, as the parts of the second operand of K Q^T
-  bf8* const qf = (bf8*)lds;
-  if (t0 < t1) {
-    for (uint32_t j = wave; j < DP / 32u; j += 4u) {
-      const uint32_t e0 = 32u * j + 8u * g;
-      const uint64_t qp = a.q + ((uint64_t)at.b * a.qs[0] + (uint64_t)qs * a.qs[1] + (uint64_t)(at.hk * a.per + qh) * a.qs[2]) * size_of(DT);
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-      if (has_row && e0 < d) {
-        if (a.qs[3] == 1u) ld8<DT>(qp + (uint64_t)e0 * size_of(DT), f);
-        else {
-#pragma unroll
-          for (uint32_t i = 0; i < 8; ++i) f[i] = ld_elem<DT>(qp + (uint64_t)(e0 + i) * a.qs[3] * size_of(DT));
-        }
-      }
-#pragma unroll
-      for (uint32_t t = 0; t < NQ; ++t) {
-        u4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = high_halves(as_u(f[2 * i]), as_u(f[2 * i + 1]));
-        qf[(t * (DP / 32u) + j) * 64u + lane] = __builtin_bit_cast(bf8, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = rest_of(f[i]);
-      }
-    }
-  }
-  __syncthreads();
+  if (head >= a.hk) t1 = t0;
 
-  uint8_t* const slab = lds + Q_LDS + wave * WAVE_LDS;
-  uint64_t* const offs = (uint64_t*)(slab + kSlab);                // [2][keys, values][64]
-  float* const sc = (float*)(slab + kSlab + 2048u);                // [GROUPS][keys, values][64]
+  uint8_t* const slab = lds + (by_head ? 4u * Q_LDS : Q_LDS) + wave * WAVE_LDS;
+  uint64_t* const offs = (uint64_t*)(slab + kSlab);                // [keys, values][64]
+  float* const sc = (float*)(slab + kSlab + 1024u);                // [GROUPS][keys, values][64]
   const uint64_t table = a.table + (uint64_t)at.b * a.ps[0] * 4u;
   float ks[GROUPS], vs[GROUPS];                                    // scales of row t + lane
   u4 r[IT];                                                        // a slab's pieces
@@ -441,29 +437,52 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     const int32_t k = t + (int32_t)lane < t1 ? t + (int32_t)lane : t1 - 1;
     return ld<uint32_t>(table + (uint64_t)divided((uint32_t)k, a.by_page) * a.ps[1] * 4u);
   };
-  const auto find = [&](int32_t t, uint32_t entry, uint32_t buf) {      // where the row lies, and its scales
+  const auto find = [&](int32_t t, uint32_t entry) {               // where the row lies, and its scales
     const uint32_t k = (uint32_t)(t + (int32_t)lane < t1 ? t + (int32_t)lane : t1 - 1), in = k - divided(k, a.by_page) * a.page;
     const bool known = entry < a.pages;
     const uint64_t e = known ? entry : 0u;
 #pragma unroll
     for (uint32_t v = 0; v < 2; ++v) {
-      offs[(buf * 2u + v) * 64u + lane] = a.kv[v].cache + (uint64_t)at.hk * a.kv[v].cs[2] + e * a.kv[v].cs[0] + (uint64_t)in * a.kv[v].cs[1];
-      const uint64_t sp = a.kv[v].scales + ((uint64_t)at.hk * a.kv[v].ss[2] + e * a.kv[v].ss[0] + (uint64_t)in * a.kv[v].ss[1]) * 4u;
+      offs[v * 64u + lane] = a.kv[v].cache + (uint64_t)head * a.kv[v].cs[2] + e * a.kv[v].cs[0] + (uint64_t)in * a.kv[v].cs[1];
+      const uint64_t sp = a.kv[v].scales + ((uint64_t)head * a.kv[v].ss[2] + e * a.kv[v].ss[0] + (uint64_t)in * a.kv[v].ss[1]) * 4u;
+      float f[GROUPS];                                             // (of more than one scale: that of each 32 elements)
+      if (MULTI && a.by_fours != 0u) {
+#pragma unroll
+        for (uint32_t q = 0; q < GROUPS; q += 4) {
+          const uint32_t left = FULL ? GROUPS - q : (32u * q < d ? (d - 32u * q + 31u) / 32u : 0u);
+          u4 w = {0, 0, 0, 0};
+          if (left >= 4u) w = ld<u4_any>(sp + 4u * q);
+          else {
+#pragma unroll
+            for (uint32_t k = 0; k < 3; ++k) {
+              if (k < left) w[k] = ld<uint32_t>(sp + 4u * (q + k));
+            }
+          }
+#pragma unroll
+          for (uint32_t k = 0; k < 4; ++k) {
+            if (q + k < GROUPS) f[q + k] = as_f(w[k]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (uint32_t q = 0; q < GROUPS; ++q) {
+          f[q] = 0.0f;
+          if (FULL || !MULTI || 32u * q < d) f[q] = ld<float>(sp + (uint64_t)(MULTI ? divided(32u * q, a.by_group) : 0u) * a.kv[v].ss[3] * 4u);
+        }
+      }
 #pragma unroll
       for (uint32_t q = 0; q < GROUPS; ++q) {
-        float f = 0.0f;                                            // (of more than one scale: that of each 32 elements)
-        if (FULL || !MULTI || 32u * q < d) f = ld<float>(sp + (uint64_t)(MULTI ? divided(32u * q, a.by_group) : 0u) * a.kv[v].ss[3] * 4u);
-        if (!known) f = __builtin_nanf("");                        // a page that is not in the cache
-        if (v) vs[q] = f;
-        else ks[q] = f;
+        const float to = known ? f[q] : __builtin_nanf("");        // a page that is not in the cache
+        if (v) vs[q] = to;
+        else ks[q] = to;
       }
     }
   };
-  const auto ask = [&](uint32_t buf, uint32_t v, uint32_t s) {
+  const auto ask = [&](uint32_t v, uint32_t s) {
 #pragma unroll
     for (uint32_t i = 0; i < IT; ++i) {
       const uint32_t c = lane & (CH - 1u);
-      const uint64_t p = offs[(buf * 2u + v) * 64u + i * (64u / CH) + lane / CH] + 64u * s + 16u * c;
+      const uint64_t p = offs[v * 64u + i * (64u / CH) + lane / CH] + 64u * s + 16u * c;
       if (FULL) r[i] = ld<u4_byte>(p);
       else {
         const uint32_t row_bytes = d * BITS / 8u, e = 64u * s + 16u * c;
@@ -495,19 +514,31 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
 #pragma unroll
   for (uint32_t j = 0; j < NV * MT; ++j) acc[j] = f4{0, 0, 0, 0};
   float m = -__builtin_inff(), l = 0.0f;
-  int32_t t = t0 + (int32_t)wave * 64;
-  uint32_t entry = 0, buf = 0;
-  if (t < t1) {
-    entry = look(t);
-    find(t, entry, 0);
-    wave_sync();
-    ask(0, 0, 0);
-    entry = look(t + 256);
+  const int32_t step = by_head ? 64 : 256;
+  int32_t t = t0 + (by_head ? 0 : (int32_t)wave * 64);
+  uint32_t entry = 0;
+  if (t < t1) entry = look(t);
+  put_queries(by_head ? 0u : wave, qv[0]);
+  put_queries(by_head ? 1u : wave + 4u, qv[1]);
+  if (by_head) {
+    for (uint32_t j = 2; j < QL; j += 2) {
+      ask_queries(j, qv[0]);
+      ask_queries(j + 1u, qv[1]);
+      put_queries(j, qv[0]);
+      put_queries(j + 1u, qv[1]);
+    }
   }
-  for (; t < t1; t += 256, buf ^= 1u) {
+  if (t < t1) {
+    find(t, entry);
+    wave_sync();
+    ask(0, 0);
+    entry = look(t + step);
+  }
+  __syncthreads();
+  for (; t < t1; t += step) {
 #pragma unroll
     for (uint32_t q = 0; q < GROUPS; ++q) {
-      sc[(2u * q) * 64u + lane] = ks[q];
+      sc[(2u * q) * 64u + lane] = ks[q] * a.scale;
       sc[(2u * q + 1u) * 64u + lane] = vs[q];
     }
     // scores: of query n, rows 16 T + 4 g + i
@@ -518,15 +549,15 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     for (uint32_t s = 0; s < NS; ++s) {
       put();
       wave_sync();
-      if (s + 1u < NS) ask(buf, 0, s + 1u);
-      else ask(buf, 1, first_slab);
+      if (s + 1u < NS) ask(0, s + 1u);
+      else ask(1, first_slab);
       uint32_t ko = hidden(key_at);
 #pragma unroll
       for (uint32_t j = 0; j < KS; ++j) {
         const uint32_t e = s * DS + 32u * j;                       // the step's first element (behind the head's last, all are 0)
         bf8 q[NQ];
 #pragma unroll
-        for (uint32_t k = 0; k < NQ; ++k) q[k] = qf[(k * (DP / 32u) + e / 32u) * 64u + lane];
+        for (uint32_t k = 0; k < NQ; ++k) q[k] = qf[(k * QL + e / 32u) * 64u + lane];
 #pragma unroll
         for (uint32_t T = 0; T < 4; ++T) {
           bf8 k;
@@ -552,12 +583,9 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
       }
       wave_sync();
     }
-    const bool next = t + 256 < t1;
-    if (next) find(t + 256, entry, buf ^ 1u);                      // (these scales go into LDS at the top)
+    if (!MULTI) {
 #pragma unroll
-    for (uint32_t T = 0; T < 4; ++T) {
-      if (!MULTI) x[T] = c[T] * *(const f4*)(sc + 16u * T + 4u * g);
-      x[T] *= a.scale;
+      for (uint32_t T = 0; T < 4; ++T) x[T] = c[T] * *(const f4*)(sc + 16u * T + 4u * g);
     }
     if (t < all_from || t + 63 > pos_first || t + 64 > t1) {       // some query does not see all of these
       const int32_t see_from = a.window != 0 ? pos - (int32_t)a.window + 1 : 0;
@@ -644,10 +672,12 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
       }
       put();
       wave_sync();
-      if (s + 1u < NV) ask(buf, 1, first_slab + s + 1u);
-      else if (next) {
-        ask(buf ^ 1u, 0, 0);
-        entry = look(t + 512);
+      if (s + 1u < NV) ask(1, first_slab + s + 1u);
+      else if (t + step < t1) {
+        find(t + step, entry);                                     // (these scales go into LDS at the top)
+        wave_sync();
+        ask(0, 0);
+        entry = look(t + 2 * step);
       }
       // The two steps of a tile of results together, two tiles at a time, as one waits for the other; or (STEPS) one step after the other, so that
       // only one step's weights are held.
@@ -693,50 +723,51 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     }
   }
 
-  // the four wavefronts' sums
   l = sum4(l);
-  __syncthreads();
-  float* const stats = (float*)lds;                                // [4][16][2]
-  float* const sums = (float*)(lds + 512u);                        // [2][16][DP]
-  if (g == 0u) {
-    stats[(wave * 16u + n) * 2u] = m;
-    stats[(wave * 16u + n) * 2u + 1u] = l;
-  }
-  __syncthreads();
-  float most = -__builtin_inff(), total = 0.0f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) most = __builtin_fmaxf(most, stats[(k * 16u + n) * 2u]);
-  const float ref = most == -__builtin_inff() ? 0.0f : most;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) total += stats[(k * 16u + n) * 2u + 1u] * __builtin_amdgcn_exp2f(stats[(k * 16u + n) * 2u] - ref);
-  const float by = __builtin_amdgcn_exp2f(m - ref);
-#pragma unroll
-  for (uint32_t j = 0; j < NV * MT; ++j) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[j][i] *= by;
-  }
-  // (two and two, then the two: always in this order)
-  for (uint32_t k = 2; k >= 1u; k /= 2u) {
-    if (wave >= k && wave < 2u * k) {
-#pragma unroll
-      for (uint32_t j = 0; j < NV * MT; ++j) *(f4*)(sums + ((wave - k) * NV * MT + j) * 256u + lane * 4u) = acc[j];
+  if (!by_head) {                                                  // the four wavefronts' sums
+    __syncthreads();
+    float* const stats = (float*)lds;                              // [4][16][2]
+    float* const sums = (float*)(lds + 512u);                      // [2][16][DV]
+    if (g == 0u) {
+      stats[(wave * 16u + n) * 2u] = m;
+      stats[(wave * 16u + n) * 2u + 1u] = l;
     }
     __syncthreads();
-    if (wave < k) {
+    float most = -__builtin_inff(), total = 0.0f;
 #pragma unroll
-      for (uint32_t j = 0; j < NV * MT; ++j) acc[j] += *(const f4*)(sums + (wave * NV * MT + j) * 256u + lane * 4u);
+    for (int k = 0; k < 4; ++k) most = __builtin_fmaxf(most, stats[(k * 16u + n) * 2u]);
+    const float ref = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) total += stats[(k * 16u + n) * 2u + 1u] * __builtin_amdgcn_exp2f(stats[(k * 16u + n) * 2u] - ref);
+    const float by = __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+    for (uint32_t j = 0; j < NV * MT; ++j) acc[j] *= by;
+    // (two and two, then the two: always in this order)
+    for (uint32_t k = 2; k >= 1u; k /= 2u) {
+      if (wave >= k && wave < 2u * k) {
+#pragma unroll
+        for (uint32_t j = 0; j < NV * MT; ++j) *(f4*)(sums + ((wave - k) * NV * MT + j) * 256u + lane * 4u) = acc[j];
+      }
+      __syncthreads();
+      if (wave < k) {
+#pragma unroll
+        for (uint32_t j = 0; j < NV * MT; ++j) acc[j] += *(const f4*)(sums + (wave * NV * MT + j) * 256u + lane * 4u);
+      }
+      __syncthreads();
     }
-    __syncthreads();
+    if (wave != 0u) return;
+    m = most;
+    l = total;
   }
-  if (wave != 0u || !has_row) return;
+  if (!has_row || head >= a.hk) return;
   const bool last = a.pieces == 1u;
   query(qs, qh);
-  const float inv = last ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
-  const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(at.hk * a.per + qh) * a.os[2]) * size_of(DT);
-  const uint64_t all = (uint64_t)a.b * a.hk * a.rows, mine = ((uint64_t)at.b * a.hk + at.hk) * a.rows + row, slice = (uint64_t)at.piece * all + mine;
+  const float inv = last ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+  const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(head * a.per + qh) * a.os[2]) * size_of(DT);
+  const uint64_t all = (uint64_t)a.b * a.hk * a.rows, mine = ((uint64_t)at.b * a.hk + head) * a.rows + row, slice = (uint64_t)at.piece * all + mine;
   if (!last && g == 0u && at.part == 0u) {
-    st<float>(a.stats + slice * 8u, most);
-    st<float>(a.stats + slice * 8u + 4u, total);
+    st<float>(a.stats + slice * 8u, m);
+    st<float>(a.stats + slice * 8u + 4u, l);
   }
 #pragma unroll
   for (uint32_t j = 0; j < NV * MT; ++j) {
@@ -756,92 +787,119 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
   }
 }
 
-// The pieces' sums: a workgroup has a query, each of its wavefronts adds every so many pieces, eight on their way at a time.
+// The pieces' sums.  A query has a wavefront, or, of more than 64 pieces, the workgroup (WIDE); a part of a wavefront has a quarter of the head's
+// elements in lanes and every so many of the pieces, eight on their way at a time.  2,048 queries of 128 elements, 8 pieces: 5.3 us (with a
+// workgroup each 9).
 constexpr uint32_t kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
-template <uint32_t DT> __global__ void __launch_bounds__(kJoinThreads, 8) gpuos_cache_join_kernel(const AttendArgs a) {
-  __shared__ alignas(16) float weight[kPiecesMost], sums[kJoinWaves][256], tops[kJoinWaves], totals[kJoinWaves];
-  const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u, mine = blockIdx.x;
+template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads, 8) gpuos_cache_join_kernel(const AttendArgs a) {
+  __shared__ alignas(16) float weight[WIDE ? kPiecesMost : kJoinWaves * 64u], sums[WIDE ? kJoinWaves : 1][256], tops[kJoinWaves], totals[kJoinWaves];
+  const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u;
   const uint64_t all = (uint64_t)a.b * a.hk * a.rows;
+  const uint64_t mine = WIDE ? blockIdx.x : (uint64_t)blockIdx.x * kJoinWaves + wave;
+  if (mine >= all) return;                                         // (of a WIDE one: none)
+  const uint32_t me = WIDE ? tid : lane;                           // which piece's weight the lane finds
   static_assert(kPiecesMost <= kJoinThreads, "a thread for each piece");
   float m = -__builtin_inff(), l = 0.0f;
-  if (tid < a.pieces) {
-    const u2 v = ld<u2_any>(a.stats + (tid * all + mine) * 8u);
+  if (me < a.pieces) {
+    const u2 v = ld<u2_any>(a.stats + (me * all + mine) * 8u);
     m = as_f(v[0]);
     l = as_f(v[1]);
   }
   float top = m;
   for (int w = 32; w >= 1; w /= 2) top = __builtin_fmaxf(top, __shfl_xor(top, w, 64));
-  if (lane == 0u) tops[wave] = top;
-  __syncthreads();
+  if (WIDE) {
+    if (lane == 0u) tops[wave] = top;
+    __syncthreads();
 #pragma unroll
-  for (uint32_t k = 0; k < kJoinWaves; ++k) top = __builtin_fmaxf(top, tops[k]);
+    for (uint32_t k = 0; k < kJoinWaves; ++k) top = __builtin_fmaxf(top, tops[k]);
+  }
   const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
   float total = l == 0.0f ? 0.0f : l * by;
-  if (tid < kPiecesMost) weight[tid] = l == 0.0f ? -1.0f : by;       // (an empty piece: its sums were not written)
+  float* const weights = weight + (WIDE ? 0u : wave * 64u);
+  if (me < (WIDE ? kPiecesMost : 64u)) weights[me] = l == 0.0f ? -1.0f : by;      // (an empty piece: its sums were not written)
   for (int w = 32; w >= 1; w /= 2) total += __shfl_xor(total, w, 64);
-  if (lane == 0u) totals[wave] = total;
-  __syncthreads();
-  total = 0.0f;
+  if (WIDE) {
+    if (lane == 0u) totals[wave] = total;
+    __syncthreads();
+    total = 0.0f;
 #pragma unroll
-  for (uint32_t k = 0; k < kJoinWaves; ++k) total += totals[k];
+    for (uint32_t k = 0; k < kJoinWaves; ++k) total += totals[k];
+  } else wave_sync();
+  // lanes of a part, parts of the wavefront
+  const uint32_t lanes = a.d <= 64u ? 16u : (a.d <= 128u ? 32u : 64u), e = 4u * (lane & (lanes - 1u)), parts = 64u / lanes * (WIDE ? kJoinWaves : 1u);
+  const uint32_t first = lane / lanes + (WIDE ? wave * (64u / lanes) : 0u);
   f4 sum = {0, 0, 0, 0};
-  const bool has = 4u * lane < a.d;
-  const uint64_t from = a.part + ((uint64_t)mine * a.d + (has ? 4u * lane : 0u)) * 4u;
-  for (uint32_t k0 = wave; k0 < a.pieces; k0 += 8u * kJoinWaves) {
+  const bool has = e < a.d;
+  const uint64_t from = a.part + (mine * a.d + (has ? e : 0u)) * 4u;
+  for (uint32_t k0 = first; k0 < a.pieces; k0 += 8u * parts) {
     f4 v[8];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       v[i] = f4{0, 0, 0, 0};
-      const uint32_t k = k0 + i * kJoinWaves;
+      const uint32_t k = k0 + i * parts;
       if (has && k < a.pieces) v[i] = __builtin_bit_cast(f4, ld<u4_any>(from + (uint64_t)k * all * a.d * 4u));
     }
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t k = k0 + i * kJoinWaves;
-      const float w = k < a.pieces ? weight[k] : -1.0f;
+      const uint32_t k = k0 + i * parts;
+      const float w = k < a.pieces ? weights[k] : -1.0f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += w < 0.0f ? 0.0f : v[i][e] * w;
+      for (int c = 0; c < 4; ++c) sum[c] += w < 0.0f ? 0.0f : v[i][c] * w;
     }
   }
-  *(f4*)&sums[wave][4u * lane] = sum;
-  __syncthreads();
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  const uint32_t pair = divided(mine, a.by_rows), row = mine - pair * a.rows, b = divided(pair, a.by_hk), hk = pair - b * a.hk;
+  for (uint32_t w = lanes; w < 64u; w *= 2) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sum[c] += __shfl_xor(sum[c], (int)w, 64);
+  }
+  if (WIDE) {
+    if (lane < lanes) *(f4*)&sums[wave][e] = sum;
+    __syncthreads();
+    if (wave != 0u) return;
+    sum = f4{0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t k = 0; k < kJoinWaves; ++k) sum += *(const f4*)&sums[k][e];
+  }
+  if (lane >= lanes || !has) return;
+  sum *= total == 0.0f ? 0.0f : 1.0f / total;
+  const uint32_t pair = divided((uint32_t)mine, a.by_rows), row = (uint32_t)mine - pair * a.rows, b = divided(pair, a.by_hk), hk = pair - b * a.hk;
   const uint32_t qs = divided(row, a.by_per), qh = row - qs * a.per;
   const uint64_t op = a.out + ((uint64_t)b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(hk * a.per + qh) * a.os[2]) * size_of(DT);
-  if (tid < a.d) {
-    float o = 0.0f;
+  if (a.os[3] == 1u) st4<DT>(op + (uint64_t)e * size_of(DT), sum);
+  else {
 #pragma unroll
-    for (uint32_t k = 0; k < kJoinWaves; ++k) o += sums[k][tid];
-    st_elem<DT>(op + (uint64_t)tid * a.os[3] * size_of(DT), o * inv);
+    for (uint32_t i = 0; i < 4; ++i) st_elem<DT>(op + (uint64_t)(e + i) * a.os[3] * size_of(DT), sum[i]);
   }
 }
 
-struct AttendKernel { const void* kernel; uint32_t lds; };
-template <uint32_t FMT, uint32_t DT, bool MULTI> AttendKernel attend_kernel(uint32_t d) {
+struct AttendKernel { const void* kernel; uint32_t lds; };      // lds: with queries for each wavefront, or for all
+template <uint32_t FMT, uint32_t DT, bool MULTI> AttendKernel attend_kernel(uint32_t d, bool by_head) {
   if constexpr (DT != GPUOS_F32) {
-    if (d == 64u) return {(const void*)gpuos_cache_attend_kernel<FMT, 64, true, DT, MULTI>, attend_lds(64, DT, MULTI)};
-    if (d == 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, true, DT, MULTI>, attend_lds(128, DT, MULTI)};
-    if (d == 256u) return {(const void*)gpuos_cache_attend_kernel<FMT, 256, true, DT, MULTI>, attend_lds(256, DT, MULTI)};
+    if (d == 64u) return {(const void*)gpuos_cache_attend_kernel<FMT, 64, true, DT, MULTI>, attend_lds(64, DT, MULTI, by_head)};
+    if (d == 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, true, DT, MULTI>, attend_lds(128, DT, MULTI, by_head)};
+    if (d == 256u) return {(const void*)gpuos_cache_attend_kernel<FMT, 256, true, DT, MULTI>, attend_lds(256, DT, MULTI, by_head)};
   }
-  if (d <= 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, false, DT, MULTI>, attend_lds(128, DT, MULTI)};
-  return {(const void*)gpuos_cache_attend_kernel<FMT, 256, false, DT, MULTI>, attend_lds(256, DT, MULTI)};
+  if (d <= 128u) return {(const void*)gpuos_cache_attend_kernel<FMT, 128, false, DT, MULTI>, attend_lds(128, DT, MULTI, by_head)};
+  return {(const void*)gpuos_cache_attend_kernel<FMT, 256, false, DT, MULTI>, attend_lds(256, DT, MULTI, by_head)};
 }
-template <uint32_t FMT> AttendKernel attend_kernel(uint32_t dt, uint32_t d, bool multi) {
-  if (dt == GPUOS_F32) return multi ? attend_kernel<FMT, GPUOS_F32, true>(d) : attend_kernel<FMT, GPUOS_F32, false>(d);
-  if (dt == GPUOS_F16) return multi ? attend_kernel<FMT, GPUOS_F16, true>(d) : attend_kernel<FMT, GPUOS_F16, false>(d);
-  return multi ? attend_kernel<FMT, GPUOS_BF16, true>(d) : attend_kernel<FMT, GPUOS_BF16, false>(d);
+template <uint32_t FMT> AttendKernel attend_kernel(uint32_t dt, uint32_t d, bool multi, bool by_head) {
+  if (dt == GPUOS_F32) return multi ? attend_kernel<FMT, GPUOS_F32, true>(d, by_head) : attend_kernel<FMT, GPUOS_F32, false>(d, by_head);
+  if (dt == GPUOS_F16) return multi ? attend_kernel<FMT, GPUOS_F16, true>(d, by_head) : attend_kernel<FMT, GPUOS_F16, false>(d, by_head);
+  return multi ? attend_kernel<FMT, GPUOS_BF16, true>(d, by_head) : attend_kernel<FMT, GPUOS_BF16, false>(d, by_head);
 }
 
 int launch_attend(const AttendArgs& a, uint32_t format, void* stream) {
-  const bool multi = a.group != a.d;
-  const AttendKernel k = format == CF_E2M1 ? attend_kernel<CF_E2M1>(a.dtype, a.d, multi) : (format == CF_I8 ? attend_kernel<CF_I8>(a.dtype, a.d, multi) : attend_kernel<CF_E4M3>(a.dtype, a.d, multi));
+  const bool multi = a.group != a.d, by_head = a.by_head != 0u;
+  const AttendKernel k = format == CF_E2M1 ? attend_kernel<CF_E2M1>(a.dtype, a.d, multi, by_head) : (format == CF_I8 ? attend_kernel<CF_I8>(a.dtype, a.d, multi, by_head) : attend_kernel<CF_E4M3>(a.dtype, a.d, multi, by_head));
   void* args[] = {(void*)&a};
   const uint32_t outer = (a.blocks / a.inner + 7u) / 8u * 8u;
   const int rc = (int)hipLaunchKernel(k.kernel, dim3(outer * a.inner), dim3(kThreads), args, k.lds, (hipStream_t)stream);
   if (rc != (int)hipSuccess || a.pieces == 1u) return rc;
-  const void* const joins[] = {(const void*)gpuos_cache_join_kernel<GPUOS_F32>, (const void*)gpuos_cache_join_kernel<GPUOS_F16>, (const void*)gpuos_cache_join_kernel<GPUOS_BF16>};
-  return (int)hipLaunchKernel(joins[a.dtype], dim3(a.b * a.hk * a.rows), dim3(kJoinThreads), args, 0, (hipStream_t)stream);
+  const void* const joins[] = {(const void*)gpuos_cache_join_kernel<GPUOS_F32, false>,  (const void*)gpuos_cache_join_kernel<GPUOS_F16, false>,
+                               (const void*)gpuos_cache_join_kernel<GPUOS_BF16, false>, (const void*)gpuos_cache_join_kernel<GPUOS_F32, true>,
+                               (const void*)gpuos_cache_join_kernel<GPUOS_F16, true>,   (const void*)gpuos_cache_join_kernel<GPUOS_BF16, true>};
+  const uint32_t all = a.b * a.hk * a.rows;
+  const bool wide = a.pieces > 64u;
+  return (int)hipLaunchKernel(joins[a.dtype + (wide ? 3u : 0u)], dim3(wide ? all : (all + kJoinWaves - 1u) / kJoinWaves), dim3(kJoinThreads), args, 0, (hipStream_t)stream);
 }
 
 }  // namespace gpuos
