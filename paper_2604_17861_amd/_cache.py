@@ -2,12 +2,12 @@
 bits, and attention that reads it as it is held.  include/gpuos.h says what they compute and take; everything here is checking
 of shapes and marshalling.  They are not differentiable: what requires a gradient is refused where gradients are recorded."""
 import struct
-from array import array
 
 import torch
 from torch.autograd import forward_ad
 from torch.fx import _symbolic_trace
 
+from . import _binding as B
 from . import model as M
 from . import runtime as R
 from . import streams as S
@@ -18,8 +18,6 @@ OPERANDS = 11
 _TASK = struct.Struct("<II12q" + "Q4qB7x" * OPERANDS + "f4x")
 assert _TASK.size == S.CACHE_TASK_BYTES
 _CACHES = {torch.int8: 4, torch.float8_e4m3fn: 5, torch.uint8: 6}
-_WORDS = S.CACHE_TASK_BYTES // 8
-_POINTER = 13                      # word of the first operand's address; the others' every six words
 
 
 def _caches_operand(c):
@@ -44,41 +42,32 @@ def _check_caches(dev, hk, d, k_cache, k_scales, v_cache, v_scales):
 
 
 class _Plan:
-    """A call's descriptor by everything about it but addresses: checked and packed once, then only the addresses are put in.  places: (operand,
-    which of what _run is given).  workspace: bytes."""
-    __slots__ = ("words", "at", "device", "empty", "workspace")
+    """A call's descriptor by everything about it but addresses: checked and packed once, then only the addresses are put in.  places: which operand each
+    of the call's tensors is; written: which of them the caller gave and the call writes."""
+    __slots__ = ("task", "places", "written", "device", "workspace", "empty")
 
-    def __init__(self, task, places, device, empty):
-        self.words, self.device, self.empty = array("Q", task), device, empty
-        self.at = [(_POINTER + 6 * o, k) for o, k in places]
+    def __init__(self, task, places, written, device, empty):
+        self.task, self.places, self.written, self.device, self.empty = task, bytes(places), bytes(written), device, empty
         self.workspace = R.cache_workspace(task)
-        for o in range(OPERANDS):
-            self.words[_POINTER + 6 * o] = 0
 
 
-def _run(plan, operands, written=()):
+_launch = None
+
+
+def _run(plan, operands):
     """As model._run."""
+    global _launch
     if plan.empty:
         return
     if forward_ad._current_level >= 0:
         M._no_tangent(operands)
     if M._modes() or _symbolic_trace._is_fx_tracing_flag or M._jit_tracing():
         M._under_modes(operands)
-    words = plan.words[:]
-    for word, k in plan.at:
-        words[word] = at = operands[k].data_ptr()
-        if not at:
-            M._need(operands[k].numel() == 0, "a tensor without memory (of a trace, say)")
-    if plan.workspace:                                      # (of the current stream: the allocator gives it to no other before that one is through)
-        space = operands[0].new_empty(plan.workspace, dtype=torch.uint8)
-        R.launch_cache_at(words.buffer_info()[0], plan.device, space.data_ptr(), plan.workspace, M._stream_of(plan.device))
-    else:
-        R.launch_cache_at(words.buffer_info()[0], plan.device, 0, 0, M._stream_of(plan.device))
-    if written:
-        try:
-            torch._C._increment_version(written)
-        except RuntimeError:                                # tensors of inference mode have no versions
-            torch._C._increment_version([o for o in written if not o.is_inference()])
+    if _launch is None:
+        _launch = R.cache_launch_address()
+    rc = B.launch(_launch, plan.task, plan.places, operands, plan.written, plan.device, plan.workspace, M._stream_of(plan.device))
+    if rc:
+        raise R.GpuosError(rc, "gpuos_launch_cache")
 
 
 def append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table=None, positions=None, out=None, *, pairs=False):
@@ -146,22 +135,21 @@ def cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table
     [pages, page, H, D / 2] (uint8: two e2m1 a byte, the earlier one in the lower half) and their scales [pages, page, H, groups]
     (float32), in one launch.  Returns q' (out may be q; None without q).  Slots are distinct.  Not differentiable: what
     requires a gradient is refused where gradients are recorded."""
-    pairs = bool(pairs)
-    M._no_gradient("cache_append_qkv", q, k, v, table, k_scales, v_scales, out)
-    given = (q, k, v, table, positions, slots, k_cache, k_scales, v_cache, v_scales, out)
-    key = ("append", pairs, *map(M._sig, given))
+    given = (q, k, v, table, positions, slots, out, k_cache, k_scales, v_cache, v_scales)      # in the descriptor's order
+    key = B.key(given) + (b"append pairs" if pairs else b"append")
     plan = M._plans.get(key)
-    made = q is not None and out is None
-    if plan is None and made:
-        M._check(q, "q", M._FLOAT, (3, 4))
-    to = M._empty_like(q) if made else out
-    operands = (q, k, v, table, positions, slots, to, k_cache, k_scales, v_cache, v_scales)
     if plan is None:
-        task = append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions, to, pairs=pairs)
-        empty = k.numel() == 0 and (q is None or q.numel() == 0)
-        plan = M._keep(key, _Plan(task, [(i, i) for i, t in enumerate(operands) if t is not None], k.get_device(), empty))
-    _run(plan, operands, (k_cache, k_scales, v_cache, v_scales) if made or q is None else (to, k_cache, k_scales, v_cache, v_scales))
-    return to
+        if q is not None and out is None:
+            M._check(q, "q", M._FLOAT, (3, 4))
+        M._no_gradient("cache_append_qkv", *given)
+    made = q is not None and out is None
+    operands = (q, k, v, table, positions, slots, M._empty_like(q), k_cache, k_scales, v_cache, v_scales) if made else given
+    if plan is None:
+        task = append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions, operands[6], pairs=bool(pairs))
+        plan = M._keep(key, _Plan(task, range(11), ([] if made or q is None else [6]) + [7, 8, 9, 10], k.get_device(),
+                                  k.numel() == 0 and (q is None or q.numel() == 0)))
+    _run(plan, operands)
+    return operands[6]
 
 
 def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, *, scale=None, window=0, out=None):
@@ -171,17 +159,17 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
     rows up to its own, with window > 0 the last `window` of these.  scale: of the scores (None: 1 / sqrt(D)).  A query that
     sees nothing gets zeros.  Not differentiable: what requires a gradient is refused where gradients are recorded."""
     longest, window = int(longest), int(window)
-    M._no_gradient("cache_attention", q, k_scales, v_scales, out)
-    given = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths)
-    key = ("attention", longest, window, scale if scale is None else float(scale), *map(M._sig, given), M._sig(out))
+    given = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, out)      # in the descriptor's order
+    key = B.key(given), longest, window, scale if scale is None else float(scale)
     plan = M._plans.get(key)
     if plan is None:
         M._check(q, "q", M._FLOAT, (3, 4))
-    written, out = () if out is None else (out,), M._empty_like(q) if out is None else out
-    operands = (*given, out)
+        M._no_gradient("cache_attention", *given)
+    made = out is None
+    operands = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, M._empty_like(q)) if made else given
     if plan is None:
         by = float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.shape[-1] else 1.0
-        task = attention_task(*operands[:7], longest, out, scale=by, window=window)
-        plan = M._keep(key, _Plan(task, [(i, i) for i, t in enumerate(operands) if t is not None], q.get_device(), q.numel() == 0))
-    _run(plan, operands, written)
-    return out
+        task = attention_task(*operands[:7], longest, operands[7], scale=by, window=window)
+        plan = M._keep(key, _Plan(task, range(8), [] if made else [7], q.get_device(), q.numel() == 0))
+    _run(plan, operands)
+    return operands[7]

@@ -1,11 +1,15 @@
-"""Build libgpuos.so (HIP kernels + host runtime) for gfx950, in-tree."""
+"""Build libgpuos.so (HIP kernels + host runtime) for gfx950 and _binding.so (the module on PyTorch tensors), in-tree."""
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgpuos.so")
+BINDING, BINDING_SOURCE = os.path.join(HERE, "_binding.so"), os.path.join(CSRC, "gpuos_binding.cpp")
 SOURCES = ["gpuos_kernels.hip", "gpuos_model.hip", "gpuos_cache.hip", "gpuos_runtime.cpp", "gpuos_model.cpp", "gpuos_cache.cpp", "gpuos_jit.cpp"]
 HEADERS = ["gpuos_internal.h", "gpuos_device.h", "gpuos_model.h", "gpuos_model_device.h", "gpuos_cache.h", "gpuos_on_device.h", os.path.join("..", "..", "include", "gpuos.h")]
 
@@ -16,25 +20,43 @@ FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-shared", "-ffp
          "-Wno-unused-but-set-variable", "-pthread", "-DGPUOS_CSRC_DIR=" + CSRC, "-ldl"]
 
 
+def _older(made, deps):
+    return not os.path.exists(made) or any(os.path.getmtime(d) > os.path.getmtime(made) for d in deps)
+
+
 def needs_build():
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)]
-    return any(os.path.getmtime(d) > t for d in deps)
+    return (_older(LIB, [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)])
+            or _older(BINDING, [BINDING_SOURCE, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]))
+
+
+def binding_command():
+    """The host compiler's command for the module, against the headers and libraries of the PyTorch that is installed."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1"] + ["-isystem" + i for i in include]
+            + ["-o", BINDING, BINDING_SOURCE, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+
+
+def _all(jobs):
+    """Run commands beside each other: what they say, or the first that failed as an exception."""
+    running = [subprocess.Popen(j, cwd=CSRC, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for j in jobs]
+    said = [r.communicate()[0] for r in running]
+    out = ["\n".join(l for l in t.splitlines() if "packed-fp32-ops" not in l) for t in said]
+    for r, t in zip(running, out):
+        if r.returncode != 0:
+            raise RuntimeError(os.path.basename(r.args[0]) + " failed:\n" + t)
+    return "\n".join(t for t in out if t.strip())
 
 
 def build(force=True, verbose=False):
     if not force and not needs_build():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        cmd.insert(1, "-Rpass-analysis=kernel-resource-usage")
-    r = subprocess.run(cmd, cwd=CSRC, capture_output=True, text=True)
-    out = "\n".join(l for l in (r.stdout + r.stderr).splitlines() if "packed-fp32-ops" not in l)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+    flags = (["-Rpass-analysis=kernel-resource-usage"] if verbose else []) + [f for f in FLAGS if f not in ("-shared", "-ldl")]
+    with tempfile.TemporaryDirectory() as made:                 # (a source at a time would take as long as all of them: two to four minutes)
+        objects = [os.path.join(made, s + ".o") for s in SOURCES]
+        jobs = [[hipcc] + flags + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)] + [binding_command()]
+        out = _all(jobs) + _all([[hipcc, "--offload-arch=gfx950", "-shared", "-pthread", "-o", LIB] + objects + ["-ldl"]])
     if verbose or out.strip():
         print(out, file=sys.stderr)
     return LIB

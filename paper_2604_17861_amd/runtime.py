@@ -457,9 +457,6 @@ def launch_model_at(tasks, n, device, stream):
         raise GpuosError(rc, "gpuos_launch_model")
 
 
-_launch_cache = None
-
-
 def cache_workspace(task):
     """gpuos_cache_workspace of a cache operator's descriptor (bytes): the bytes that its launch needs."""
     assert isinstance(task, bytes) and len(task) == S.CACHE_TASK_BYTES
@@ -471,17 +468,12 @@ def cache_workspace(task):
 def launch_cache(task, workspace=0, workspace_bytes=0, device=0, stream=0):
     """gpuos_launch_cache: a cache operator's descriptor (bytes) on `stream` (a stream's handle); workspace: a device address."""
     assert isinstance(task, bytes) and len(task) == S.CACHE_TASK_BYTES
-    launch_cache_at(task, device, workspace, workspace_bytes, stream)
+    _check(lib().gpuos_launch_cache(device, task, workspace, workspace_bytes, stream), "gpuos_launch_cache")
 
 
-def launch_cache_at(task, device, workspace, workspace_bytes, stream):
-    """launch_cache of a descriptor at an address."""
-    global _launch_cache
-    if _launch_cache is None:
-        _launch_cache = lib().gpuos_launch_cache
-    rc = _launch_cache(device, task, workspace, workspace_bytes, stream)
-    if rc != OK:
-        raise GpuosError(rc, "gpuos_launch_cache")
+def cache_launch_address():
+    """Where gpuos_launch_cache is, for a caller in C."""
+    return ctypes.cast(lib().gpuos_launch_cache, ctypes.c_void_p).value
 
 
 def _impl_table(table):
