@@ -13,14 +13,20 @@ struct CachePart {
   uint64_t cache, scales;
   uint32_t cs[3], ss[4];           // page, place, head (, group)
 };
-struct AppendArgs {
-  uint64_t x[3], out, table, positions, slots;       // x: queries, keys, values
-  CachePart kv[2];
-  uint32_t xs[3][4], os[4], ps[2], ls[2], ts;        // strides: B, S, H, D; of positions, slots; of the table's rows
-  uint32_t hq, hk, seq, d, half, places, pages, page, group;
-  uint32_t blocks_q, blocks_k, blocks;               // blocks of heads: of queries, of keys (as many of values), of a token
+// Queries, keys or values: where the rows are, and where they go: the rotated rows, or a cache and its scales.
+struct AppendSide {
+  uint64_t x, to, scales;
+  uint32_t xs[4], ts[4], ss[4];    // strides: B, S, H, D; the same, or page, place, head (bytes); page, place, head, group
+  uint32_t heads, blocks;          // heads, and blocks of them
   uint32_t items, chunks;
-  Div by_blocks, by_seq, by_page;
+  Div by_blocks;
+};
+struct AppendArgs {
+  AppendSide side[3];
+  uint64_t table, positions, slots;
+  uint32_t ps[2], ls[2], ts;                         // strides of positions, slots: B, S; of the table's rows
+  uint32_t seq, d, half, places, pages, page, group;
+  Div by_seq, by_page;
   uint32_t dtype, format;
   uint32_t vec, pairs;                               // rows in vectors (the rules are at the packing); neighbours are rotated together
 };
@@ -82,44 +88,55 @@ class CachePack : ModelPack {
     if ((keys && (!k->ptr || !v->ptr || !slots->ptr)) || (queries && (!q->ptr || !out->ptr))) return GPUOS_E_INVAL;
     const uint32_t dt = k->dtype;
     if (!is_float(dt) || v->dtype != dt || (hq != 0 && (q->dtype != dt || out->dtype != dt))) return GPUOS_E_INVAL;
-    if (hq != 0 && (!operand(*q, 4, qz, false, false, a->xs[0]) || !operand(*out, 4, qz, true, false, a->os))) return GPUOS_E_INVAL;
-    if (!operand(*k, 4, kz, false, false, a->xs[1]) || !operand(*v, 4, kz, false, false, a->xs[2])) return GPUOS_E_INVAL;
+    AppendSide &sq = a->side[0], &sk = a->side[1], &sv = a->side[2];
+    if (hq != 0 && (!operand(*q, 4, qz, false, false, sq.xs) || !operand(*out, 4, qz, true, false, sq.ts))) return GPUOS_E_INVAL;
+    if (!operand(*k, 4, kz, false, false, sk.xs) || !operand(*v, 4, kz, false, false, sv.xs)) return GPUOS_E_INVAL;
     if (slots->dtype != GPUOS_I32 || !operand(*slots, 2, kz, false, false, a->ls)) return GPUOS_E_INVAL;
     uint32_t ts[2] = {0, 0};
     if (rot > 0) {
       if (places < 1 || !table->ptr || table->dtype != GPUOS_F32 || !operand(*table, 2, tz, false, true, ts)) return GPUOS_E_INVAL;
       if (pos->ptr && (pos->dtype != GPUOS_I32 || !operand(*pos, 2, kz, false, false, a->ps))) return GPUOS_E_INVAL;
     }
-    const int rc = caches(t, 7, hk, d, pages, page, groups, true, keys && pages != 0, 8, a->kv, &a->format);
+    CachePart kv[2];
+    const int rc = caches(t, 7, hk, d, pages, page, groups, true, keys && pages != 0, 8, kv, &a->format);
     if (rc != GPUOS_OK) return rc;
-    a->x[0] = (uint64_t)q->ptr; a->x[1] = (uint64_t)k->ptr; a->x[2] = (uint64_t)v->ptr;
-    a->out = (uint64_t)out->ptr;
+    sq.x = (uint64_t)q->ptr; sk.x = (uint64_t)k->ptr; sv.x = (uint64_t)v->ptr;
+    sq.to = (uint64_t)out->ptr;
+    for (int c = 0; c < 2; ++c) {
+      AppendSide& side = a->side[1 + c];
+      side.to = kv[c].cache;
+      side.scales = kv[c].scales;
+      for (int i = 0; i < 3; ++i) side.ts[i] = kv[c].cs[i];
+      for (int i = 0; i < 4; ++i) side.ss[i] = kv[c].ss[i];
+    }
     a->table = rot > 0 ? (uint64_t)table->ptr : 0;
     a->positions = rot > 0 ? (uint64_t)pos->ptr : 0;
     a->slots = (uint64_t)slots->ptr;
     a->ts = ts[0];
-    a->hq = (uint32_t)hq; a->hk = (uint32_t)hk; a->seq = (uint32_t)s; a->d = (uint32_t)d;
+    a->seq = (uint32_t)s; a->d = (uint32_t)d;
     a->half = (uint32_t)(rot / 2); a->places = (uint32_t)places;
     a->pages = (uint32_t)pages; a->page = (uint32_t)page; a->group = (uint32_t)(d / groups);
     a->dtype = dt;
     a->pairs = (t.flags & GPUOS_FLAG_PAIRS) ? 1u : 0u;
-    // Vectors: a lane takes eight elements that are all rotated by the same half of the pairs, or not rotated.
-    const bool dense = (hq == 0 || (a->xs[0][3] == 1 && a->os[3] == 1)) && a->xs[1][3] == 1 && a->xs[2][3] == 1;
-    a->vec = dense && d % 8 == 0 && (a->pairs ? rot : rot / 2) % 8 == 0 ? 1u : 0u;
-    const uint32_t block = a->vec ? kAppendBlock : 1;
-    a->blocks_q = (a->hq + block - 1) / block;
-    a->blocks_k = (a->hk + block - 1) / block;
-    a->blocks = a->blocks_q + 2 * a->blocks_k;
     if (*empty) return GPUOS_OK;
-    a->items = (uint32_t)(b * s * a->blocks);
-    a->by_blocks = make_div(a->blocks);
     a->by_seq = make_div(a->seq);
     a->by_page = make_div(a->page);
+    // Vectors: a lane takes eight elements that are all rotated by the same half of the pairs, or not rotated.
+    const bool dense = (hq == 0 || (sq.xs[3] == 1 && sq.ts[3] == 1)) && (hk == 0 || (sk.xs[3] == 1 && sv.xs[3] == 1));
+    a->vec = dense && d % 8 == 0 && (a->pairs ? rot : rot / 2) % 8 == 0 ? 1u : 0u;
+    const uint32_t block = a->vec ? kAppendBlock : 1;
     uint32_t lanes = 1;
     while (lanes < (a->d + 7) / 8) lanes *= 2;
     const uint32_t pass = kThreads / lanes;
-    const uint64_t passes = ((uint64_t)a->items + pass - 1) / pass;
-    a->chunks = passes < 65536 ? (uint32_t)passes : 65536u;
+    for (int c = 0; c < 3; ++c) {
+      AppendSide& side = a->side[c];
+      side.heads = (uint32_t)(c == 0 ? hq : hk);
+      side.blocks = (side.heads + block - 1) / block;
+      side.by_blocks = make_div(side.blocks);
+      side.items = (uint32_t)(b * s) * side.blocks;
+      const uint64_t passes = ((uint64_t)side.items + pass - 1) / pass;
+      side.chunks = passes < 65536 ? (uint32_t)passes : 65536u;
+    }
     return GPUOS_OK;
   }
 

@@ -75,9 +75,6 @@ template <uint32_t DT> DEV void st4(uint64_t p, f4 f) {
 // lanes is a group's maximum.  Products and sums of the rotation are rounded by themselves (no fused multiply-add), so that the codes
 // are those of the definition.
 // ---------------------------------------------------------------------------
-DEV uint64_t pick(uint32_t kind, uint64_t a, uint64_t b, uint64_t c) { return kind == 0 ? a : (kind == 1 ? b : c); }
-DEV uint32_t pick(uint32_t kind, uint32_t a, uint32_t b, uint32_t c) { return kind == 0 ? a : (kind == 1 ? b : c); }
-
 // eight codes of |y| <= qmax (1 + 2^-23): to the nearest, to the even one of two
 DEV u2 encode(const float* y, uint32_t format) {
   u2 w = {0, 0};
@@ -101,149 +98,169 @@ DEV u2 encode(const float* y, uint32_t format) {
   return w;
 }
 
+// the largest over `width` lanes, a power of two of them
+DEV uint32_t most_of(uint32_t v, uint32_t width) {
+  auto with = [&](int other) { v = v > (uint32_t)other ? v : (uint32_t)other; };
+  if (width > 1u) with(__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));      // quad_perm 1 0 3 2
+  if (width > 2u) with(__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));      // quad_perm 2 3 0 1
+  if (width > 4u) with(__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));     // half a row of 16 mirrored
+  if (width > 8u) with(__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));     // a row mirrored
+  if (width > 16u) {
+    auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = r[0] > r[1] ? r[0] : r[1];
+  }
+  if (width > 32u) {
+    auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = r[0] > r[1] ? r[0] : r[1];
+  }
+  return v;
+}
+
+// The grid's second index is the side: queries, keys, values.  An item is a token and a block of its heads.
 // VEC: rows in vectors of eight, each all first, all second or all not rotated elements (neighbours: all rotated or none), last dims dense;
 // else element by element, a head at a time.
-template <uint32_t DT, bool VEC> __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_append_kernel(const AppendArgs a) {
+template <uint32_t DT, bool VEC> __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_append_kernel(const AppendArgs args) {
+  const AppendSide& a = args.side[blockIdx.y];
+  if (blockIdx.x >= a.chunks) return;
   constexpr uint32_t ES = size_of(DT);
   constexpr int U = VEC ? kAppendBlock : 1;
-  const uint32_t units = (a.d + 7u) / 8u, lg = units <= 1u ? 0u : 32u - (uint32_t)__builtin_clz(units - 1u), lanes = 1u << lg;
-  const uint32_t u = threadIdx.x & (lanes - 1u), row = threadIdx.x >> lg, step = kThreads >> lg, j0 = 8u * u;
-  const uint32_t lg_width = a.group == a.d ? lg : 28u - (uint32_t)__builtin_clz(a.group), width = 1u << lg_width;      // lanes of a group
-  const uint32_t n = a.half;
-  const uint32_t left = u < units ? (VEC || a.d - j0 >= 8u ? 8u : a.d - j0) : 0u;      // elements that the lane has
-  const bool first = j0 < n;                                                 // (of a vector's: all)
+  const uint32_t d = args.d, n = args.half, format = args.format;
+  const bool stored = blockIdx.y != 0u, turns = blockIdx.y != 2u && n != 0u, pairs = args.pairs != 0u;
+  const uint32_t units = (d + 7u) / 8u, lg = units <= 1u ? 0u : 32u - (uint32_t)__builtin_clz(units - 1u), lanes = 1u << lg;
+  const uint32_t u = threadIdx.x & (lanes - 1u), row = threadIdx.x >> lg, step = kThreads >> lg;
+  const uint32_t lg_width = args.group == d ? lg : 28u - (uint32_t)__builtin_clz(args.group), width = 1u << lg_width;      // lanes of a group
+  const bool mine = u < units;                                               // (the others do as the last that has some, and store nothing)
+  const uint32_t j0 = 8u * (mine ? u : units - 1u), left = VEC || d - j0 >= 8u ? 8u : d - j0;
+  const bool first = j0 < n, turned = turns && j0 < 2u * n;                  // (of a vector's elements: all)
   for (uint32_t base = blockIdx.x * step; base < a.items; base += a.chunks * step) {
     const uint32_t item = base + row < a.items ? base + row : a.items - 1u;
-    const bool there = base + row < a.items && u < units;
-    const uint32_t token = divided(item, a.by_blocks), blk = item - token * a.blocks;
-    const uint32_t b = divided(token, a.by_seq), s = token - b * a.seq;
-    const uint32_t kind = blk < a.blocks_q ? 0u : (blk < a.blocks_q + a.blocks_k ? 1u : 2u);
-    const uint32_t h = (blk - pick(kind, 0u, a.blocks_q, a.blocks_q + a.blocks_k)) * U, count = kind == 0 ? a.hq : a.hk;
-    const uint32_t heads = there ? (count - h < (uint32_t)U ? count - h : (uint32_t)U) : 0u;
-    const uint32_t sb = pick(kind, a.xs[0][0], a.xs[1][0], a.xs[2][0]), ss = pick(kind, a.xs[0][1], a.xs[1][1], a.xs[2][1]);
-    const uint32_t sh = pick(kind, a.xs[0][2], a.xs[1][2], a.xs[2][2]), sd = VEC ? 1u : pick(kind, a.xs[0][3], a.xs[1][3], a.xs[2][3]);
-    const uint64_t xp = pick(kind, a.x[0], a.x[1], a.x[2]) + ((uint64_t)b * sb + (uint64_t)s * ss + (uint64_t)h * sh) * ES;
-    const bool turns = kind != 2u && n != 0u, turned = turns && j0 < 2u * n;
-    uint32_t place = 0;
-    bool has = true;
-    if (turns) {
-      place = a.positions != 0 ? ld<uint32_t>(a.positions + ((uint64_t)b * a.ps[0] + (uint64_t)s * a.ps[1]) * 4u) : s;
-      has = place < a.places;
-    }
-    const uint64_t cosines = a.table + (uint64_t)(has ? place : 0u) * a.ts * 4u, sines = cosines + (uint64_t)n * 4u;
-    const uint32_t slot = kind != 0u ? ld<uint32_t>(a.slots + ((uint64_t)b * a.ls[0] + (uint64_t)s * a.ls[1]) * 4u) : 0xffffffffu;
-    // the elements, the other ones of their pairs, cosines and signed sines: z = x c + p s
+    const bool there = base + row < a.items && mine;
+    const uint32_t token = divided(item, a.by_blocks), h = (item - token * a.blocks) * U;
+    const uint32_t b = divided(token, args.by_seq), s = token - b * args.seq;
+    const uint64_t xp = a.x + ((uint64_t)b * a.xs[0] + (uint64_t)s * a.xs[1] + (uint64_t)h * a.xs[2]) * ES;
+    const uint32_t last = a.heads - 1u - h < (uint32_t)U - 1u ? a.heads - 1u - h : (uint32_t)U - 1u;      // of the block's heads
+    uint32_t place = 0, slot = 0;
+    if (turns) place = args.positions != 0 ? ld<uint32_t>(args.positions + ((uint64_t)b * args.ps[0] + (uint64_t)s * args.ps[1]) * 4u) : s;
+    if (stored) slot = ld<uint32_t>(args.slots + ((uint64_t)b * args.ls[0] + (uint64_t)s * args.ls[1]) * 4u);
+    const bool has = place < args.places || !turns;
+    const uint64_t cosines = args.table + (uint64_t)(has ? place : 0u) * args.ts * 4u, sines = cosines + (uint64_t)n * 4u;
     float z[U][8];
     if constexpr (VEC) {
-      float x[U][8], p[U][8], c[8], sn[8];
+      float p[U][8];                                                         // the other elements of their pairs
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[k][i] = p[k][i] = 0.0f;
-        if ((uint32_t)k < heads) {
-          const uint64_t at = xp + (uint64_t)k * sh * ES;
-          ld8<DT>(at + (uint64_t)j0 * ES, x[k]);
-          if (turned && a.pairs == 0) ld8<DT>(at + (uint64_t)(first ? j0 + n : j0 - n) * ES, p[k]);
-        }
+      for (uint32_t k = 0; k < (uint32_t)U; ++k) {
+        const uint64_t at = xp + (uint64_t)(k < last ? k : last) * a.xs[2] * ES;
+        ld8<DT>(at + j0 * ES, z[k]);
+        if (turned && !pairs) ld8<DT>(at + (first ? j0 + n : j0 - n) * ES, p[k]);
       }
+      if (turned) {
+        float c[8], sn[8];
+        if (pairs) {
+          const u4 cc = ld<u4_any>(cosines + j0 * 2u), sc = ld<u4_any>(sines + j0 * 2u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = sn[i] = 0.0f;
-      if (turned && heads != 0u) {
-        if (a.pairs != 0) {
-          const u4 cc = ld<u4_any>(cosines + (j0 / 2u) * 4u), sc = ld<u4_any>(sines + (j0 / 2u) * 4u);
+          for (int i = 0; i < 4; ++i) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) { c[i] = as_f(cc[i / 2]); sn[i] = i & 1 ? as_f(sc[i / 2]) : -as_f(sc[i / 2]); }
+            for (uint32_t k = 0; k < (uint32_t)U; ++k) {
+              const float y = z[k][2 * i], w = z[k][2 * i + 1];
+              z[k][2 * i] = y * as_f(cc[i]) - w * as_f(sc[i]);
+              z[k][2 * i + 1] = w * as_f(cc[i]) + y * as_f(sc[i]);
+            }
+          }
         } else {
-          ld8<GPUOS_F32>(cosines + (first ? j0 : j0 - n) * 4u, c);
-          ld8<GPUOS_F32>(sines + (first ? j0 : j0 - n) * 4u, sn);
+          const uint32_t at = (first ? j0 : j0 - n) * 4u, sign = first ? 0x80000000u : 0u;
+          ld8<GPUOS_F32>(cosines + at, c);
+          ld8<GPUOS_F32>(sines + at, sn);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sn[i] = first ? -sn[i] : sn[i];
+          for (int i = 0; i < 8; ++i) {
+            sn[i] = as_f(as_u(sn[i]) ^ sign);
+#pragma unroll
+            for (uint32_t k = 0; k < (uint32_t)U; ++k) z[k][i] = z[k][i] * c[i] + p[k][i] * sn[i];
+          }
         }
-      }
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[k][i] = turned ? x[k][i] * c[i] + (a.pairs != 0 ? x[k][i ^ 1] : p[k][i]) * sn[i] : x[k][i];
       }
     } else {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
         const uint32_t j = j0 + i;
         z[0][i] = 0.0f;
-        if (heads != 0u && i < left) {
-          z[0][i] = ld_elem<DT>(xp + (uint64_t)j * sd * ES);
+        if (i < left) {
+          z[0][i] = ld_elem<DT>(xp + (uint64_t)j * a.xs[3] * ES);
           if (turns && j < 2u * n) {
-            const uint32_t o = a.pairs != 0 ? j ^ 1u : (j < n ? j + n : j - n), at = a.pairs != 0 ? j / 2u : (j < n ? j : j - n);
-            const float c = ld<float>(cosines + (uint64_t)at * 4u), sn = ld<float>(sines + (uint64_t)at * 4u), p = ld_elem<DT>(xp + (uint64_t)o * sd * ES);
-            z[0][i] = z[0][i] * c + p * ((a.pairs != 0 ? (j & 1u) == 0u : j < n) ? -sn : sn);
+            const uint32_t o = pairs ? j ^ 1u : (j < n ? j + n : j - n), at = pairs ? j / 2u : (j < n ? j : j - n);
+            const float c = ld<float>(cosines + (uint64_t)at * 4u), sn = ld<float>(sines + (uint64_t)at * 4u), p = ld_elem<DT>(xp + (uint64_t)o * a.xs[3] * ES);
+            z[0][i] = z[0][i] * c + p * ((pairs ? (j & 1u) == 0u : j < n) ? -sn : sn);
           }
         }
       }
     }
-    const bool kept = slot < a.pages * a.page;
-    const uint32_t page = divided(kept ? slot : 0u, a.by_page), in = slot - page * a.page;
+    if (__builtin_amdgcn_ballot_w64(!has) != 0) {                            // a position outside the table
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if (__builtin_amdgcn_ballot_w64((uint32_t)k < heads) == 0) continue;       // (the same in every lane: the maxima need them all)
-      if (!has) {
+      for (uint32_t k = 0; k < (uint32_t)U; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[k][i] = (uint32_t)i < left ? __builtin_nanf("") : 0.0f;
+        for (uint32_t i = 0; i < 8; ++i) z[k][i] = has || i >= left ? z[k][i] : __builtin_nanf("");
       }
-      const bool here = (uint32_t)k < heads;
-      if (kind == 0u && here) {
-        const uint64_t to = a.out + ((uint64_t)b * a.os[0] + (uint64_t)s * a.os[1] + (uint64_t)(h + k) * a.os[2]) * ES;
-        if (VEC) st8<DT>(to + (uint64_t)j0 * ES, z[k]);
+    }
+    if (!stored) {
+      const uint64_t to = a.to + ((uint64_t)b * a.ts[0] + (uint64_t)s * a.ts[1] + (uint64_t)h * a.ts[2]) * ES;
+#pragma unroll
+      for (uint32_t k = 0; k < (uint32_t)U; ++k) {
+        if (!there || k > last) continue;
+        const uint64_t at = to + (uint64_t)k * a.ts[2] * ES;
+        if constexpr (VEC) st8<DT>(at + j0 * ES, z[k]);
         else {
 #pragma unroll
           for (uint32_t i = 0; i < 8; ++i) {
-            if (i < left) st_elem<DT>(to + (uint64_t)(j0 + i) * a.os[3] * ES, z[k][i]);
+            if (i < left) st_elem<DT>(at + (uint64_t)(j0 + i) * a.ts[3] * ES, z[k][i]);
           }
         }
       }
+      continue;
+    }
+    const bool kept = there && slot < args.pages * args.page;
+    const uint32_t page = divided(kept ? slot : 0u, args.by_page), in = kept ? slot - page * args.page : 0u;
+    const uint64_t to = a.to + (uint64_t)page * a.ts[0] + (uint64_t)in * a.ts[1] + (uint64_t)h * a.ts[2];
+    const uint64_t scale_to = a.scales + ((uint64_t)page * a.ss[0] + (uint64_t)in * a.ss[1] + (uint64_t)h * a.ss[2] + (uint64_t)(u >> lg_width) * a.ss[3]) * 4u;
+    const float qmax = format == CF_E2M1 ? 6.0f : (format == CF_I8 ? 127.0f : 448.0f);
+#pragma unroll
+    for (uint32_t k = 0; k < (uint32_t)U; ++k) {
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t m = as_u(z[k][i]) & 0x7fffffffu;
         top = m > top ? m : top;
       }
-      for (uint32_t w = 1; w < width; w *= 2) {
-        const uint32_t m = (uint32_t)__shfl_xor((int)top, (int)w, 64);
-        top = m > top ? m : top;
-      }
-      if (kind != 0u && here && kept) {
-        const float qmax = a.format == CF_E2M1 ? 6.0f : (a.format == CF_I8 ? 127.0f : 448.0f);
-        const float m = __builtin_fmaxf(as_f(top), 0x1p-100f), inv = qmax / m;
-        const bool bad = top >= 0x7f800000u;
-        float y[8];
+      top = most_of(top, width);                                             // (lanes without elements have the last one's)
+      const float m = __builtin_fmaxf(as_f(top), 0x1p-100f), inv = qmax / m;
+      const bool bad = top >= 0x7f800000u;
+      if (__builtin_amdgcn_ballot_w64(bad) != 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = bad ? 0.0f : z[k][i] * inv;
-        const u2 w = encode(y, a.format);
-        const bool v = kind == 2u;
-        const uint64_t to = (v ? a.kv[1].cache : a.kv[0].cache) + (uint64_t)page * (v ? a.kv[1].cs[0] : a.kv[0].cs[0]) +
-                            (uint64_t)in * (v ? a.kv[1].cs[1] : a.kv[0].cs[1]) + (uint64_t)(h + k) * (v ? a.kv[1].cs[2] : a.kv[0].cs[2]);
-        if (a.format == CF_E2M1) {
-          if (VEC || left == 8u) st<u1_any>(to + j0 / 2u, w[0]);
-          else for (uint32_t i = 0; i < left / 2u; ++i) st<uint8_t>(to + j0 / 2u + i, (uint8_t)(w[0] >> (8u * i)));
-        } else {
-          if (VEC || left == 8u) st<u2_any>(to + j0, w);
-          else for (uint32_t i = 0; i < left; ++i) st<uint8_t>(to + j0 + i, (uint8_t)((i < 4u ? w[0] : w[1]) >> (8u * (i & 3u))));
-        }
-        if ((u & (width - 1u)) == 0u) {
-          const uint64_t at = (v ? a.kv[1].scales : a.kv[0].scales) + ((uint64_t)page * (v ? a.kv[1].ss[0] : a.kv[0].ss[0]) + (uint64_t)in * (v ? a.kv[1].ss[1] : a.kv[0].ss[1]) +
-                              (uint64_t)(h + k) * (v ? a.kv[1].ss[2] : a.kv[0].ss[2]) + (uint64_t)(u >> lg_width) * (v ? a.kv[1].ss[3] : a.kv[0].ss[3])) * 4u;
-          st<float>(at, bad ? __builtin_nanf("") : m / qmax);
-        }
+        for (int i = 0; i < 8; ++i) z[k][i] = bad ? 0.0f : z[k][i];
       }
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = z[k][i] * inv;
+      const u2 w = encode(y, format);
+      if (!kept || k > last) continue;
+      const uint64_t at = to + (uint64_t)k * a.ts[2];
+      if (format == CF_E2M1) {
+        if (VEC || left == 8u) st<u1_any>(at + j0 / 2u, w[0]);
+        else for (uint32_t i = 0; i < left / 2u; ++i) st<uint8_t>(at + j0 / 2u + i, (uint8_t)(w[0] >> (8u * i)));
+      } else {
+        if (VEC || left == 8u) st<u2_any>(at + j0, w);
+        else for (uint32_t i = 0; i < left; ++i) st<uint8_t>(at + j0 + i, (uint8_t)((i < 4u ? w[0] : w[1]) >> (8u * (i & 3u))));
+      }
+      if ((u & (width - 1u)) == 0u) st<float>(scale_to + (uint64_t)k * a.ss[2] * 4u, bad ? __builtin_nanf("") : m / qmax);
     }
   }
 }
 
 int launch_append(const AppendArgs& a, void* stream) {
+  const uint32_t chunks = a.side[0].chunks > a.side[1].chunks ? a.side[0].chunks : a.side[1].chunks;
   const void* const kernels[] = {(const void*)gpuos_cache_append_kernel<GPUOS_F32, true>,   (const void*)gpuos_cache_append_kernel<GPUOS_F16, true>,
                                  (const void*)gpuos_cache_append_kernel<GPUOS_BF16, true>,  (const void*)gpuos_cache_append_kernel<GPUOS_F32, false>,
                                  (const void*)gpuos_cache_append_kernel<GPUOS_F16, false>, (const void*)gpuos_cache_append_kernel<GPUOS_BF16, false>};
   void* args[] = {(void*)&a};
-  return (int)hipLaunchKernel(kernels[a.dtype + (a.vec ? 0u : 3u)], dim3(a.chunks), dim3(kThreads), args, 0, (hipStream_t)stream);
+  return (int)hipLaunchKernel(kernels[a.dtype + (a.vec ? 0u : 3u)], dim3(chunks, 3), dim3(kThreads), args, 0, (hipStream_t)stream);
 }
 
 // ---------------------------------------------------------------------------
