@@ -38,10 +38,14 @@ PyObject* key(PyObject*, PyObject* arg) {
         return nullptr;
       }
       const at::Tensor& t = THPVariable_Unpack(o);
+      if (t.layout() != at::kStrided) {
+        PyErr_SetString(PyExc_ValueError, "a tensor without strides");
+        return nullptr;
+      }
       const c10::Device d = t.device();
       put(to, t.dim() | (int64_t)t.scalar_type() << 8 | (int64_t)(uint8_t)d.type() << 16 | (int64_t)(uint8_t)d.index() << 24 |
                   (int64_t)t.is_neg() << 32 | (int64_t)t.is_conj() << 33);
-      const at::IntArrayRef sizes = t.sizes(), strides = t.strides();      // (of a layout without strides: an exception)
+      const at::IntArrayRef sizes = t.sizes(), strides = t.strides();
       for (int64_t n : sizes) put(to, n);
       for (int64_t n : strides) put(to, n);
       grad = grad || t.requires_grad();

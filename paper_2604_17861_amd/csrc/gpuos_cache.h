@@ -1,7 +1,6 @@
 // gpuos_cache.h -- cache operators (gpuos_cache_task): what their kernels are given and, for the host, the check of a
 // descriptor and its packing.
 #pragma once
-#include <stdlib.h>
 #include "gpuos_model.h"
 
 namespace gpuos {
@@ -174,7 +173,6 @@ class CachePack : ModelPack {
     a->by_fours = a->group == 32 && a->kv[0].ss[3] == 1 && a->kv[1].ss[3] == 1 ? 1u : 0u;
     // Four heads of a row that lie together are read together, if their queries fit into LDS; else a workgroup has a head.
     a->by_head = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
-    if (getenv("GH")) a->by_head = atoi(getenv("GH"));
     a->heads = a->by_head ? (a->hk + 3) / 4 : a->hk;
     const uint64_t pairs = (uint64_t)b * a->heads * a->tiles;
     a->pieces = pieces(pairs, (uint64_t)seen, a->by_head ? 128 : 512);
@@ -200,11 +198,12 @@ class CachePack : ModelPack {
     return GPUOS_OK;
   }
 
-  // Pieces that a sequence's rows are cut into, each a workgroup's; a second launch joins them.
+  // Pieces that a sequence's rows are cut into, each a workgroup's, for 768 workgroups (three a compute unit); a second launch joins them.
+  // 64 sequences of 2,048 to 4,096 rows of 8 heads of 128, 4 bits, in 512 / 768 / 1,024 / 1,536 workgroups: 56, 55, 56, 62 us (with pieces
+  // of one length for all sequences, so more of them for the longer ones, 67).
   static uint32_t pieces(uint64_t pairs, uint64_t seen, uint64_t least) {
-    static const uint64_t T = getenv("GT") ? atoi(getenv("GT")) : 768, MN = getenv("GM") ? atoi(getenv("GM")) : least;
-    uint64_t n = (T + pairs - 1) / pairs;
-    const uint64_t most = (seen + MN - 1) / MN;
+    uint64_t n = (768 + pairs - 1) / pairs;
+    const uint64_t most = (seen + least - 1) / least;
     if (n > most) n = most;
     if (n > kPiecesMost) n = kPiecesMost;
     return n < 1 ? 1u : (uint32_t)n;

@@ -854,7 +854,7 @@ template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads
     for (uint32_t i = 0; i < 8; ++i) {
       v[i] = f4{0, 0, 0, 0};
       const uint32_t k = k0 + i * parts;
-      if (has && k < a.pieces) v[i] = __builtin_bit_cast(f4, ld<u4_any>(from + (uint64_t)k * all * a.d * 4u));
+      if (has && k < a.pieces && weights[k] >= 0.0f) v[i] = __builtin_bit_cast(f4, ld<u4_any>(from + (uint64_t)k * all * a.d * 4u));
     }
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
