@@ -71,6 +71,7 @@ int launch_attend(const AttendArgs& a, uint32_t format, void* stream);
 class CachePack : ModelPack {
  public:
   static constexpr uint32_t kHead = 256;   // elements of a head that attention takes
+  static constexpr int64_t kRowsMost = 1 << 30;      // rows of a sequence: what a place is computed from stays within 32 bits
   static constexpr uint64_t kBlocksMost = 14000000;      // workgroups of a launch: a grid, an eighth larger, has fewer than 2^32 threads
 
   static int append(const gpuos_cache_task& t, AppendArgs* a, bool* empty) {
@@ -157,11 +158,11 @@ class CachePack : ModelPack {
     if (lengths->ptr && (lengths->dtype != GPUOS_I32 || !operand(*lengths, 1, pz, false, false, &a->ls))) return GPUOS_E_INVAL;
     const int rc = caches(t, 1, hk, d, pages, page, groups, false, !*empty, 32, a->kv, format);
     if (rc != GPUOS_OK) return rc;
-    if (longest > width * page) return GPUOS_E_INVAL;           // the table names every row there may be
+    if (longest > width * page || longest > kRowsMost) return GPUOS_E_INVAL;      // the table names every row there may be
     if (!(t.alpha == t.alpha)) return GPUOS_E_INVAL;
     a->q = (uint64_t)q->ptr; a->out = (uint64_t)out->ptr; a->table = (uint64_t)table->ptr; a->lengths = (uint64_t)lengths->ptr;
     a->b = (uint32_t)b; a->s = (uint32_t)s; a->hq = (uint32_t)hq; a->hk = (uint32_t)hk; a->per = (uint32_t)(hq / hk); a->d = (uint32_t)d;
-    a->pages = (uint32_t)pages; a->page = (uint32_t)page; a->group = (uint32_t)(d / groups); a->longest = (uint32_t)longest; a->window = (uint32_t)window;
+    a->pages = (uint32_t)pages; a->page = (uint32_t)page; a->group = (uint32_t)(d / groups); a->longest = (uint32_t)longest; a->window = window >= longest ? 0u : (uint32_t)window;      // (one that cuts nothing off is none)
     a->dtype = q->dtype;
     a->scale = t.alpha * 1.44269504088896340736f;
     if (*empty) return GPUOS_OK;
@@ -169,7 +170,7 @@ class CachePack : ModelPack {
     a->lg_parts = d > 128 ? 1u : 0u;
     a->tiles = ((a->rows + kTileRows - 1) / kTileRows) << a->lg_parts;
     // what a tile of queries sees, at most
-    const int64_t seen = window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
+    const int64_t seen = a->window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
     a->by_fours = a->group == 32 && a->kv[0].ss[3] == 1 && a->kv[1].ss[3] == 1 ? 1u : 0u;
     // Four heads of a row that lie together are read together, if their queries fit into LDS; else a workgroup has a head.
     a->by_head = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;

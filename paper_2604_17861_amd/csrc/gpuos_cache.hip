@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
 #pragma unroll
     for (uint32_t s = 0; s < NV; ++s) {
       if constexpr (FMT == CF_E4M3) {
-        // A code that is no number makes its row none: the code becomes 0, the row's scale a NaN.
+        // A code that is no number makes its row none, in this slab and those behind it: the code becomes 0, the row's scale a NaN.
         uint32_t any = 0;
 #pragma unroll
         for (uint32_t i = 0; i < IT; ++i) {

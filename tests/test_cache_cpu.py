@@ -73,7 +73,7 @@ def test_descriptors_of_appending_that_are_refused(bad):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(d=0), dict(d=60), dict(d=264), dict(hk=3), dict(hk=0), dict(pages=0), dict(page=0), dict(groups=4), dict(groups=3), dict(longest=65), dict(longest=-1), dict(width=3), dict(window=-1), dict(flags=4),
+    dict(d=0), dict(d=60), dict(d=264), dict(hk=3), dict(hk=0), dict(pages=0), dict(page=0), dict(groups=4), dict(groups=3), dict(longest=65), dict(longest=-1), dict(longest=2 ** 30 + 1, width=2 ** 27), dict(width=3), dict(window=-1), dict(flags=4),
     dict(alpha=float("nan")), dict(b=MOST, s=2), dict(b=2 ** 20, s=2 ** 6, hq=64), dict(s=2 ** 22, hq=64),
     dict(q=NO), dict(kc=NO), dict(ks=NO), dict(vc=NO), dict(vs=NO), dict(table=NO), dict(out=NO),
     dict(q=op(I32, 256, 256, 64, 1)), dict(out=op(F16, 256, 256, 64, 1)), dict(out=op(BF16, 0, 256, 64, 1)), dict(table=op(F32, 4, 1)), dict(lengths=op(F32, 1)), dict(vc=op(I8, 2048, 128, 64, 1)),
@@ -106,7 +106,9 @@ def launched(_launched, monkeypatch):  # noqa: F811
             torch.autograd.graph.increment_version(tensors[i]) if not tensors[i].is_inference() else None
         calls.append(struct.unpack_from("<I", task)[0])
         return 0
+    make = M._empty_like
     monkeypatch.setattr(B, "launch", launch)
+    monkeypatch.setattr(M, "_empty_like", lambda x: make(x).zero_())
     return calls
 
 
@@ -210,6 +212,14 @@ def test_traces_and_tangents_are_refused(launched):
         with forward_ad.dual_level(), pytest.raises(ValueError, match="forward-mode"):
             f(forward_ad.make_dual(q, torch.ones_like(q)))
         assert len(launched) == done
+
+
+def test_a_compiled_program_calls_them(launched):
+    q, k, v, slots, caches, table = inputs()
+
+    def f(q):
+        return M.cache_attention(M.cache_append_qkv(q * 2, k, v, slots, *caches, table), *caches, PAGES, None, 8) * 0
+    assert torch.equal(torch.compile(f, backend="eager")(q), torch.zeros_like(q)) and launched == [1, 2]
 
 
 def test_tensors_without_memory_are_refused():

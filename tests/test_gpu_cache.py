@@ -246,6 +246,33 @@ def test_attention_takes_rows_of_any_strides_and_one_token_a_sequence():
     assert bool((M.cache_attention(up(q), *mine, up(pages), None, 0) == 0).all())
 
 
+@pytest.mark.parametrize("fmt,d", ((E2M1, 64), (E2M1, 72), (I8, 128), (E4M3, 40)))
+def test_codes_at_any_address(fmt, d):
+    """Rows of a cache one byte off any alignment, wider than they are, and scales of every third float."""
+    case = (2, 1, 6, 3, d, 1, 5, 200, (200, 77), 0, "plain")
+    q, caches, pages, lengths = attend_inputs(case, F16, fmt)
+    mine = []
+    for c in caches:
+        n = c.shape[-1]
+        if c.dtype == F32:
+            wide = torch.zeros(*c.shape[:-1], 3 * n, device="cuda")[..., 1::3]
+        else:
+            wide = torch.zeros(*c.shape[:-1], n + 9, dtype=torch.uint8, device="cuda").view(c.dtype)[..., 1:1 + n]
+        mine.append(wide)
+        wide.view(torch.uint8 if c.dtype != F32 else F32).copy_(c.view(torch.uint8 if c.dtype != F32 else F32).cuda())
+    got = M.cache_attention(up(q), *mine, up(pages), up(lengths), 200)
+    assert torch.equal(got, M.cache_attention(up(q), *[up(c) for c in caches], up(pages), up(lengths), 200))
+    gen = torch.Generator().manual_seed(1)
+    k, v, slots = normal(gen, 30, 3, d, dtype=F16), normal(gen, 30, 3, d, dtype=F16), torch.randperm(60, generator=gen)[:30].to(torch.int32)
+    _, want = ref.append(None, k, v, slots, caches, None, None, False)
+    M.cache_append_qkv(None, up(k), up(v), up(slots), *mine)
+    for g, w in zip(mine, want):
+        same(g.contiguous(), w)
+    rows = mine[0].view(torch.uint8) if fmt != E2M1 else mine[0]
+    base = rows.as_strided((*rows.shape[:-1], rows.shape[-1] + 9), rows.stride(), rows.storage_offset() - 1)
+    assert bool((base[..., 0] == 0).all()) and bool((base[..., rows.shape[-1] + 1:] == 0).all())      # what lies between the rows
+
+
 def test_attention_of_a_cache_past_32_bits():
     """Rows 5 GB into codes and into scales."""
     pages, page, h, d = 82000, 64, 8, 128
