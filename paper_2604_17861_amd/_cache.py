@@ -2,6 +2,7 @@
 bits, and attention that reads it as it is held.  include/gpuos.h says what they compute and take; everything here is checking
 of shapes and marshalling.  They are not differentiable: what requires a gradient is refused where gradients are recorded."""
 import struct
+import sys
 
 import torch
 from torch.autograd import forward_ad
@@ -128,6 +129,11 @@ def attention_task(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, long
                   M._operand(lengths), M._operand(oo)), scale)
 
 
+def _untraced(f):
+    """f, kept from torch.compile, under which its checks see other values than are there.  (Only where that is loaded: it takes 0.8 s.)"""
+    return torch.compiler.disable(f) if "torch._dynamo" in sys.modules else f
+
+
 def cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table=None, positions=None, *, pairs=False, out=None):
     """Rotate q and k [T, H, D] or [B, S, H, D] by the angles of table [places, R] (cosines | sines, float32; None: not at all) at the tokens'
     positions (None: 0, 1, ... in every sequence; pairs: neighbours are rotated together, else the halves), and quantise k
@@ -145,7 +151,7 @@ def cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table
     made = q is not None and out is None
     operands = (q, k, v, table, positions, slots, M._empty_like(q), k_cache, k_scales, v_cache, v_scales) if made else given
     if plan is None:
-        task = append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions, operands[6], pairs=bool(pairs))
+        task = _untraced(append_task)(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions, operands[6], pairs=bool(pairs))
         plan = M._keep(key, _Plan(task, range(11), ([] if made or q is None else [6]) + [7, 8, 9, 10], k.get_device(),
                                   k.numel() == 0 and (q is None or q.numel() == 0)))
     _run(plan, operands)
@@ -169,7 +175,7 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
     operands = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, M._empty_like(q)) if made else given
     if plan is None:
         by = float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.shape[-1] else 1.0
-        task = attention_task(*operands[:7], longest, operands[7], scale=by, window=window)
+        task = _untraced(attention_task)(*operands[:7], longest, operands[7], scale=by, window=window)
         plan = M._keep(key, _Plan(task, range(8), [] if made else [7], q.get_device(), q.numel() == 0))
     _run(plan, operands)
     return operands[7]
