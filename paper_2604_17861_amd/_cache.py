@@ -149,7 +149,7 @@ def cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table
             M._check(q, "q", M._FLOAT, (3, 4))
         M._no_gradient("cache_append_qkv", *given)
     made = q is not None and out is None
-    operands = (q, k, v, table, positions, slots, M._empty_like(q), k_cache, k_scales, v_cache, v_scales) if made else given
+    operands = (q, k, v, table, positions, slots, B.like(q), k_cache, k_scales, v_cache, v_scales) if made else given
     if plan is None:
         task = _untraced(append_task)(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions, operands[6], pairs=bool(pairs))
         plan = M._keep(key, _Plan(task, range(11), ([] if made or q is None else [6]) + [7, 8, 9, 10], k.get_device(),
@@ -172,7 +172,7 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
         M._check(q, "q", M._FLOAT, (3, 4))
         M._no_gradient("cache_attention", *given)
     made = out is None
-    operands = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, M._empty_like(q)) if made else given
+    operands = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, B.like(q)) if made else given
     if plan is None:
         by = float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.shape[-1] else 1.0
         task = _untraced(attention_task)(*operands[:7], longest, operands[7], scale=by, window=window)

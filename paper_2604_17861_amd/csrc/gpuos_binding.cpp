@@ -108,8 +108,24 @@ PyObject* launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// like(tensor): an empty tensor of its shape, dtype and device, without strides of its own.
+PyObject* like(PyObject*, PyObject* o) {
+  if (!THPVariable_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, "a tensor");
+    return nullptr;
+  }
+  try {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return THPVariable_Wrap(at::empty(t.sizes(), t.options().requires_grad(false)));
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef methods[] = {{"key", key, METH_O, "a call's tensors without their addresses"},
                          {"launch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(launch)), METH_FASTCALL, "a descriptor with its tensors' addresses"},
+                         {"like", like, METH_O, "an empty tensor like one"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

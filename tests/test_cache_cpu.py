@@ -106,9 +106,9 @@ def launched(_launched, monkeypatch):  # noqa: F811
             torch.autograd.graph.increment_version(tensors[i]) if not tensors[i].is_inference() else None
         calls.append(struct.unpack_from("<I", task)[0])
         return 0
-    make = M._empty_like
+    make = B.like
     monkeypatch.setattr(B, "launch", launch)
-    monkeypatch.setattr(M, "_empty_like", lambda x: make(x).zero_())
+    monkeypatch.setattr(B, "like", lambda x: make(x).zero_())
     return calls
 
 
