@@ -74,6 +74,11 @@ template <uint32_t DT> DEV void st4(uint64_t p, f4 f) {
 // for), and written once, in 16 or 32 bits or as codes.  A power of two of lanes holds a row, eight elements each; what goes over
 // lanes is a group's maximum.  Products and sums of the rotation are rounded by themselves (no fused multiply-add), so that the codes
 // are those of the definition.
+// Queries, keys and values are the grid's second index, so that what a workgroup does is the same in all its lanes: with heads of all three in one
+// list, chosen by lanes, an item took 600 vector instructions, and those were what bounded it: 16,384 tokens of 32 + 8 + 8 heads of 128 bf16
+// into 4 bits 103 us, so 82 (364 MB, 4.4 TB/s; a large copy makes 5.0); 8,192 of 16 + 16 + 16 of fp16 into e4m3 56 and 37.6 (170 MB, 4.5).  A token of
+// 32 heads 4.2 us: three trips to memory.  Blocks of four heads instead of two cost a token 1.6 us and gain nothing, stores past
+// the caches neither.
 // ---------------------------------------------------------------------------
 // eight codes of |y| <= qmax (1 + 2^-23): to the nearest, to the even one of two
 DEV u2 encode(const float* y, uint32_t format) {
@@ -276,6 +281,14 @@ int launch_append(const AppendArgs& a, void* stream) {
 // The first product is K Q^T: lane (n, g) then holds the scores of query n and rows 4 g .. 4 g + 3 of either half, and these eight are the
 // inputs of its part of the second, V^T P^T, if the rows are summed in that order: scores never change lanes, and a query's maximum, sum and
 // results are all in lanes of its number.  64 rows go at a time, four tiles of the first product, two steps of the second.
+//
+// A token a sequence: bound by memory.  64 sequences of 2,048 to 4,096 rows (8 heads of 128, 4 bits, 32 queries, 215 MB) 55 us (3.9 TB/s) and
+// 5 for joining; without any product, loads and LDS alone, the same.  128 sequences of 4,096 take 52 us more than 64 (287 MB, 5.5 TB/s), so some 15 are begin
+// and end: lengths, page table, keys, values, each a trip to memory behind the other.  131,072 rows of one (a scale for 32 elements, 168 MB) 43 and 6.  A
+// request of 301 rows 8.8.  A second slab on its way made no difference.
+// Prompts: bound by vector instructions, some 430 for 64 rows and 16 queries (a third conversions), 48 matrix instructions beside them: 1,024 queries of
+// 32 heads behind 3,072 rows 135 us, 450 TFLOP/s; 4 of those 515.  (Four wavefronts that share what one of them has converted, as bf16 in LDS, were no
+// faster: 326 and 512; two barriers for 64 rows cost what the conversions do.)
 // ---------------------------------------------------------------------------
 template <uint32_t FMT> struct Code { static constexpr uint32_t BITS = FMT == CF_E2M1 ? 4u : 8u; };
 
@@ -351,7 +364,8 @@ DEV AttendPlace attend_place(const AttendArgs& a) {
   return p;
 }
 
-// A wavefront's codes go by way of LDS, 64 rows by 64 bytes at a time (a slab): read from memory in pieces of 16 bytes, four lanes a row, the
+// A wavefront's codes go by way of LDS (from memory straight to the lanes that multiply, each load touched 16 or 64 lines, and values of
+// more than one scale came byte by byte), 64 rows by 64 bytes at a time (a slab): read from memory in pieces of 16 bytes, four lanes a row, the
 // next slab on its way while one is worked on.  Piece c of row t lies in place c ^ swizzle(t), so that neither product's reads meet in a
 // bank: for the first a lane reads its row's codes, for the second a column's of 16 rows (4 bits) or eight, which the LDS transposes.
 DEV uint32_t swizzle(uint32_t t) { return ((t >> 2) ^ (t >> 4)) & 3u; }
