@@ -586,7 +586,8 @@ int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t ou
 
 /* A cache operator on `stream`, as gpuos_launch_model: nothing is allocated or waited for, and the call may be captured.
  * workspace: device memory, 16-byte aligned, of as many bytes as gpuos_cache_workspace says (GPUOS_E_NOMEM: fewer); it
- * belongs to the call until its kernels have run, so two calls that may run at a time need one each. */
+ * belongs to the call until its kernels have run, so two calls that may run at a time need one each.
+ * These kernels have room beside a worker as those of gpuos_launch_model have. */
 int gpuos_launch_cache(int32_t device, const gpuos_cache_task* task, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* The workspace that a task needs, in bytes; 0 for most.  It depends on sizes alone.  No GPU needed. */

@@ -47,7 +47,7 @@ struct AttendArgs {
 constexpr uint32_t kAppendBlock = 2;       // heads of an item
 constexpr uint32_t kTileRows = 16;         // queries of a tile: a side of a matrix instruction's result
 constexpr uint32_t kTileTokens = 64;       // rows of the cache that a wavefront takes at once
-constexpr uint32_t kPiecesMost = 256;
+constexpr uint32_t kPiecesMost = 256;      // (one sequence of 131,072 rows, 8 heads, in 128 / 256 / 384: 61, 44, 48 us, and 5.8, 7.1, 7.5 for joining)
 
 // Elements of a head that the kernel of a head's d has room for.
 constexpr uint32_t attend_room(uint32_t d, uint32_t dt) { return d == 64u && dt != GPUOS_F32 ? 64u : (d <= 128u ? 128u : 256u); }
@@ -172,14 +172,17 @@ class CachePack : ModelPack {
     // what a tile of queries sees, at most
     const int64_t seen = a->window != 0 && window + s - 1 < longest ? window + s - 1 : longest;
     a->by_fours = a->group == 32 && a->kv[0].ss[3] == 1 && a->kv[1].ss[3] == 1 ? 1u : 0u;
-    // Four heads of a row that lie together are read together, if their queries fit into LDS; else a workgroup has a head.
+    // Four heads of a row that lie together are read together, by a wavefront each, if their queries fit into LDS; else a workgroup has a head, and its
+    // wavefronts every fourth 64 rows.  64 sequences of 4,096 rows of 8 heads of 128, int8: 134 and 162 us, 4 bits 75 and 80.  (Short ones are cut into
+    // rows all the same: with a head each a wavefront has more of them behind each other.)
     a->by_head = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
     a->heads = a->by_head ? (a->hk + 3) / 4 : a->hk;
     const uint64_t pairs = (uint64_t)b * a->heads * a->tiles;
     a->pieces = pieces(pairs, (uint64_t)seen, a->by_head ? 128 : 512);
     if (pairs * a->pieces > kBlocksMost) return GPUOS_E_INVAL;
     a->blocks = (uint32_t)(pairs * a->pieces);
-    // All heads of a piece of a sequence go to one die, if the dies then have about as much to do; else all queries of a head; else each workgroup to the next.
+    // All heads of a piece of a sequence go to one die, if the dies then have about as much to do; else all queries of a head; else each workgroup to the
+    // next.  (By the first rule alone 1,024 queries of one sequence were all on one die: 825 us, so 130.)
     const uint32_t inners[2] = {a->heads * a->tiles, a->tiles};
     a->inner = 1;
     for (uint32_t n : inners) {
@@ -199,7 +202,8 @@ class CachePack : ModelPack {
     return GPUOS_OK;
   }
 
-  // Pieces that a sequence's rows are cut into, each a workgroup's, for 768 workgroups (three a compute unit); a second launch joins them.
+  // Pieces that a sequence's rows are cut into, each a workgroup's, of 512 rows at least, of 128 where a wavefront has a head (one sequence of 301 rows: 9.0 us,
+  // in two pieces 6.5 and 3.7 for joining), for 768 workgroups (three a compute unit); a second launch joins them.
   // 64 sequences of 2,048 to 4,096 rows of 8 heads of 128, 4 bits, in 512 / 768 / 1,024 / 1,536 workgroups: 56, 55, 56, 62 us (with pieces
   // of one length for all sequences, so more of them for the longer ones, 67).
   static uint32_t pieces(uint64_t pairs, uint64_t seen, uint64_t least) {

@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
       offs[v * 64u + lane] = a.kv[v].cache + (uint64_t)head * a.kv[v].cs[2] + e * a.kv[v].cs[0] + (uint64_t)in * a.kv[v].cs[1];
       const uint64_t sp = a.kv[v].scales + ((uint64_t)head * a.kv[v].ss[2] + e * a.kv[v].ss[0] + (uint64_t)in * a.kv[v].ss[1]) * 4u;
       float f[GROUPS];                                             // (of more than one scale: that of each 32 elements)
-      if (MULTI && a.by_fours != 0u) {
+      if (MULTI && a.by_fours != 0u) {                             // (131,072 rows with a scale for 32: 54 us, so 43)
 #pragma unroll
         for (uint32_t q = 0; q < GROUPS; q += 4) {
           const uint32_t left = FULL ? GROUPS - q : (32u * q < d ? (d - 32u * q + 31u) / 32u : 0u);
@@ -819,9 +819,10 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
 }
 
 // The pieces' sums.  A query has a wavefront, or, of more than 64 pieces, the workgroup (WIDE); a part of a wavefront has a quarter of the head's
-// elements in lanes and every so many of the pieces, eight on their way at a time.  2,048 queries of 128 elements, 8 pieces: 5.3 us (with a
-// workgroup each 9).
-constexpr uint32_t kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
+// elements in lanes and every so many of the pieces, six on their way at a time (eight do not fit into
+// 64 registers).  2,048 queries of 128 elements, 6 pieces: 4.7 us (with a
+// workgroup each 7.6).
+constexpr uint32_t kJoinThreads = 512, kJoinWaves = kJoinThreads / 64, kJoinAhead = 6;
 template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads, 8) gpuos_cache_join_kernel(const AttendArgs a) {
   __shared__ alignas(16) float weight[WIDE ? kPiecesMost : kJoinWaves * 64u], sums[WIDE ? kJoinWaves : 1][256], tops[kJoinWaves], totals[kJoinWaves];
   const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u;
@@ -862,16 +863,16 @@ template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads
   f4 sum = {0, 0, 0, 0};
   const bool has = e < a.d;
   const uint64_t from = a.part + (mine * a.d + (has ? e : 0u)) * 4u;
-  for (uint32_t k0 = first; k0 < a.pieces; k0 += 8u * parts) {
-    f4 v[8];
+  for (uint32_t k0 = first; k0 < a.pieces; k0 += kJoinAhead * parts) {
+    f4 v[kJoinAhead];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
+    for (uint32_t i = 0; i < kJoinAhead; ++i) {
       v[i] = f4{0, 0, 0, 0};
       const uint32_t k = k0 + i * parts;
       if (has && k < a.pieces && weights[k] >= 0.0f) v[i] = __builtin_bit_cast(f4, ld<u4_any>(from + (uint64_t)k * all * a.d * 4u));
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
+    for (uint32_t i = 0; i < kJoinAhead; ++i) {
       const uint32_t k = k0 + i * parts;
       const float w = k < a.pieces ? weights[k] : -1.0f;
 #pragma unroll

@@ -4,11 +4,14 @@
     cache_store_kv(k, v, slots, k_cache, k_scales, v_cache, v_scales)  # into a paged cache of 8-bit values (this and on: no gradients)
     k, v = cache_load_kv(k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, dtype=q.dtype)
     x = penalize_logits(x, history=tokens, params=params, allowed=bits)
+    q = cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table, positions)        # rotated, into a cache of 4 or 8 bits
+    o = cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, longest)              # over the cache as it is held
 
 The functions launch the library's kernels on PyTorch's current stream of the tensors' device (gpuos_launch_model): they
 wait for nothing, and may be captured into a graph.  The `*_task` functions make the descriptors that the functions
 launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as tasks of the ring (bind the operators with
-`register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  include/gpuos.h says what every operator computes and takes.
+`register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  (The last two are kernels only,
+gpuos_launch_cache.)  include/gpuos.h says what every operator computes and takes.
 
 PyTorch sees no operators here.  norm_rope and norm_rope_qk are autograd functions; everything else is refused where a gradient would be
 lost, and so are second derivatives, forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a
