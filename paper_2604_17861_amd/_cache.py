@@ -8,7 +8,6 @@ import torch
 from torch.autograd import forward_ad
 from torch.fx import _symbolic_trace
 
-from . import _binding as B
 from . import model as M
 from . import runtime as R
 from . import streams as S
@@ -40,6 +39,20 @@ def _check_caches(dev, hk, d, k_cache, k_scales, v_cache, v_scales):
     M._check(v_scales, "v_scales", M._F32, (4,), k_scales.shape, dev)
     M._need(k_scales.shape[:3] == k_cache.shape[:3] and k_scales.shape[3] >= 1 and d % k_scales.shape[3] == 0,
             "scales are [pages, page, heads, groups] of the caches %s, not %s", list(k_cache.shape), list(k_scales.shape))
+
+
+B = None                           # the module _binding, with the first call
+
+
+def _load():
+    """As runtime.lib: what is not built raises with the first call, not with the import."""
+    global B
+    try:
+        from . import _binding
+    except ImportError as e:
+        raise FileNotFoundError("_binding.so is not built for this PyTorch; run `python -m paper_2604_17861_amd.build`") from e
+    B = _binding
+    return B
 
 
 class _Plan:
@@ -142,7 +155,7 @@ def cache_append_qkv(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table
     (float32), in one launch.  Returns q' (out may be q; None without q).  Slots are distinct.  Not differentiable: what
     requires a gradient is refused where gradients are recorded."""
     given = (q, k, v, table, positions, slots, out, k_cache, k_scales, v_cache, v_scales)      # in the descriptor's order
-    key = B.key(given) + (b"append pairs" if pairs else b"append")
+    key = (B or _load()).key(given) + (b"append pairs" if pairs else b"append")
     plan = M._plans.get(key)
     if plan is None:
         if q is not None and out is None:
@@ -166,7 +179,7 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
     sees nothing gets zeros.  Not differentiable: what requires a gradient is refused where gradients are recorded."""
     longest, window = int(longest), int(window)
     given = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, out)      # in the descriptor's order
-    key = B.key(given), longest, window, scale if scale is None else float(scale)
+    key = (B or _load()).key(given), longest, window, scale if scale is None else float(scale)
     plan = M._plans.get(key)
     if plan is None:
         M._check(q, "q", M._FLOAT, (3, 4))
