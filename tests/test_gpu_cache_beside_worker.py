@@ -61,8 +61,12 @@ def test_a_dispatch_filters_tasks_are_waited_for():
     q, caches, pages, lengths = attend_inputs((2, 1, 4, 4, 64, 1, 16, 60, (60, 33), 0, "plain"), F32, I8)
     x, mine, table, n = up(q), [up(c) for c in caches], up(pages), up(lengths)
     want = M.cache_attention(x * 0.5 + 0.25, *mine, table, n, 60) * 2.0
-    for _ in range(5):
-        with GpuosMode():
-            y = x * 0.5 + 0.25
-            got = M.cache_attention(y, *mine, table, n, 60) * 2.0
-        assert torch.equal(got, want)
+    mode = GpuosMode(wait_timeout_ms=20000, idle_exit_ms=5000)
+    try:
+        for _ in range(5):
+            with mode:
+                y = x * 0.5 + 0.25
+                got = M.cache_attention(y, *mine, table, n, 60) * 2.0
+            assert torch.equal(got, want)
+    finally:
+        mode.close()
