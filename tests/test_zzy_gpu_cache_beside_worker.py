@@ -8,7 +8,7 @@ import torch
 from paper_2604_17861_amd import model as M
 from paper_2604_17861_amd import runtime as R
 from paper_2604_17861_amd.dispatch import GpuosMode
-from test_gpu_cache import E2M1, E4M3, I8, attend_inputs, caches_of
+from test_zzy_gpu_cache import E2M1, E4M3, I8, attend_inputs, caches_of
 from test_gpu_model import BF16, F16, F32, _let_go, laid, normal, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu

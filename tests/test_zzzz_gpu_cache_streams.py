@@ -7,7 +7,7 @@ import torch
 
 import cache_reference as ref
 from paper_2604_17861_amd import model as M
-from test_gpu_cache import E2M1, I8, attend_inputs, caches_of, close
+from test_zzy_gpu_cache import E2M1, I8, attend_inputs, caches_of, close
 from test_gpu_model import BF16, F16, _let_go, normal, same, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
