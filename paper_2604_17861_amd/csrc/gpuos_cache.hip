@@ -287,7 +287,7 @@ int launch_append(const AppendArgs& a, void* stream) {
 // and end: lengths, page table, keys, values, each a trip to memory behind the other.  131,072 rows of one (a scale for 32 elements, 168 MB) 43 and 6.  A
 // request of 301 rows 8.8.  A second slab on its way made no difference.
 // Prompts: bound by vector instructions, some 430 for 64 rows and 16 queries (a third conversions), 48 matrix instructions beside them: 1,024 queries of
-// 32 heads behind 3,072 rows 135 us, 450 TFLOP/s; 4 of those 515.  (Four wavefronts that share what one of them has converted, as bf16 in LDS, were no
+// 32 heads, the last of 4,096 rows, 135 us, 450 TFLOP/s; 4 of those 515.  (Four wavefronts that share what one of them has converted, as bf16 in LDS, were no
 // faster: 326 and 512; two barriers for 64 rows cost what the conversions do.)
 // ---------------------------------------------------------------------------
 template <uint32_t FMT> struct Code { static constexpr uint32_t BITS = FMT == CF_E2M1 ? 4u : 8u; };
@@ -509,23 +509,40 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
       }
     }
   };
+  // A row's pieces end where the row does: the last, of 4, 8 or 12 bytes, is asked for as the row's last 16 (loads of words behind a branch
+  // waited for those in front of them: 16 sequences of up to 4,096 rows, 8 heads of 96, 4 bits, 26.5 us, so 22.5).
+  const uint32_t row_bytes = d * BITS / 8u;
+  const auto moved = [&](uint32_t s) -> uint32_t {                 // by so many bytes
+    const uint32_t past = 64u * s + 16u * (hidden(lane) & (CH - 1u)) + 16u;
+    return (past > row_bytes ? past : row_bytes) - row_bytes;
+  };
   const auto ask = [&](uint32_t v, uint32_t s) {
+    const uint32_t c = (FULL ? lane : hidden(lane)) & (CH - 1u), e = 64u * s + 16u * c;
+    if (FULL || row_bytes >= 16u) {
+      const uint32_t from = FULL || e + 16u <= row_bytes ? e : row_bytes - 16u;
 #pragma unroll
-    for (uint32_t i = 0; i < IT; ++i) {
-      const uint32_t c = lane & (CH - 1u);
-      const uint64_t p = offs[v * 64u + i * (64u / CH) + lane / CH] + 64u * s + 16u * c;
-      if (FULL) r[i] = ld<u4_byte>(p);
-      else {
-        const uint32_t row_bytes = d * BITS / 8u, e = 64u * s + 16u * c;
+      for (uint32_t i = 0; i < IT; ++i) r[i] = ld<u4_byte>(offs[v * 64u + i * (64u / CH) + lane / CH] + from);
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < IT; ++i) {
+        const uint64_t p = offs[v * 64u + i * (64u / CH) + lane / CH] + e;
         r[i] = u4{0, 0, 0, 0};
-        if (e + 16u <= row_bytes) r[i] = ld<u4_byte>(p);
-        else {
 #pragma unroll
-          for (uint32_t w = 0; w < 4; ++w) {
-            if (e + 4u * w < row_bytes) r[i][w] = ld<u1_any>(p + 4u * w);
-          }
+        for (uint32_t w = 0; w < 3; ++w) {
+          if (e + 4u * w < row_bytes) r[i][w] = ld<u1_any>(p + 4u * w);
         }
       }
+    }
+  };
+  // what `ask` asked for further in front goes where it belongs; what is behind the row meets zeros of the query, or is a result that nobody stores:
+  // it is cleared only where a code may be no number
+  const auto settle = [&](uint32_t s) {
+    if (FULL || row_bytes < 16u || (FMT != CF_E4M3 && (row_bytes & 15u) == 0u)) return;
+    const uint32_t by = moved(s);
+#pragma unroll
+    for (uint32_t i = 0; i < IT; ++i) {
+      const u4 w = r[i], o = by & 4u ? u4{w[1], w[2], w[3], 0} : w, h = by & 8u ? u4{o[2], o[3], 0, 0} : o;
+      r[i] = by < 16u ? h : u4{0, 0, 0, 0};
     }
   };
   // Places in LDS: of piece c of row t, 64 t + 16 (c ^ swizzle(t)).  Those of a lane differ by an exclusive or and a constant from the first,
@@ -578,6 +595,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     for (int T = 0; T < 4; ++T) x[T] = c[T] = f4{0, 0, 0, 0};
 #pragma unroll
     for (uint32_t s = 0; s < NS; ++s) {
+      settle(s);
       put();
       wave_sync();
       if (s + 1u < NS) ask(0, s + 1u);
@@ -701,6 +719,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
           }
         }
       }
+      settle(first_slab + s);
       put();
       wave_sync();
       if (s + 1u < NV) ask(1, first_slab + s + 1u);
