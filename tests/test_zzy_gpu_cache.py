@@ -189,6 +189,22 @@ def test_attention(case, dtype, fmt):
 
 
 @pytest.mark.parametrize("fmt", (E2M1, I8, E4M3))
+@pytest.mark.parametrize("d", (16, 24, 32, 48, 56, 72, 88, 104, 120, 136, 152, 184, 200, 216, 248))
+def test_rows_that_end_inside_a_piece_of_a_load(d, fmt):
+    """A row's bytes modulo 16 take every value there is; what lies beside a head's codes is another's, or a code that is no number."""
+    dtype = (BF16, F16, F32)[d // 8 % 3]
+    q, caches, pages, lengths = attend_inputs((2, 2, 6, 3, d, 1, 5, 140, (140, 66), 0, "plain"), dtype, fmt, seed=d)
+    if fmt == E4M3:
+        for c in caches[::2]:
+            assert c.dtype == E4M3
+            c.view(torch.uint8)[:, :, 1] = 0x7f                  # the head between the others: its own queries' results are none
+    mine = [on_gpu(c) for c in caches]
+    got = M.cache_attention(up(q), *mine, up(pages), up(lengths), 140)
+    o = close(got, q, caches, pages, lengths, 140, d ** -0.5, 0)
+    assert bool(torch.isnan(o[:, :, 2:4]).all()) == (fmt == E4M3) and not torch.isnan(o[:, :, :2]).any() and not torch.isnan(o[:, :, 4:]).any()
+
+
+@pytest.mark.parametrize("fmt", (E2M1, I8, E4M3))
 @pytest.mark.parametrize("multi", (1, 2))
 def test_attention_of_what_is_not_seen(fmt, multi):
     """Behind the lengths, before a window, in pages that no table names: scales that are no numbers, infinite or huge, codes that are none."""
