@@ -330,7 +330,7 @@ typedef struct gpuos_model_task {
  *   Sequence b has lengths[b] rows in the cache, the S queries' own last: query s is at n = lengths[b] - S + s and sees the rows t <= n,
  *   with a window above 0 of those the t > n - window.  out = softmax(alpha q . k_t) v_t over these; zeros where there are none.  Head h of
  *   the queries goes with head h / (Hq / Hk) of the cache.  Sums and the softmax are held in fp32, the result is
- *   rounded once.  A row in a page that is not in the cache is NaN, and so is what a query that sees it gets; what a query does not see
+ *   rounded once.  In place (out = q) see GPUOS_CACHE_SUMS_BYTES.  A row in a page that is not in the cache is NaN, and so is what a query that sees it gets; what a query does not see
  *   changes nothing, nor does a row whose weight is below fp32's range.  What sees a code of E4M3 that is no number gets NaN: of a
  *   key's all of it, of a value's that element at least.
  *   No result depends on the order in which anything runs.
@@ -590,7 +590,9 @@ int gpuos_model_plan(const gpuos_model_task* task, uint32_t impl_id, uint32_t ou
  * These kernels have room beside a worker as those of gpuos_launch_model have. */
 int gpuos_launch_cache(int32_t device, const gpuos_cache_task* task, void* workspace, uint64_t workspace_bytes, void* stream);
 
-/* The workspace that a task needs, in bytes; 0 for most.  It depends on sizes alone.  No GPU needed. */
+/* The workspace that a task needs, in bytes; 0 for most.  It depends on sizes alone: an attention in place (out = q) with
+ * D > 128 needs GPUOS_CACHE_SUMS_BYTES, if that is more, and takes 2^26 - 8 heads of queries at most.  No GPU needed. */
+#define GPUOS_CACHE_SUMS_BYTES(B, S, Hq, D) (4ull * (B) * (S) * (Hq) * ((D) + 2))
 int gpuos_cache_workspace(const gpuos_cache_task* task, uint64_t* bytes);
 
 /* Flush, then block until `ticket` and every earlier ticket completed

@@ -176,7 +176,7 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
     most there may be) of sequence b, through pages [B, width], in caches and scales as cache_append_qkv fills them, Hq a
     multiple of their H, D a multiple of 8 up to 256, a scale for D or 32 elements and more.  The S queries are the last of those rows: each sees the
     rows up to its own, with window > 0 the last `window` of these.  scale: of the scores (None: 1 / sqrt(D)).  A query that
-    sees nothing gets zeros.  Not differentiable: what requires a gradient is refused where gradients are recorded."""
+    sees nothing gets zeros.  out may be q.  Not differentiable: what requires a gradient is refused where gradients are recorded."""
     longest, window = int(longest), int(window)
     given = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, out)      # in the descriptor's order
     key = (B or _load()).key(given), longest, window, scale if scale is None else float(scale)

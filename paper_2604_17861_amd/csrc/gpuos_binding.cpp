@@ -68,7 +68,7 @@ PyObject* launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const launch_t function = reinterpret_cast<launch_t>(PyLong_AsVoidPtr(a[0]));
   const long device = PyLong_AsLong(a[5]);
-  const long long space = PyLong_AsLongLong(a[6]);
+  long long space = PyLong_AsLongLong(a[6]);
   void* stream = PyLong_AsVoidPtr(a[7]);
   if (PyErr_Occurred()) return nullptr;
   try {
@@ -91,6 +91,10 @@ PyObject* launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
       task.operand[(int)places[i]].ptr = p;
       some = &t;
+    }
+    if (task.op == GPUOS_CACHE_ATTENTION && task.operand[0].ptr == task.operand[7].ptr && task.size[4] > 128) {
+      const long long sums = (long long)GPUOS_CACHE_SUMS_BYTES(task.size[0], task.size[1], task.size[2], task.size[4]);
+      if (space < sums) space = sums;
     }
     at::Tensor workspace;                                       // of the current stream: the allocator gives it to no other before that one is through
     if (space > 0 && some) workspace = at::empty({(int64_t)space}, some->options().dtype(at::kByte).requires_grad(false));

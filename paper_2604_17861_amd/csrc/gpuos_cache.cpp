@@ -24,6 +24,8 @@ int gpuos_launch_cache(int32_t device, const gpuos_cache_task* task, void* works
   uint64_t bytes = 0;
   const int rc = CachePack::attend(*task, &a, &format, &bytes, &empty);
   if (rc != GPUOS_OK || empty) return rc;
+  const uint64_t sums = a.joined ? (uint64_t)a.pieces * GPUOS_CACHE_SUMS_BYTES((uint64_t)a.b, a.s, a.hq, a.d) : 0;
+  if (bytes < sums) bytes = sums;
   if (bytes != 0 && (!workspace || (uint64_t)workspace % 16 != 0 || workspace_bytes < bytes)) return GPUOS_E_NOMEM;
   a.part = (uint64_t)workspace;
   a.stats = a.part + (uint64_t)a.pieces * a.b * a.s * a.hq * a.d * 4u;

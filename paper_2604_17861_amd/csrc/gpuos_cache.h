@@ -38,6 +38,7 @@ struct AttendArgs {
   uint32_t by_fours;                                 // scales of 32 elements each, side by side: read in fours
   uint32_t by_head, heads;                           // a wavefront has a head of its own: heads of keys in fours (else heads)
   uint32_t lg_parts;                                 // parts of a result that are a workgroup each: 1 or 2
+  uint32_t joined;                                   // a second launch makes the results out of the pieces' sums
   uint32_t blocks, inner;                            // workgroups, and how many that follow each other go to one die
   Div by_page, by_per, by_tiles, by_inner, by_pieces, by_rows, by_heads, by_hk, by_group;
   uint32_t dtype;
@@ -47,6 +48,8 @@ struct AttendArgs {
 constexpr uint32_t kAppendBlock = 2;       // heads of an item
 constexpr uint32_t kTileRows = 16;         // queries of a tile: a side of a matrix instruction's result
 constexpr uint32_t kTileTokens = 64;       // rows of the cache that a wavefront takes at once
+constexpr uint32_t kJoinThreads = 512;     // a workgroup of the second launch: a wavefront a query, or all of them
+constexpr int64_t kJoinedMost = (1 << 26) - 8;      // heads of queries that it takes, eight a workgroup: a grid of fewer than 2^32 threads
 constexpr uint32_t kPiecesMost = 256;      // (one sequence of 131,072 rows, 8 heads, in 128 / 256 / 384: 61, 44, 48 us, and 5.8, 7.1, 7.5 for joining)
 
 // Elements of a head that the kernel of a head's d has room for.
@@ -199,6 +202,9 @@ class CachePack : ModelPack {
     a->by_heads = make_div(a->heads);
     a->by_hk = make_div(a->hk);
     if (a->pieces > 1) *bytes = (uint64_t)a->pieces * b * s * hq * (d + 2) * 4;
+    // In place two workgroups that have a query's parts would read it and store over it: the second launch stores, as it does for pieces.
+    a->joined = a->pieces > 1 || (a->lg_parts != 0 && a->out == a->q) ? 1u : 0u;
+    if (a->joined && b * s * hq > kJoinedMost) return GPUOS_E_INVAL;
     return GPUOS_OK;
   }
 

@@ -810,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
     l = total;
   }
   if (!has_row || head >= a.hk) return;
-  const bool last = a.pieces == 1u;
+  const bool last = a.joined == 0u;
   query(qs, qh);
   const float inv = last ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
   const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(head * a.per + qh) * a.os[2]) * size_of(DT);
@@ -841,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
 // elements in lanes and every so many of the pieces, six on their way at a time (eight do not fit into
 // 64 registers).  2,048 queries of 128 elements, 6 pieces: 4.7 us (with a
 // workgroup each 7.6).
-constexpr uint32_t kJoinThreads = 512, kJoinWaves = kJoinThreads / 64, kJoinAhead = 6;
+constexpr uint32_t kJoinWaves = kJoinThreads / 64, kJoinAhead = 6;
 template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads, 8) gpuos_cache_join_kernel(const AttendArgs a) {
   __shared__ alignas(16) float weight[WIDE ? kPiecesMost : kJoinWaves * 64u], sums[WIDE ? kJoinWaves : 1][256], tops[kJoinWaves], totals[kJoinWaves];
   const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63u;
@@ -944,7 +944,7 @@ int launch_attend(const AttendArgs& a, uint32_t format, void* stream) {
   void* args[] = {(void*)&a};
   const uint32_t outer = (a.blocks / a.inner + 7u) / 8u * 8u;
   const int rc = (int)hipLaunchKernel(k.kernel, dim3(outer * a.inner), dim3(kThreads), args, k.lds, (hipStream_t)stream);
-  if (rc != (int)hipSuccess || a.pieces == 1u) return rc;
+  if (rc != (int)hipSuccess || a.joined == 0u) return rc;
   const void* const joins[] = {(const void*)gpuos_cache_join_kernel<GPUOS_F32, false>,  (const void*)gpuos_cache_join_kernel<GPUOS_F16, false>,
                                (const void*)gpuos_cache_join_kernel<GPUOS_BF16, false>, (const void*)gpuos_cache_join_kernel<GPUOS_F32, true>,
                                (const void*)gpuos_cache_join_kernel<GPUOS_F16, true>,   (const void*)gpuos_cache_join_kernel<GPUOS_BF16, true>};
