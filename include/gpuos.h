@@ -328,7 +328,7 @@ typedef struct gpuos_model_task {
  *   0 q [B,S,Hq,D]  1 keys' cache  2 their scales  3 values' cache  4 their scales  5 table [B, width], I32: page indexes,
  *   longest <= width * page, <= 2^30  6 lengths [B], I32 (none: longest; one over longest counts as it, one below 0 as 0)  7 out [B,S,Hq,D], q's dtype
  *   Sequence b has lengths[b] rows in the cache, the S queries' own last: query s is at n = lengths[b] - S + s and sees the rows t <= n,
- *   with a window above 0 of those the t > n - window.  out = softmax(alpha q . k_t) v_t over these; zeros where there are none.  Head h of
+ *   with a window above 0 of those the t > n - window.  out = softmax(alpha q . k_t) v_t over these; zeros where there are none, NaN where all scores are -inf.  Head h of
  *   the queries goes with head h / (Hq / Hk) of the cache.  Sums and the softmax are held in fp32, the result is
  *   rounded once.  In place (out = q) see GPUOS_CACHE_SUMS_BYTES.  A row in a page that is not in the cache is NaN, and so is what a query that sees it gets; what a query does not see
  *   changes nothing, nor does a row whose weight is below fp32's range.  What sees a code of E4M3 that is no number gets NaN: of a

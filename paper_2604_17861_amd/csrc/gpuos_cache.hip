@@ -347,6 +347,17 @@ DEV void wave_sync() {
 // not see there that a result of the exponential is waited for.)
 extern "C" __device__ float legacy_mul(float, float) __asm("llvm.amdgcn.fmul.legacy");
 
+// A sum of weights that is 0: of a query that sees nothing, whose result is 0; or of one all of whose scores are -inf, as the softmax has no
+// value there.  (The length is read again: kept, it would be one more register in the loop.)
+DEV float of_no_weights(const AttendArgs& a, uint32_t b, uint32_t s) {
+  int32_t len = (int32_t)a.longest;
+  if (a.lengths != 0) {
+    const int32_t l = ld<int32_t>(a.lengths + (uint64_t)b * a.ls * 4u);
+    len = l < 0 ? 0 : (l < len ? l : len);
+  }
+  return len - (int32_t)a.s + (int32_t)s >= 0 ? __builtin_nanf("") : 0.0f;
+}
+
 struct AttendPlace { uint32_t b, hk, tile, piece, part; bool there; };
 DEV AttendPlace attend_place(const AttendArgs& a) {
   // Workgroups go to the eight dies in turn; `inner` that follow each other here go to one (the rule is at the packing): heads that lie
@@ -812,7 +823,8 @@ __global__ void __launch_bounds__(kThreads, 4) gpuos_cache_attend_kernel(const A
   if (!has_row || head >= a.hk) return;
   const bool last = a.joined == 0u;
   query(qs, qh);
-  const float inv = last ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+  float inv = last ? 1.0f / l : 1.0f;
+  if (last && l == 0.0f) inv = of_no_weights(a, at.b, qs);
   const uint64_t op = a.out + ((uint64_t)at.b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(head * a.per + qh) * a.os[2]) * size_of(DT);
   const uint64_t all = (uint64_t)a.b * a.hk * a.rows, mine = ((uint64_t)at.b * a.hk + head) * a.rows + row, slice = (uint64_t)at.piece * all + mine;
   if (!last && g == 0u && at.part == 0u) {
@@ -911,9 +923,11 @@ template <uint32_t DT, bool WIDE> __global__ void __launch_bounds__(kJoinThreads
     for (uint32_t k = 0; k < kJoinWaves; ++k) sum += *(const f4*)&sums[k][e];
   }
   if (lane >= lanes || !has) return;
-  sum *= total == 0.0f ? 0.0f : 1.0f / total;
   const uint32_t pair = divided((uint32_t)mine, a.by_rows), row = (uint32_t)mine - pair * a.rows, b = divided(pair, a.by_hk), hk = pair - b * a.hk;
   const uint32_t qs = divided(row, a.by_per), qh = row - qs * a.per;
+  float inv = 1.0f / total;
+  if (total == 0.0f) inv = of_no_weights(a, b, qs);
+  sum *= inv;
   const uint64_t op = a.out + ((uint64_t)b * a.os[0] + (uint64_t)qs * a.os[1] + (uint64_t)(hk * a.per + qh) * a.os[2]) * size_of(DT);
   if (a.os[3] == 1u) st4<DT>(op + (uint64_t)e * size_of(DT), sum);
   else {
