@@ -143,7 +143,8 @@ class CachePack : ModelPack {
     return GPUOS_OK;
   }
 
-  // *bytes: what the pieces' sums take, 0 if there is one piece
+  // *bytes: what the pieces' sums take, 0 if there is one piece; by sizes alone, so that of the two ways to share out the heads (by_head) the one that
+  // has more pieces, whichever strides and dtypes choose
   static int attend(const gpuos_cache_task& t, AttendArgs* a, uint32_t* format, uint64_t* bytes, bool* empty) {
     memset(a, 0, sizeof(*a));
     *bytes = 0;
@@ -178,10 +179,12 @@ class CachePack : ModelPack {
     // Four heads of a row that lie together are read together, by a wavefront each, if their queries fit into LDS; else a workgroup has a head, and its
     // wavefronts every fourth 64 rows.  64 sequences of 4,096 rows of 8 heads of 128, int8: 134 and 162 us, 4 bits 75 and 80.  (Short ones are cut into
     // rows all the same: with a head each a wavefront has more of them behind each other.)
-    a->by_head = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
+    const bool few = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows;
+    a->by_head = few && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
     a->heads = a->by_head ? (a->hk + 3) / 4 : a->hk;
     const uint64_t pairs = (uint64_t)b * a->heads * a->tiles;
     a->pieces = pieces(pairs, (uint64_t)seen, a->by_head ? 128 : 512);
+    const uint32_t most = few ? pieces((uint64_t)b * ((a->hk + 3) / 4) * a->tiles, (uint64_t)seen, 128) : a->pieces;
     if (pairs * a->pieces > kBlocksMost) return GPUOS_E_INVAL;
     a->blocks = (uint32_t)(pairs * a->pieces);
     // All heads of a piece of a sequence go to one die, if the dies then have about as much to do; else all queries of a head; else each workgroup to the
@@ -201,7 +204,7 @@ class CachePack : ModelPack {
     a->by_rows = make_div(a->rows);
     a->by_heads = make_div(a->heads);
     a->by_hk = make_div(a->hk);
-    if (a->pieces > 1) *bytes = (uint64_t)a->pieces * b * s * hq * (d + 2) * 4;
+    if (most > 1) *bytes = (uint64_t)most * GPUOS_CACHE_SUMS_BYTES((uint64_t)b, s, hq, d);
     // In place two workgroups that have a query's parts would read it and store over it: the second launch stores, as it does for pieces.
     a->joined = a->pieces > 1 || (a->lg_parts != 0 && a->out == a->q) ? 1u : 0u;
     if (a->joined && b * s * hq > kJoinedMost) return GPUOS_E_INVAL;

@@ -31,3 +31,17 @@ def test_attention_in_place_of_more_queries_than_a_grid_of_the_second_launch_tak
     with pytest.raises(R.GpuosError) as e:
         R.cache_workspace(attention(hq=1, hk=1, s=2 ** 26, out=4096))
     assert e.value.status == R.E_INVAL
+
+
+@pytest.mark.parametrize("kw", (dict(hk=4, hq=4, d=128, longest=2048), dict(hk=8, hq=8, longest=2048), dict(hk=8, hq=8, b=64, d=128, longest=4096), dict(hk=8, hq=16, s=3, d=64, longest=700)))
+def test_a_workspace_depends_on_sizes_alone(kw):
+    """Heads behind places or before them, any dtype of the queries, any format."""
+    kw = dict(kw, pages=2 ** 20)
+    found = {(dtype, fmt, first): R.cache_workspace(attention(dtype=dtype, fmt=fmt, heads_first=first, **kw)) for dtype in (F32, F16, BF16) for fmt in (E2M1, I8) for first in (False, True)}
+    assert len(set(found.values())) == 1 and found[BF16, I8, False] > 0, found
+
+
+def test_a_workspace_holds_the_pieces_of_either_layout():
+    """In a head for each wavefront four heads of 2,048 rows are 16 pieces of 128 rows; otherwise they are four of 512, and what is asked for is enough."""
+    for first in (False, True):
+        assert R.cache_workspace(attention(hk=4, hq=4, d=128, longest=2048, heads_first=first)) == 16 * 4 * 130 * 4
