@@ -1,10 +1,11 @@
-"""Build libgpuos.so (HIP kernels + host runtime) for gfx950 and _binding.so (the module on PyTorch tensors), in-tree."""
+"""Build libgpuos.so (HIP kernels + host runtime) for gfx950 and, where PyTorch is installed, _binding.so (the module on its tensors), in-tree."""
 import importlib.util
 import os
 import subprocess
 import sys
 import sysconfig
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -26,15 +27,20 @@ def _older(made, deps):
 
 def needs_build():
     return (_older(LIB, [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)])
-            or _older(BINDING, [BINDING_SOURCE, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]))
+            or has_torch() and _older(BINDING, [BINDING_SOURCE, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]))
+
+
+def has_torch():
+    return importlib.util.find_spec("torch") is not None
 
 
 def binding_command():
     """The host compiler's command for the module, against the headers and libraries of the PyTorch that is installed."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
-    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
-    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1"] + ["-isystem" + i for i in include]
-            + ["-o", BINDING, BINDING_SOURCE, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    import torch
+    home = os.path.dirname(torch.__file__)
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi()] + ["-isystem" + i for i in include]
+            + ["-o", BINDING, BINDING_SOURCE, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def _all(jobs):
@@ -53,10 +59,13 @@ def build(force=True, verbose=False):
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = (["-Rpass-analysis=kernel-resource-usage"] if verbose else []) + [f for f in FLAGS if f not in ("-shared", "-ldl")]
-    with tempfile.TemporaryDirectory() as made:                 # (a source at a time would take as long as all of them: two to four minutes)
+    with tempfile.TemporaryDirectory() as made, ThreadPoolExecutor(1) as beside:      # (a source at a time would take as long as all of them: two to four minutes)
+        module = beside.submit(lambda: _all([binding_command()])) if has_torch() else None
         objects = [os.path.join(made, s + ".o") for s in SOURCES]
-        jobs = [[hipcc] + flags + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)] + [binding_command()]
+        jobs = [[hipcc] + flags + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)]
         out = _all(jobs) + _all([[hipcc, "--offload-arch=gfx950", "-shared", "-pthread", "-o", LIB] + objects + ["-ldl"]])
+        if module:                                              # (whatever becomes of it, the library is there)
+            out += module.result()
     if verbose or out.strip():
         print(out, file=sys.stderr)
     return LIB
