@@ -8,7 +8,6 @@ import torch
 from torch.autograd import forward_ad
 from torch.fx import _symbolic_trace
 
-from . import model as M
 from . import runtime as R
 from . import streams as S
 
@@ -115,8 +114,9 @@ def append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table=None
                   _caches_operand(v_cache), M._operand(v_scales)))
 
 
-def attention_task(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, out, *, scale, window=0):
+def attention_task(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, out, *, scale=None, window=0):
     """GPUOS_CACHE_ATTENTION as a descriptor (for runtime.launch_cache; it holds addresses, the caller keeps the tensors)."""
+    longest, window = int(longest), int(window)
     M._check(q, "q", M._FLOAT, (3, 4))
     dev = q.device
     M._check(k_cache, "k_cache", _CACHES, (4,), None, dev)
@@ -137,6 +137,7 @@ def attention_task(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, long
     M._need(group == d or (group >= 32 and group & (group - 1) == 0), "a scale is for the whole head or for a power of two of elements from 32 on, not %d", group)
     if lengths is not None:
         M._check(lengths, "lengths", M._INT, None, (b,), dev)
+    scale = float(scale) if scale is not None else d ** -0.5 if d else 1.0
     return _pack(ATTENTION, 0, (b, s, hq, hk, d, k_cache.shape[0], k_cache.shape[1], k_scales.shape[3], pages.shape[1], longest, min(window, 2 ** 31 - 1)),
                  (M._operand(qo), _caches_operand(k_cache), M._operand(k_scales), _caches_operand(v_cache), M._operand(v_scales), M._operand(pages),
                   M._operand(lengths), M._operand(oo)), scale)
@@ -187,8 +188,11 @@ def cache_attention(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, lon
     made = out is None
     operands = (q, k_cache, k_scales, v_cache, v_scales, pages, lengths, B.like(q)) if made else given
     if plan is None:
-        by = float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.shape[-1] else 1.0
-        task = _untraced(attention_task)(*operands[:7], longest, operands[7], scale=by, window=window)
+        task = _untraced(attention_task)(*operands[:7], longest, operands[7], scale=scale, window=window)
         plan = M._keep(key, _Plan(task, range(8), [] if made else [7], q.get_device(), q.numel() == 0))
     _run(plan, operands)
     return operands[7]
+
+
+# Behind the functions, because model takes them from here, whichever of the two is imported first.
+from . import model as M  # noqa: E402

@@ -10,8 +10,8 @@
 The functions launch the library's kernels on PyTorch's current stream of the tensors' device (gpuos_launch_model): they
 wait for nothing, and may be captured into a graph.  The `*_task` functions make the descriptors that the functions
 launch; `b"".join` of some goes to `Runtime.submit_model`, which runs them as tasks of the ring (bind the operators with
-`register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  (The last two are kernels only,
-gpuos_launch_cache.)  include/gpuos.h says what every operator computes and takes.
+`register` first), or to `runtime.launch_model`; they hold addresses, the caller keeps the tensors.  (The last two are kernels only:
+`runtime.launch_cache`, one descriptor with a workspace of `runtime.cache_workspace` bytes.)  include/gpuos.h says what every operator computes and takes.
 
 PyTorch sees no operators here.  norm_rope and norm_rope_qk are autograd functions; everything else is refused where a gradient would be
 lost, and so are second derivatives, forward mode and traces (make_fx, torch.export, torch.jit.trace).  torch.compile breaks its graph at a
@@ -536,3 +536,4 @@ def penalize_logits(x, *, history=None, prompt_lengths=None, params=None, bias=N
 
 # ---- a cache of 4 or 8 bits and the attention that reads it ------------------------------------------
 from ._cache import cache_append_qkv, cache_attention  # noqa: E402,F401
+from ._cache import append_task as cache_append_task, attention_task as cache_attention_task  # noqa: E402,F401
