@@ -475,7 +475,12 @@ void gpuos_default_config(gpuos_config* cfg);
  * memory, fine-grained coherent, mapped to the device), the device-side mirror
  * and operator table, and launch the persistent worker once.
  * queue_capacity: power of two in [2, 65536]; 0 => 4096 (the paper's default).
- * cfg: NULL => defaults on the current device.  *out receives the context. */
+ * cfg: NULL => defaults on the current device.  *out receives the context.
+ * The worker's stream lies on one of the process's few hardware queues, by the HIP runtime's choice, which depends on the streams
+ * that the process has used.  If that is the queue of another context's worker, the call waits until that worker has left: after its
+ * idle_exit_ms, or until it is stopped, by another thread (wait_timeout_ms does not bound this wait, which is inside the runtime).  So does
+ * gpuos_start_worker's kernel, and so does work on any stream of that queue.  A process with more than one context gives each an
+ * idle_exit_ms, or makes them all before it works on other streams. */
 int gpuos_init(gpuos_ctx** out, uint32_t queue_capacity, const gpuos_config* cfg);
 
 /* gpuos_init for callers that cannot allocate (harnesses that forbid hipMalloc /
