@@ -330,9 +330,11 @@ typedef struct gpuos_model_task {
  *   Sequence b has lengths[b] rows in the cache, the S queries' own last: query s is at n = lengths[b] - S + s and sees the rows t <= n,
  *   with a window above 0 of those the t > n - window.  out = softmax(alpha q . k_t) v_t over these; zeros where there are none, NaN where all scores are -inf.  Head h of
  *   the queries goes with head h / (Hq / Hk) of the cache.  Sums and the softmax are held in fp32, the result is
- *   rounded once.  In place (out = q) see GPUOS_CACHE_SUMS_BYTES.  A row in a page that is not in the cache is NaN, and so is what a query that sees it gets; what a query does not see
- *   changes nothing, nor does a row whose weight is below fp32's range.  What sees a code of E4M3 that is no number gets NaN: of a
- *   key's all of it, of a value's that element at least.
+ *   rounded once.  In place (out = q) see GPUOS_CACHE_SUMS_BYTES.  A row in a page that is not in the cache is NaN, and so is what a query
+ *   that sees it gets; what a query does not see changes nothing.  A row whose weight is below fp32's range adds nothing; where its value is no number or has an
+ *   infinite scale, whether the result is NaN depends on where the row lies.  What sees a code of E4M3 that is no number gets NaN: of a
+ *   key's all of it, of a value's (of a weight within fp32's range) that element at least.  (The weights that are summed are 2^8 at most: rows whose values
+ *   add up to over 2^120 leave fp32's range.)
  *   No result depends on the order in which anything runs.
  */
 enum gpuos_cache_op { GPUOS_CACHE_APPEND = 1, GPUOS_CACHE_ATTENTION = 2 };
@@ -479,8 +481,9 @@ void gpuos_default_config(gpuos_config* cfg);
  * The worker's stream lies on one of the process's few hardware queues, by the HIP runtime's choice, which depends on the streams
  * that the process has used.  If that is the queue of another context's worker, the call waits until that worker has left: after its
  * idle_exit_ms, or until it is stopped, by another thread (wait_timeout_ms does not bound this wait, which is inside the runtime).  So does
- * gpuos_start_worker's kernel, and so does work on any stream of that queue.  A process with more than one context gives each an
- * idle_exit_ms, or makes them all before it works on other streams. */
+ * gpuos_start_worker's kernel, and so does work on any stream of that queue.  gpuos_shutdown frees device memory, which waits for every
+ * kernel on the GPU, another context's worker among them.  A process with more than one context gives each an idle_exit_ms, and stops all
+ * workers before it shuts the first one down. */
 int gpuos_init(gpuos_ctx** out, uint32_t queue_capacity, const gpuos_config* cfg);
 
 /* gpuos_init for callers that cannot allocate (harnesses that forbid hipMalloc /

@@ -7,7 +7,6 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
-#include <vector>
 
 #include "../../include/gpuos.h"
 

@@ -47,7 +47,6 @@ struct AttendArgs {
 
 constexpr uint32_t kAppendBlock = 2;       // heads of an item
 constexpr uint32_t kTileRows = 16;         // queries of a tile: a side of a matrix instruction's result
-constexpr uint32_t kTileTokens = 64;       // rows of the cache that a wavefront takes at once
 constexpr uint32_t kJoinThreads = 512;     // a workgroup of the second launch: a wavefront a query, or all of them
 constexpr int64_t kJoinedMost = (1 << 26) - 8;      // heads of queries that it takes, eight a workgroup: a grid of fewer than 2^32 threads
 constexpr uint32_t kPiecesMost = 256;      // (one sequence of 131,072 rows, 8 heads, in 128 / 256 / 384: 61, 44, 48 us, and 5.8, 7.1, 7.5 for joining)
@@ -178,7 +177,8 @@ class CachePack : ModelPack {
     a->by_fours = a->group == 32 && a->kv[0].ss[3] == 1 && a->kv[1].ss[3] == 1 ? 1u : 0u;
     // Four heads of a row that lie together are read together, by a wavefront each, if their queries fit into LDS; else a workgroup has a head, and its
     // wavefronts every fourth 64 rows.  64 sequences of 4,096 rows of 8 heads of 128, int8: 134 and 162 us, 4 bits 75 and 80.  (Short ones are cut into
-    // rows all the same: with a head each a wavefront has more of them behind each other.)
+    // rows all the same: with a head each a wavefront has more of them behind each other.)  Pages of one place, whose stride stands for 0, count as heads apart;
+    // the limit of 3 heads is not measured (of 5, three wavefronts of eight have none).
     const bool few = hk >= 3 && seen > 512 && a->rows <= 2 * kTileRows;
     a->by_head = few && a->kv[0].cs[2] < a->kv[0].cs[1] && attend_lds(attend_room(a->d, q->dtype), q->dtype, groups > 1, true) <= kLdsMost ? 1u : 0u;
     a->heads = a->by_head ? (a->hk + 3) / 4 : a->hk;

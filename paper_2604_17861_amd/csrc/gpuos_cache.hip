@@ -276,8 +276,11 @@ int launch_append(const AppendArgs& a, void* stream) {
 //
 // A workgroup has up to 16 queries that share a head of keys and a piece of the sequence; each of its four wavefronts takes 64 rows of the
 // cache at a time.  Both products are matrix instructions of 16 x 16 x 32 on bf16.  Codes of all formats are bf16 numbers as they stand,
-// so what is multiplied is exact: a row's scale goes onto the sum of a group's products (keys) or onto p (values), in fp32; p and q of
-// more than 8 bits go in as two or three bf16 numbers that add up to them.
+// so what is multiplied is exact: a row's scale goes onto the sum of a group's products (keys) or onto p (values), in fp32; a q of 16 or 32 bits goes in
+// as two or three bf16 numbers that add up to it, and so does p times its scale for results of 32 bits, as three.  For results of 16 bits it goes in as two, the
+// first cut off and the second rounded, within 2^-16 of it: a 256th of half a step of bf16, a 32nd of one of fp16; a third part would be a third more matrix
+// instructions for bf16, a quarter for fp16.  Of 1,000 results of bf16 3 to 6, of fp16 22, are then rounded to the other neighbour than from sums of torch in 32 bits, and the
+// error against 64 bits is the same to four digits (1.66e-3 and 2.07e-4 of the norm).
 // The first product is K Q^T: lane (n, g) then holds the scores of query n and rows 4 g .. 4 g + 3 of either half, and these eight are the
 // inputs of its part of the second, V^T P^T, if the rows are summed in that order: scores never change lanes, and a query's maximum, sum and
 // results are all in lanes of its number.  64 rows go at a time, four tiles of the first product, two steps of the second.
