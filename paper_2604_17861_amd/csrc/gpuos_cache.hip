@@ -78,7 +78,8 @@ template <uint32_t DT> DEV void st4(uint64_t p, f4 f) {
 // list, chosen by lanes, an item took 600 vector instructions, and those were what bounded it: 16,384 tokens of 32 + 8 + 8 heads of 128 bf16
 // into 4 bits 103 us, so 82 (364 MB, 4.4 TB/s; a large copy makes 5.0); 8,192 of 16 + 16 + 16 of fp16 into e4m3 56 and 37.6 (170 MB, 4.5).  A token of
 // 32 heads 4.2 us: three trips to memory.  Blocks of four heads instead of two cost a token 1.6 us and gain nothing, stores past
-// the caches neither.
+// the caches neither.  Element by element the 16,384 tokens take 546 us (a last dim of every second element; eight loads and addresses in place of one); heads
+// of 100 318.
 // ---------------------------------------------------------------------------
 // eight codes of |y| <= qmax (1 + 2^-23): to the nearest, to the even one of two
 DEV u2 encode(const float* y, uint32_t format) {
@@ -290,7 +291,7 @@ int launch_append(const AppendArgs& a, void* stream) {
 // and end: lengths, page table, keys, values, each a trip to memory behind the other.  131,072 rows of one (a scale for 32 elements, 168 MB) 43 and 6.  A
 // request of 301 rows 8.8.  A second slab on its way made no difference.
 // Prompts: bound by vector instructions, some 430 for 64 rows and 16 queries (a third conversions), 48 matrix instructions beside them: 1,024 queries of
-// 32 heads, the last of 4,096 rows, 135 us, 450 TFLOP/s; 4 of those 515.  (Four wavefronts that share what one of them has converted, as bf16 in LDS, were no
+// 32 heads, the last of 4,096 rows, 128 us, 470 TFLOP/s; 4 of those 515.  (Four wavefronts that share what one of them has converted, as bf16 in LDS, were no
 // faster: 326 and 512; two barriers for 64 rows cost what the conversions do.)
 // ---------------------------------------------------------------------------
 template <uint32_t FMT> struct Code { static constexpr uint32_t BITS = FMT == CF_E2M1 ? 4u : 8u; };
