@@ -115,7 +115,8 @@ def append_task(q, k, v, slots, k_cache, k_scales, v_cache, v_scales, table=None
 
 
 def attention_task(q, k_cache, k_scales, v_cache, v_scales, pages, lengths, longest, out, *, scale=None, window=0):
-    """GPUOS_CACHE_ATTENTION as a descriptor (for runtime.launch_cache; it holds addresses, the caller keeps the tensors)."""
+    """GPUOS_CACHE_ATTENTION as a descriptor (for runtime.launch_cache; it holds addresses, the caller keeps the tensors).  Its workspace has
+    runtime.cache_workspace bytes, with out = q and D > 128 at least 4 B S Hq (D + 2)."""
     longest, window = int(longest), int(window)
     M._check(q, "q", M._FLOAT, (3, 4))
     dev = q.device

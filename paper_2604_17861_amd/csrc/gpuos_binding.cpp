@@ -4,6 +4,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
@@ -70,7 +71,7 @@ PyObject* launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
   long long space = PyLong_AsLongLong(a[6]);
   void* stream = PyLong_AsVoidPtr(a[7]);
   if (PyErr_Occurred()) return nullptr;
-  try {
+  HANDLE_TH_ERRORS                                              // (out of memory, and what a dispatch mode raises, as from any other function of PyTorch's)
     gpuos_cache_task task;
     memcpy(&task, PyBytes_AS_STRING(a[1]), sizeof task);
     const char* places = PyBytes_AS_STRING(a[2]);
@@ -105,10 +106,7 @@ PyObject* launch(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
     }
     return PyLong_FromLong(rc);
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
+  END_HANDLE_TH_ERRORS
 }
 
 // like(tensor): an empty tensor of its shape, dtype and device, without strides of its own.
@@ -117,13 +115,10 @@ PyObject* like(PyObject*, PyObject* o) {
     PyErr_SetString(PyExc_TypeError, "a tensor");
     return nullptr;
   }
-  try {
+  HANDLE_TH_ERRORS
     const at::Tensor& t = THPVariable_Unpack(o);
     return THPVariable_Wrap(at::empty(t.sizes(), t.options().requires_grad(false)));
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
+  END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {{"key", key, METH_O, "a call's tensors without their addresses"},

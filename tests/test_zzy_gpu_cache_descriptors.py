@@ -1,8 +1,9 @@
-"""The cache operators' descriptors as what a program makes and launches itself."""
+"""The cache operators' descriptors as what a program makes and launches itself; what goes wrong inside a call."""
 import pytest
 import torch
 
 from paper_2604_17861_amd import model as M
+from paper_2604_17861_amd import _binding as B
 from paper_2604_17861_amd import runtime as R
 from paper_2604_17861_amd import streams as S
 from test_gpu_model import BF16
@@ -34,3 +35,9 @@ def test_descriptors_do_what_the_functions_do(d, longest):
     assert torch.equal(out, want)
     run(M.cache_attention_task(into, *mine, pages, lengths, longest, into), 4 * 2 * 3 * 8 * (d + 2))      # in place
     assert torch.equal(into, want)
+
+
+def test_no_memory_is_an_error_of_its_own():
+    x = torch.zeros(1, device="cuda").expand(2 ** 44)        # (64 TB: refused at once)
+    with pytest.raises(torch.OutOfMemoryError):
+        B.like(x)
